@@ -419,6 +419,86 @@ typedef struct {
 int kvcomm_align_kv_q8_batch(const kvcomm_model *model, int32_t gran, kvcomm_tensor anchor_layout,
                              const kvcomm_align_q8_job *jobs, int32_t n_jobs, void *stream);
 
+/* --------------------------------------------------------------------------------------
+ * The suffix's own queries, keys and values (workflow step 4; q, k, v as in Sec. 3.1) from a layer's projections:
+ * what kvcomm_suffix_attn expects to be stored already.  Token i (0 <= i < n_tokens) stands at position
+ * first_pos + i; with a norm (norm_eps > 0) every head's query and key is first divided by its root mean square:
+ *   x'              = norm_eps > 0 ?  x / sqrt(mean_c x[c]^2 + norm_eps) * weight[c]  :  x
+ *   q_out[l,h,i,:]  = R(first_pos + i) q'[l,h,i,:]      k_out likewise      v_out[l,h,i,:] = v[l,h,i,:]
+ * with R as in kvcomm_align_kv.  fp32 arithmetic (angles in double), one rounding at the store.
+ *
+ *   q, q_out             [L, Hq, n_tokens, D]; k, k_out, v, v_out [L, Hkv, n_tokens, D].  The inputs are normally
+ *                        strided views of one projection [token, head, channel], k_out and v_out views of the agent's
+ *                        cache at the suffix's rows.  A pair whose two pointers are NULL is left out (at least one is given).
+ *   q_weight, k_weight   DEVICE [L, D] of the model's type, or NULL (ones); layer l's begins at element l * stride
+ *                        (0: one for all layers; pointer and stride aligned like a tensor's).  Only with a norm and its pair.
+ * An output may be exactly its own input (same pointer and strides); any other sharing of bytes between an output and
+ * another tensor of the call returns KVCOMM_EINVAL (whole (layer, head) blocks are compared, first to last token: queries that lie
+ * token by token beside the keys cannot be rotated in place).
+ * Errors: KVCOMM_EINVAL / KVCOMM_EUNSUPPORTED as above; KVCOMM_EINVAL for n_tokens <= 0, positions beyond INT32_MAX,
+ * norm_eps negative, infinite or NaN, a weight without a norm or without its tensor.       */
+int kvcomm_place_qkv(const kvcomm_model *model, kvcomm_tensor q, kvcomm_tensor k, kvcomm_tensor v,
+                     int32_t n_tokens, int32_t first_pos,
+                     const void *q_weight, const void *k_weight, int64_t q_weight_stride, int64_t k_weight_stride,
+                     float norm_eps, kvcomm_tensor q_out, kvcomm_tensor k_out, kvcomm_tensor v_out, void *stream);
+
+/* --------------------------------------------------------------------------------------
+ * A cache held in 4 bits per value (the appendix on memory cost: the caches of the agents are what fills the memory).
+ * 32 neighbouring channels of a row share a scale 2^(byte - 127); a value is one OCP 4-bit floating-point code (E2M1): bit 3 the
+ * sign, codes 0 ... 7 the sizes 0, 0.5, 1, 1.5, 2, 3, 4, 6; value = scale * size.  17 bytes per 32 values.  LOSSY.
+ *   codes    [L, Hkv, n, D/2] bytes, channel 2c in the low half of byte c, strides in bytes; pointer 16-byte aligned,
+ *            strides multiples of 16.
+ *   scales   [L, Hkv, n, D/32] bytes, strides in bytes; pointer and strides multiples of D/32.
+ * A scale byte of 255 stands for a block of NaN; 0 and 1 are read as 2^-127 and 2^-126, whose smallest values (below 2^-126)
+ * a bf16 attention may take as 0.
+ *
+ * kvcomm_quantize_kv4: n_tokens rows of keys and values [L, Hkv, n_tokens, D] into their rows of a compact cache.  The scale of a
+ * block is the least power of two with max|x| <= 7 * scale, between 2^-125 and 2^125; x / scale is rounded to the nearest size,
+ * ties to the even code, so |error| <= scale (half the top step), and what lies beyond 7 * 2^125 saturates.  A block with a NaN or an infinity
+ * gets byte 255.  Reproducible bit for bit.
+ * kvcomm_dequantize_kv4: the values back, exact in either type (below 2^-126: subnormal).
+ * Errors as for kvcomm_capture_offsets; KVCOMM_EINVAL where an output shares bytes with another tensor of the call.  */
+typedef struct {
+    kvcomm_tensor codes, scales;
+} kvcomm_tensor4;
+
+int kvcomm_quantize_kv4(const kvcomm_model *model, kvcomm_tensor k, kvcomm_tensor v, int32_t n_tokens,
+                        kvcomm_tensor4 out_k, kvcomm_tensor4 out_v, void *stream);
+
+int kvcomm_dequantize_kv4(const kvcomm_model *model, kvcomm_tensor4 k, kvcomm_tensor4 v, int32_t n_tokens,
+                          kvcomm_tensor out_k, kvcomm_tensor out_v, void *stream);
+
+/* --------------------------------------------------------------------------------------
+ * kvcomm_suffix_attn over a compact cache: cache_k / cache_v hold the n_ctx + tq tokens in 4 bits, q and out are of the model's
+ * type, bf16 (f32 models: KVCOMM_EUNSUPPORTED).  Decoded values are exact in bf16; from there on the arithmetic is that of
+ * kvcomm_suffix_attn's bf16 path.  lse_out, softmax_scale, workspace (kvcomm_suffix_attn_kv4_workspace() bytes, 16-byte aligned,
+ * or none) and errors as there.  A key that a query does not see has no influence on it, whatever it holds.        */
+size_t kvcomm_suffix_attn_kv4_workspace(const kvcomm_model *model, int32_t n_ctx, int32_t tq);
+
+int kvcomm_suffix_attn_kv4(const kvcomm_model *model, kvcomm_tensor q,
+                           kvcomm_tensor4 cache_k, kvcomm_tensor4 cache_v,
+                           int32_t n_ctx, int32_t tq, float softmax_scale,
+                           kvcomm_tensor out, float *lse_out,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
+/* --------------------------------------------------------------------------------------
+ * kvcomm_suffix_attn with a sliding window and sinks: suffix query i, at position p = n_ctx + i, attends to the last `window` tokens
+ * up to its own and to the cache's first n_sinks tokens,
+ *   token j is seen  iff  j <= p  and  (j > p - window  or  j < n_sinks).
+ * window >= 1 (a query always sees itself; window >= n_ctx + tq is kvcomm_suffix_attn), n_sinks >= 0.  The cache is laid out as there;
+ * rows that no query sees are not looked at, or without influence, whatever they hold: a stream may have dropped them.  Time goes by the
+ * keys that are seen, not by the length of the cache.  f32 and bf16, lse_out, softmax_scale, workspace
+ * (kvcomm_suffix_attn_window_workspace() bytes, 16-byte aligned, or none) and errors as for kvcomm_suffix_attn; KVCOMM_EINVAL for
+ * window <= 0 or n_sinks < 0.                                                              */
+size_t kvcomm_suffix_attn_window_workspace(const kvcomm_model *model, int32_t n_ctx, int32_t tq,
+                                           int32_t window, int32_t n_sinks);
+
+int kvcomm_suffix_attn_window(const kvcomm_model *model, kvcomm_tensor q,
+                              kvcomm_tensor cache_k, kvcomm_tensor cache_v,
+                              int32_t n_ctx, int32_t tq, int32_t window, int32_t n_sinks, float softmax_scale,
+                              kvcomm_tensor out, float *lse_out,
+                              void *workspace, size_t workspace_bytes, void *stream);
+
 /* Human-readable name of a kvcomm_status; never NULL. */
 const char *kvcomm_status_string(int status);
 

@@ -12,7 +12,8 @@ from .binding import (  # noqa: F401
     kvcomm_anchor_weights_batch, kvcomm_anchor_weights_batch_workspace,
     kvcomm_anchor_weights_rule, kvcomm_anchor_weights_rule_workspace, kvcomm_anchor_weights_static,
     kvcomm_anchor_weights_static_capacity, kvcomm_anchor_weights_workspace,
-    kvcomm_capture_offsets, kvcomm_quantize_deltas, kvcomm_suffix_attn, kvcomm_suffix_attn_confined,
-    kvcomm_suffix_attn_confined_ws, kvcomm_suffix_attn_workspace, kvcomm_weight_slots, library_path,
+    kvcomm_capture_offsets, kvcomm_dequantize_kv4, kvcomm_place_qkv, kvcomm_quantize_deltas, kvcomm_quantize_kv4, kvcomm_suffix_attn,
+    kvcomm_suffix_attn_confined, kvcomm_suffix_attn_confined_ws, kvcomm_suffix_attn_kv4, kvcomm_suffix_attn_kv4_workspace,
+    kvcomm_suffix_attn_window, kvcomm_suffix_attn_window_workspace, kvcomm_suffix_attn_workspace, kvcomm_weight_slots, library_path,
     load_library,
 )

@@ -54,6 +54,10 @@ class _CTensor(ctypes.Structure):
                 ("stride_token", ctypes.c_int64)]
 
 
+class _CTensor4(ctypes.Structure):
+    _fields_ = [("codes", _CTensor), ("scales", _CTensor)]
+
+
 class _CAlignJob(ctypes.Structure):
     _fields_ = [("base_k", _CTensor), ("base_v", _CTensor), ("out_k", _CTensor), ("out_v", _CTensor),
                 ("seg_len", ctypes.c_int32), ("delta_pos", ctypes.c_int32),
@@ -126,7 +130,9 @@ def _load_native(lib):
 _NATIVE_CALLS = ("kvcomm_weight_slots", "kvcomm_suffix_attn_workspace", "kvcomm_anchor_weights_rule",
                  "kvcomm_anchor_weights_batch", "kvcomm_align_kv_batch", "kvcomm_align_kv_batch_beside", "kvcomm_align_kv_q8_batch", "kvcomm_align_kv",
                  "kvcomm_align_kv_q8", "kvcomm_suffix_attn", "kvcomm_suffix_attn_confined_ws", "kvcomm_anchor_predict",
-                 "kvcomm_capture_offsets", "kvcomm_quantize_deltas")
+                 "kvcomm_capture_offsets", "kvcomm_quantize_deltas", "kvcomm_place_qkv", "kvcomm_quantize_kv4", "kvcomm_dequantize_kv4",
+                 "kvcomm_suffix_attn_kv4_workspace", "kvcomm_suffix_attn_kv4", "kvcomm_suffix_attn_window_workspace",
+                 "kvcomm_suffix_attn_window")
 
 
 def library_path():
@@ -198,6 +204,21 @@ def load_library():
     lib.kvcomm_align_kv_q8.restype = ctypes.c_int
     lib.kvcomm_align_kv_q8_batch.argtypes = [mp, i32, _CTensor, ctypes.POINTER(_CAlignQ8Job), i32, vp]
     lib.kvcomm_align_kv_q8_batch.restype = ctypes.c_int
+    i64 = ctypes.c_int64
+    lib.kvcomm_place_qkv.argtypes = [mp, _CTensor, _CTensor, _CTensor, i32, i32, vp, vp, i64, i64, f32, _CTensor, _CTensor, _CTensor, vp]
+    lib.kvcomm_place_qkv.restype = ctypes.c_int
+    lib.kvcomm_quantize_kv4.argtypes = [mp, _CTensor, _CTensor, i32, _CTensor4, _CTensor4, vp]
+    lib.kvcomm_quantize_kv4.restype = ctypes.c_int
+    lib.kvcomm_dequantize_kv4.argtypes = [mp, _CTensor4, _CTensor4, i32, _CTensor, _CTensor, vp]
+    lib.kvcomm_dequantize_kv4.restype = ctypes.c_int
+    lib.kvcomm_suffix_attn_kv4_workspace.argtypes = [mp, i32, i32]
+    lib.kvcomm_suffix_attn_kv4_workspace.restype = sz
+    lib.kvcomm_suffix_attn_kv4.argtypes = [mp, _CTensor, _CTensor4, _CTensor4, i32, i32, f32, _CTensor, vp, vp, sz, vp]
+    lib.kvcomm_suffix_attn_kv4.restype = ctypes.c_int
+    lib.kvcomm_suffix_attn_window_workspace.argtypes = [mp, i32, i32, i32, i32]
+    lib.kvcomm_suffix_attn_window_workspace.restype = sz
+    lib.kvcomm_suffix_attn_window.argtypes = [mp, _CTensor, _CTensor, _CTensor, i32, i32, i32, i32, f32, _CTensor, vp, vp, sz, vp]
+    lib.kvcomm_suffix_attn_window.restype = ctypes.c_int
     lib.kvcomm_status_string.argtypes = [ctypes.c_int]
     lib.kvcomm_status_string.restype = ctypes.c_char_p
     lib.kvcomm_version.argtypes = []
@@ -787,3 +808,170 @@ def kvcomm_align_kv_q8_batch(model, jobs, gran=W_TOKEN, stream=None):
     _check(lib.kvcomm_align_kv_q8_batch(ctypes.byref(model.c()), gran,
                                         layout if layout is not None else _CTensor(None, 0, 0, 0), cjobs, n,
                                         _stream_ptr(stream)))
+
+
+def _sized(t, dtype, shape, what):
+    """Descriptor of a tensor of exactly this shape."""
+    d = _desc(t, dtype, what)
+    if tuple(t.shape) != shape:
+        raise KVCommError(EINVAL, f"{what}: expected shape {shape}, not {tuple(t.shape)}")
+    return d
+
+
+def _on_stream_of(tensors, stream):
+    """The stream's handle, if the tensors of a call all lie on its device."""
+    dev = getattr(stream, "device_index", None)
+    dev = torch.cuda.current_device() if dev is None else dev
+    if any(t is not None and (not t.is_cuda or t.get_device() != dev) for t in tensors):
+        raise KVCommError(EINVAL, f"all tensors of a call have to lie on the device of its stream ({dev})")
+    return _stream_ptr(stream)
+
+
+def _compact(model, pair, n, what):
+    """(codes, scales) of a tensor in 4 bits -> descriptor."""
+    codes, scales = pair
+    head = (model.n_layers, model.n_kv_heads, n)
+    return _CTensor4(_sized(codes, torch.uint8, head + (model.head_dim // 2,), what + " codes"),
+                     _sized(scales, torch.uint8, head + (model.head_dim // 32,), what + " scales"))
+
+
+def _new_compact(model, n, device):
+    head = (model.n_layers, model.n_kv_heads, n)
+    return (torch.empty(head + (model.head_dim // 2,), dtype=torch.uint8, device=device),
+            torch.empty(head + (model.head_dim // 32,), dtype=torch.uint8, device=device))
+
+
+def kvcomm_place_qkv(model, q, k, v, first_pos, q_out=None, k_out=None, v_out=None, q_weight=None, k_weight=None, norm_eps=0.0, stream=None):
+    """Projections of a suffix q [L,Hq,n,D], k, v [L,Hkv,n,D] -> (q_out, k_out, v_out): per-head RMS norm of q and k where norm_eps > 0 (times
+    q_weight, k_weight [D] or [L, D]), rotation of token i to position first_pos + i, v copied.  k_out and v_out are normally views of the agent's
+    cache; outputs that are not passed are made.  None in the place of q, k or v leaves it out."""
+    lib = load_library()
+    ins, outs = [q, k, v], [q_out, k_out, v_out]
+    for i, x in enumerate(ins):
+        if x is not None and outs[i] is None:
+            with on_stream(stream):
+                outs[i] = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if _done(_native.place_qkv(model, q, k, v, first_pos, q_weight, k_weight, norm_eps, outs[0], outs[1], outs[2], stream)):
+        return tuple(outs)
+    n = next((x.shape[2] for x in ins if x is not None), 0)
+    none = _CTensor(None, 0, 0, 0)
+    cin, cout = [none] * 3, [none] * 3
+    for i, (x, y, what) in enumerate(zip(ins, outs, "qkv")):
+        if (x is None) != (y is None):
+            raise KVCommError(EINVAL, f"{what}_out without {what}")
+        if x is not None:
+            shape = (model.n_layers, model.n_kv_heads if i else model.n_q_heads, n, model.head_dim)
+            cin[i], cout[i] = _sized(x, model.dtype, shape, what), _sized(y, model.dtype, shape, what + "_out")
+    weights = []
+    for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None and (w.dtype != model.dtype or not w.is_cuda or w.stride(-1) != 1 or
+                              tuple(w.shape) not in ((model.head_dim,), (model.n_layers, model.head_dim))):
+            raise KVCommError(EINVAL, f"{what}: expected a {model.dtype} device tensor [D] or [L, D] with contiguous channels")
+        weights.append((None, 0) if w is None else (w.data_ptr(), w.stride(0) if w.dim() == 2 else 0))
+    _check(lib.kvcomm_place_qkv(ctypes.byref(model.c()), *cin, n, int(first_pos), weights[0][0], weights[1][0], weights[0][1], weights[1][1],
+                                float(norm_eps), *cout, _on_stream_of((*ins, *outs, q_weight, k_weight), stream)))
+    return tuple(outs)
+
+
+def kvcomm_quantize_kv4(model, k, v, out_k=None, out_v=None, stream=None):
+    """Rows of keys and values [L,Hkv,n,D] -> (codes [L,Hkv,n,D/2], scales [L,Hkv,n,D/32]) of each, uint8 (made if not passed): a compact cache's
+    rows, 4 bits per value and a power-of-two scale per 32 channels."""
+    lib = load_library()
+    n = k.shape[2]
+    with on_stream(stream) if out_k is None or out_v is None else contextlib.nullcontext():
+        out_k = _new_compact(model, n, k.device) if out_k is None else out_k
+        out_v = _new_compact(model, n, k.device) if out_v is None else out_v
+    if _done(_native.quantize_kv4(model, k, v, out_k, out_v, stream)):
+        return out_k, out_v
+    shape = (model.n_layers, model.n_kv_heads, n, model.head_dim)
+    _check(lib.kvcomm_quantize_kv4(ctypes.byref(model.c()), _sized(k, model.dtype, shape, "k"), _sized(v, model.dtype, shape, "v"), n,
+                                   _compact(model, out_k, n, "out_k"), _compact(model, out_v, n, "out_v"),
+                                   _on_stream_of((k, v, *out_k, *out_v), stream)))
+    return out_k, out_v
+
+
+def kvcomm_dequantize_kv4(model, k, v, out_k=None, out_v=None, stream=None):
+    """The values [L,Hkv,n,D] that compact keys and values (each a pair of codes and scales) hold, in the model's type."""
+    lib = load_library()
+    n = k[0].shape[2]
+    shape = (model.n_layers, model.n_kv_heads, n, model.head_dim)
+    with on_stream(stream) if out_k is None or out_v is None else contextlib.nullcontext():
+        out_k = torch.empty(shape, dtype=model.dtype, device=k[0].device) if out_k is None else out_k
+        out_v = torch.empty(shape, dtype=model.dtype, device=k[0].device) if out_v is None else out_v
+    if _done(_native.dequantize_kv4(model, k, v, out_k, out_v, stream)):
+        return out_k, out_v
+    _check(lib.kvcomm_dequantize_kv4(ctypes.byref(model.c()), _compact(model, k, n, "k"), _compact(model, v, n, "v"), n,
+                                     _sized(out_k, model.dtype, shape, "out_k"), _sized(out_v, model.dtype, shape, "out_v"),
+                                     _on_stream_of((*k, *v, out_k, out_v), stream)))
+    return out_k, out_v
+
+
+def kvcomm_suffix_attn_kv4_workspace(model, n_ctx, tq):
+    return int(load_library().kvcomm_suffix_attn_kv4_workspace(ctypes.byref(model.c()), int(n_ctx), int(tq)))
+
+
+def kvcomm_suffix_attn_window_workspace(model, n_ctx, tq, window, n_sinks=0):
+    return int(load_library().kvcomm_suffix_attn_window_workspace(ctypes.byref(model.c()), int(n_ctx), int(tq), int(window), int(n_sinks)))
+
+
+def _attn_outputs(q, out, lse_out, want_lse, stream):
+    if out is None or (want_lse and lse_out is None):
+        with on_stream(stream):
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+            if want_lse and lse_out is None:
+                lse_out = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
+    return out, lse_out
+
+
+def _attn_checked(model, q, out, lse_out, workspace):
+    """(descriptor of q, of out, pointer of lse_out, pointer and bytes of workspace) of a call that the native module declined."""
+    shape = (model.n_layers, model.n_q_heads, q.shape[2], model.head_dim)
+    cq, cout = _sized(q, model.dtype, shape, "q"), _sized(out, model.dtype, shape, "out")
+    if lse_out is not None and (lse_out.dtype != torch.float32 or not lse_out.is_cuda or not lse_out.is_contiguous() or
+                                lse_out.numel() != shape[0] * shape[1] * shape[2]):
+        raise KVCommError(EINVAL, "lse_out: expected a contiguous fp32 device tensor [L, Hq, tq]")
+    ws = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    return cq, cout, None if lse_out is None else lse_out.data_ptr(), ws
+
+
+def kvcomm_suffix_attn_kv4(model, q, cache_k, cache_v, n_ctx, softmax_scale=0.0, out=None, lse_out=None, want_lse=False, stream=None,
+                           workspace=None):
+    """kvcomm_suffix_attn over a compact cache: cache_k / cache_v are pairs of codes [L,Hkv,n_ctx+Tq,D/2] and scales [L,Hkv,n_ctx+Tq,D/32].
+
+    workspace: kvcomm_suffix_attn_kv4_workspace() bytes on the device (made here if not given)."""
+    lib = load_library()
+    tq = q.shape[2]
+    out, lse_out = _attn_outputs(q, out, lse_out, want_lse, stream)
+    if workspace is None:
+        need = _native.suffix_attn_kv4_workspace(model, n_ctx, tq)
+        need = kvcomm_suffix_attn_kv4_workspace(model, n_ctx, tq) if need is None else need
+        workspace = _attn_scratch(need, q.device, stream) if need else None
+    if not _done(_native.suffix_attn_kv4(model, q, cache_k, cache_v, n_ctx, softmax_scale, out, lse_out, workspace, stream)):
+        cq, cout, lse, ws = _attn_checked(model, q, out, lse_out, workspace)
+        N = int(n_ctx) + tq
+        _check(lib.kvcomm_suffix_attn_kv4(ctypes.byref(model.c()), cq, _compact(model, cache_k, N, "cache_k"), _compact(model, cache_v, N, "cache_v"),
+                                          int(n_ctx), tq, float(softmax_scale), cout, lse, *ws,
+                                          _on_stream_of((q, *cache_k, *cache_v, out, lse_out, workspace), stream)))
+    return (out, lse_out) if want_lse else out
+
+
+def kvcomm_suffix_attn_window(model, q, cache_k, cache_v, n_ctx, window, n_sinks=0, softmax_scale=0.0, out=None, lse_out=None, want_lse=False,
+                              stream=None, workspace=None):
+    """kvcomm_suffix_attn where the query at position p sees the tokens (p - window, p] and the cache's first n_sinks tokens.
+
+    workspace: kvcomm_suffix_attn_window_workspace() bytes on the device (made here if not given)."""
+    lib = load_library()
+    tq = q.shape[2]
+    out, lse_out = _attn_outputs(q, out, lse_out, want_lse, stream)
+    if workspace is None:
+        need = _native.suffix_attn_window_workspace(model, n_ctx, tq, window, n_sinks)
+        need = kvcomm_suffix_attn_window_workspace(model, n_ctx, tq, window, n_sinks) if need is None else need
+        workspace = _attn_scratch(need, q.device, stream) if need else None
+    if not _done(_native.suffix_attn_window(model, q, cache_k, cache_v, n_ctx, window, n_sinks, softmax_scale, out, lse_out, workspace, stream)):
+        cq, cout, lse, ws = _attn_checked(model, q, out, lse_out, workspace)
+        shape = (model.n_layers, model.n_kv_heads, int(n_ctx) + tq, model.head_dim)
+        _check(lib.kvcomm_suffix_attn_window(ctypes.byref(model.c()), cq, _sized(cache_k, model.dtype, shape, "cache_k"),
+                                             _sized(cache_v, model.dtype, shape, "cache_v"), int(n_ctx), tq, int(window), int(n_sinks),
+                                             float(softmax_scale), cout, lse, *ws,
+                                             _on_stream_of((q, cache_k, cache_v, out, lse_out, workspace), stream)))
+    return (out, lse_out) if want_lse else out

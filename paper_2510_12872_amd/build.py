@@ -9,6 +9,8 @@ import os
 import shutil
 import subprocess
 import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
@@ -19,11 +21,11 @@ MARSHAL = os.path.join(_HERE, "_marshal.so")
 PROBE_SRC = os.path.join(_HERE, "tools", "hbm_stream_probe.hip")
 PROBE = os.path.join(_HERE, "tools", "hbm_stream_probe")
 SOURCES = ["align_kv.hip", "anchor_weights.hip", "anchor_update.hip", "delta_q8.hip", "suffix_attn.hip",
-           "attn_rows.hip", "attn_f32.hip", "status.hip"]
+           "attn_rows.hip", "attn_f32.hip", "attn_window.hip", "kv4.hip", "place_qkv.hip", "status.hip"]
 
 # -packed-fp32-ops: keep the compiler from forming packed fp32 instructions.
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-command-line-argument",
     "-I", os.path.join(ROOT, "include"), "-I", CSRC,
@@ -39,10 +41,17 @@ def hipcc_path():
 
 def build(verbose=False, extra_flags=()):
     """Compile every HIP source into libkvcomm.so.  Always recompiles."""
-    cmd = [hipcc_path()] + HIPCC_FLAGS + list(extra_flags) + ["-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
-    if verbose:
-        print(" ".join(cmd))
-    subprocess.run(cmd, check=True)
+    with tempfile.TemporaryDirectory() as tmp:
+        def compile_one(source):
+            obj = os.path.join(tmp, source + ".o")
+            cmd = [hipcc_path()] + HIPCC_FLAGS + list(extra_flags) + ["-c", "-o", obj, os.path.join(CSRC, source)]
+            if verbose:
+                print(" ".join(cmd))
+            subprocess.run(cmd, check=True)
+            return obj
+        with ThreadPoolExecutor(min(len(SOURCES), os.cpu_count() or 1, 16)) as pool:   # the sources do not depend on each other
+            objects = list(pool.map(compile_one, SOURCES))
+        subprocess.run([hipcc_path(), "--offload-arch=gfx950", "-fPIC", "-shared", "-o", LIB] + objects, check=True)
     probe = [hipcc_path(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-Xclang", "-target-feature", "-Xclang",
              "-packed-fp32-ops", "-Wall", "-Wno-unused-command-line-argument", "-o", PROBE, PROBE_SRC]
     if verbose:

@@ -26,6 +26,11 @@ struct AttnParams {
     int32_t n_splits;  // 1: results go straight to `out`
     int32_t groups_per_tile;  // groups of a row tile: bf16, of 32 rows (= wavefronts that own rows; one of 16 in a tile of 16 rows); fp32, of 16
     divisor_t by_G, by_Hkv, by_row_tiles, by_splits, by_groups;   // set_divisors()
+    // kvcomm_suffix_attn_window: token j is seen from position p iff j <= p and (j > p - window or j < n_sinks).  0: no window.
+    int32_t window, n_sinks;
+    // kvcomm_suffix_attn_kv4: k and v point at codes (strides in bytes), these at their scales.
+    const uint8_t *k_scales, *v_scales;
+    Strides s_ks, s_vs;
 };
 __device__ __forceinline__ void await_attn_args(const AttnParams &p)
 {

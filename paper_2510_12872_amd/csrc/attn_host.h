@@ -1,0 +1,66 @@
+// What the attention calls check and fill in alike.
+#pragma once
+
+#include "attn_plan.h"
+#include "fp4.h"
+
+namespace kvc {
+
+// Checks of every attention call but those of its cache, and the parameters that depend on no plan.
+static inline int attn_params(const kvcomm_model *model, const kvcomm_tensor &q, int32_t n_ctx, int32_t tq, float softmax_scale, const kvcomm_tensor &out,
+                              float *lse_out, AttnParams &p)
+{
+    int st = check_model(model);
+    if (st) return st;
+    if (tq <= 0 || n_ctx < 0) return KVCOMM_EINVAL;
+    if ((st = check_tensor(q, model->dtype, true)) || (st = check_tensor(out, model->dtype, true))) return st;
+    p.q = q.ptr;
+    p.out = out.ptr;
+    p.lse = lse_out;
+    p.s_q = strides_of(q);
+    p.s_o = strides_of(out);
+    p.L = model->n_layers;
+    p.Hkv = model->n_kv_heads;
+    p.G = model->n_q_heads / model->n_kv_heads;
+    p.n_ctx = n_ctx;
+    p.tq = tq;
+    p.N = n_ctx + tq;
+    p.scale = softmax_scale > 0.f ? softmax_scale : (float)(1.0 / sqrt((double)model->head_dim));
+    p.scale_log2 = (float)((double)p.scale * 1.4426950408889634);
+    p.n_splits = 1;
+    p.groups_per_tile = 1;
+    return KVCOMM_OK;
+}
+
+// The cache of a call, [L, Hkv, n_ctx + tq, D] of the model's type.
+static inline int attn_cache(const kvcomm_model &model, const kvcomm_tensor &k, const kvcomm_tensor &v, AttnParams &p)
+{
+    int st;
+    if ((st = check_tensor(k, model.dtype, true)) || (st = check_tensor(v, model.dtype, true))) return st;
+    p.k = k.ptr;
+    p.v = v.ptr;
+    p.s_k = strides_of(k);
+    p.s_v = strides_of(v);
+    return KVCOMM_OK;
+}
+
+// The same in 4 bits.
+static inline int attn_cache4(const kvcomm_model &model, const kvcomm_tensor4 &k, const kvcomm_tensor4 &v, AttnParams &p)
+{
+    int st;
+    if ((st = check_tensor4(k, model.head_dim)) || (st = check_tensor4(v, model.head_dim))) return st;
+    p.k = k.codes.ptr;
+    p.v = v.codes.ptr;
+    p.s_k = strides_of(k.codes);
+    p.s_v = strides_of(v.codes);
+    p.k_scales = static_cast<const uint8_t *>(k.scales.ptr);
+    p.v_scales = static_cast<const uint8_t *>(v.scales.ptr);
+    p.s_ks = strides_of(k.scales);
+    p.s_vs = strides_of(v.scales);
+    return KVCOMM_OK;
+}
+
+// Tokens of a cache whose tiles the kernels count and address with 32-bit integers.
+constexpr int64_t kMaxTokens = (int64_t)1 << 30;
+
+}  // namespace kvc

@@ -42,11 +42,18 @@ struct Library {
     decltype(&kvcomm_anchor_predict) anchor_predict;
     decltype(&kvcomm_capture_offsets) capture_offsets;
     decltype(&kvcomm_quantize_deltas) quantize_deltas;
+    decltype(&kvcomm_place_qkv) place_qkv;
+    decltype(&kvcomm_quantize_kv4) quantize_kv4;
+    decltype(&kvcomm_dequantize_kv4) dequantize_kv4;
+    decltype(&kvcomm_suffix_attn_kv4_workspace) attn_kv4_workspace;
+    decltype(&kvcomm_suffix_attn_kv4) suffix_attn_kv4;
+    decltype(&kvcomm_suffix_attn_window_workspace) attn_window_workspace;
+    decltype(&kvcomm_suffix_attn_window) suffix_attn_window;
     PyObject *model_type, *current_device, *current_stream;
 } lib;
 
 struct Names {
-    PyObject *n_layers, *n_kv_heads, *n_q_heads, *head_dim, *dtype, *rope_theta, *cuda_stream;
+    PyObject *n_layers, *n_kv_heads, *n_q_heads, *head_dim, *dtype, *rope_theta, *cuda_stream, *device_index;
     PyObject *seg_base_k, *anchor_base_k, *anchor_len, *base_k, *base_v, *anchor_dk, *anchor_dv, *anchor_dk8, *anchor_dv8, *scale_k,
         *scale_v, *weights, *delta_pos, *anchor_delta_pos, *out_k, *out_v;
 } names;
@@ -85,6 +92,7 @@ const at::Tensor &as_tensor(PyObject *o)
 struct Call {   // the model of a call and its tensors' type
     kvcomm_model m;
     at::ScalarType dtype;
+    mutable int device = -1;   // of the tensors that have gone through on()
     explicit Call(PyObject *model)
     {
         if (Py_TYPE(model) != (PyTypeObject *)lib.model_type) throw Decline{};
@@ -104,6 +112,13 @@ struct Call {   // the model of a call and its tensors' type
         if (dtype != at::kBFloat16 && dtype != at::kFloat) throw Decline{};
         m.dtype = dtype == at::kBFloat16 ? KVCOMM_BF16 : KVCOMM_F32;
     }
+    // All tensors of a call lie on one device
+    const at::Tensor &on(const at::Tensor &t) const
+    {
+        if (device >= 0 && t.get_device() != device) throw Decline{};
+        device = t.get_device();
+        return t;
+    }
 
 private:
     struct py {   // owned reference
@@ -121,6 +136,14 @@ kvcomm_tensor desc(const at::Tensor &t, at::ScalarType dtype)
     return kvcomm_tensor{t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)};
 }
 kvcomm_tensor desc(PyObject *o, at::ScalarType dtype) { return desc(as_tensor(o), dtype); }
+
+// The same of exactly these heads, tokens and channels, on the call's device
+kvcomm_tensor sized(const Call &c, PyObject *o, at::ScalarType dtype, int64_t H, int64_t n, int64_t D)
+{
+    const at::Tensor &t = c.on(as_tensor(o));
+    if (t.dim() != 4 || t.size(0) != c.m.n_layers || t.size(1) != H || t.size(2) != n || t.size(3) != D) throw Decline{};
+    return desc(t, dtype);
+}
 
 bool same_layout(const kvcomm_tensor &a, const kvcomm_tensor &b)
 {
@@ -229,6 +252,17 @@ void *stream_of(PyObject *o)
     Py_DECREF(h);
     if (!ok) throw Decline{};
     return reinterpret_cast<void *>((uintptr_t)v);
+}
+
+// The same, of the call's device: a stream of another one would run the kernels where the tensors are not.
+void *stream_of(const Call &c, PyObject *o)
+{
+    PyObject *dev = o == Py_None ? PyObject_CallNoArgs(lib.current_device) : PyObject_GetAttr(o, names.device_index);
+    if (!dev) throw Decline{};
+    const long v = PyLong_CheckExact(dev) ? PyLong_AsLong(dev) : -1;
+    Py_DECREF(dev);
+    if (v != c.device) throw Decline{};
+    return stream_of(o);
 }
 
 PyObject *item(PyObject *dict, PyObject *name)   // borrowed; None where there is none
@@ -472,6 +506,136 @@ PyObject *suffix_attn(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// (model, n_ctx, tq)
+PyObject *suffix_attn_kv4_workspace(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return entry<3>(args, n, [](PyObject *const *a) {
+        const Call c(a[0]);
+        return (long long)lib.attn_kv4_workspace(&c.m, as_int(a[1]), as_int(a[2]));
+    });
+}
+
+// (model, n_ctx, tq, window, n_sinks)
+PyObject *suffix_attn_window_workspace(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return entry<5>(args, n, [](PyObject *const *a) {
+        const Call c(a[0]);
+        return (long long)lib.attn_window_workspace(&c.m, as_int(a[1]), as_int(a[2]), as_int(a[3]), as_int(a[4]));
+    });
+}
+
+// What the attention calls over caches of checked sizes share, from (q, n_ctx, softmax_scale, out, lse_out, workspace, stream)
+struct Attention {
+    kvcomm_tensor q, out;
+    int32_t tq, n_ctx;
+    int64_t N;
+    float scale;
+    float *lse = nullptr;
+    Scratch ws;
+    void *stream;
+    Attention(const Call &c, PyObject *const (&o)[7]) : tq(tokens_of(as_tensor(o[0]))), n_ctx(as_int(o[1])), N((int64_t)n_ctx + tq), scale((float)as_double(o[2])), ws(o[5])
+    {
+        q = sized(c, o[0], c.dtype, c.m.n_q_heads, tq, c.m.head_dim);
+        out = sized(c, o[3], c.dtype, c.m.n_q_heads, tq, c.m.head_dim);
+        if (o[4] != Py_None) {
+            const at::Tensor &t = c.on(as_tensor(o[4]));
+            if (t.scalar_type() != at::kFloat || !t.is_contiguous() || t.numel() != (int64_t)c.m.n_layers * c.m.n_q_heads * tq) throw Decline{};
+            lse = static_cast<float *>(t.data_ptr());
+        }
+        if (o[5] != Py_None) c.on(as_tensor(o[5]));
+        stream = stream_of(c, o[6]);
+    }
+};
+
+// A compact tensor: (codes, scales)
+kvcomm_tensor4 compact(const Call &c, PyObject *o, int64_t n)
+{
+    const Items it(o, 2, 2);
+    return kvcomm_tensor4{sized(c, it.p[0], at::kByte, c.m.n_kv_heads, n, c.m.head_dim / 2),
+                          sized(c, it.p[1], at::kByte, c.m.n_kv_heads, n, c.m.head_dim / 32)};
+}
+
+// (model, q, cache_k, cache_v, n_ctx, softmax_scale, out, lse_out, workspace, stream); the caches are (codes, scales)
+PyObject *suffix_attn_kv4(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return entry<10>(args, n, [](PyObject *const *a) {
+        const Call c(a[0]);
+        const Attention t(c, {a[1], a[4], a[5], a[6], a[7], a[8], a[9]});
+        const kvcomm_tensor4 k = compact(c, a[2], t.N), v = compact(c, a[3], t.N);
+        return unlocked([&] { return lib.suffix_attn_kv4(&c.m, t.q, k, v, t.n_ctx, t.tq, t.scale, t.out, t.lse, t.ws.ptr, t.ws.bytes, t.stream); });
+    });
+}
+
+// (model, q, cache_k, cache_v, n_ctx, window, n_sinks, softmax_scale, out, lse_out, workspace, stream)
+PyObject *suffix_attn_window(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return entry<12>(args, n, [](PyObject *const *a) {
+        const Call c(a[0]);
+        const Attention t(c, {a[1], a[4], a[7], a[8], a[9], a[10], a[11]});
+        const int32_t window = as_int(a[5]), sinks = as_int(a[6]);
+        const kvcomm_tensor k = sized(c, a[2], c.dtype, c.m.n_kv_heads, t.N, c.m.head_dim),
+                            v = sized(c, a[3], c.dtype, c.m.n_kv_heads, t.N, c.m.head_dim);
+        return unlocked([&] {
+            return lib.suffix_attn_window(&c.m, t.q, k, v, t.n_ctx, t.tq, window, sinks, t.scale, t.out, t.lse, t.ws.ptr, t.ws.bytes, t.stream);
+        });
+    });
+}
+
+// (model, q, k, v, first_pos, q_weight, k_weight, norm_eps, q_out, k_out, v_out, stream); None in the place of a pair or a weight that is not given
+PyObject *place_qkv(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return entry<12>(args, n, [](PyObject *const *a) {
+        const Call c(a[0]);
+        int64_t tokens = -1;
+        kvcomm_tensor in[3] = {}, out[3] = {};
+        for (int i = 0; i < 3; ++i) {
+            PyObject *x = a[1 + i], *y = a[8 + i];
+            if ((x == Py_None) != (y == Py_None)) throw Decline{};
+            if (x == Py_None) continue;
+            if (tokens < 0) tokens = tokens_of(as_tensor(x));
+            const int64_t heads = i == 0 ? c.m.n_q_heads : c.m.n_kv_heads;
+            in[i] = sized(c, x, c.dtype, heads, tokens, c.m.head_dim);
+            out[i] = sized(c, y, c.dtype, heads, tokens, c.m.head_dim);
+        }
+        if (tokens < 0) throw Decline{};
+        const void *w[2] = {};
+        int64_t ws[2] = {};
+        for (int i = 0; i < 2; ++i) {
+            if (a[5 + i] == Py_None) continue;
+            const at::Tensor &t = c.on(as_tensor(a[5 + i]));
+            const int64_t d = t.dim();
+            if (t.scalar_type() != c.dtype || d < 1 || d > 2 || t.size(d - 1) != c.m.head_dim || t.stride(d - 1) != 1 || (d == 2 && t.size(0) != c.m.n_layers))
+                throw Decline{};
+            w[i] = t.data_ptr();
+            ws[i] = d == 2 ? t.stride(0) : 0;
+        }
+        const int32_t first = as_int(a[4]);
+        const float eps = (float)as_double(a[7]);
+        void *stream = stream_of(c, a[11]);
+        return unlocked([&] {
+            return lib.place_qkv(&c.m, in[0], in[1], in[2], (int32_t)tokens, first, w[0], w[1], ws[0], ws[1], eps, out[0], out[1], out[2], stream);
+        });
+    });
+}
+
+// Into 4 bits: (model, k, v, out_k, out_v, stream); back: (model, k, v as (codes, scales), out_k, out_v, stream)
+template <bool BACK>
+PyObject *convert_kv4(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return entry<6>(args, n, [](PyObject *const *a) {
+        const Call c(a[0]);
+        PyObject *const *x = a + (BACK ? 3 : 1), *const *x4 = a + (BACK ? 1 : 3);
+        const int32_t tokens = tokens_of(as_tensor(x[0]));
+        const kvcomm_tensor k = sized(c, x[0], c.dtype, c.m.n_kv_heads, tokens, c.m.head_dim),
+                            v = sized(c, x[1], c.dtype, c.m.n_kv_heads, tokens, c.m.head_dim);
+        const kvcomm_tensor4 k4 = compact(c, x4[0], tokens), v4 = compact(c, x4[1], tokens);
+        void *stream = stream_of(c, a[5]);
+        return unlocked([&] {
+            return BACK ? lib.dequantize_kv4(&c.m, k4, v4, tokens, k, v, stream) : lib.quantize_kv4(&c.m, k, v, tokens, k4, v4, stream);
+        });
+    });
+}
+
 // (weights, anchor_len, seg_len, gamma, entropy_out, result_out, workspace, stream)
 PyObject *anchor_predict(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -574,7 +738,10 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
         !set(lib.align_kv, "kvcomm_align_kv") || !set(lib.align_kv_q8, "kvcomm_align_kv_q8") ||
         !set(lib.suffix_attn, "kvcomm_suffix_attn") || !set(lib.suffix_attn_confined_ws, "kvcomm_suffix_attn_confined_ws") ||
         !set(lib.anchor_predict, "kvcomm_anchor_predict") || !set(lib.capture_offsets, "kvcomm_capture_offsets") ||
-        !set(lib.quantize_deltas, "kvcomm_quantize_deltas")) {
+        !set(lib.quantize_deltas, "kvcomm_quantize_deltas") || !set(lib.place_qkv, "kvcomm_place_qkv") ||
+        !set(lib.quantize_kv4, "kvcomm_quantize_kv4") || !set(lib.dequantize_kv4, "kvcomm_dequantize_kv4") ||
+        !set(lib.attn_kv4_workspace, "kvcomm_suffix_attn_kv4_workspace") || !set(lib.suffix_attn_kv4, "kvcomm_suffix_attn_kv4") ||
+        !set(lib.attn_window_workspace, "kvcomm_suffix_attn_window_workspace") || !set(lib.suffix_attn_window, "kvcomm_suffix_attn_window")) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_KeyError, "an entry point of the library is missing");
         return nullptr;
     }
@@ -598,6 +765,13 @@ PyMethodDef methods[] = {FAST("bind", bind),
                          FAST("anchor_predict", anchor_predict),
                          FAST("capture_offsets", capture_offsets),
                          FAST("quantize_deltas", quantize_deltas),
+                         FAST("place_qkv", place_qkv),
+                         FAST("quantize_kv4", convert_kv4<false>),
+                         FAST("dequantize_kv4", convert_kv4<true>),
+                         FAST("suffix_attn_kv4_workspace", suffix_attn_kv4_workspace),
+                         FAST("suffix_attn_kv4", suffix_attn_kv4),
+                         FAST("suffix_attn_window_workspace", suffix_attn_window_workspace),
+                         FAST("suffix_attn_window", suffix_attn_window),
                          FAST("apart", apart),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -608,7 +782,7 @@ PyMODINIT_FUNC PyInit__marshal(void)
 {
 #define NAME(x) \
     if (!(names.x = PyUnicode_InternFromString(#x))) return nullptr
-    NAME(n_layers); NAME(n_kv_heads); NAME(n_q_heads); NAME(head_dim); NAME(dtype); NAME(rope_theta); NAME(cuda_stream);
+    NAME(n_layers); NAME(n_kv_heads); NAME(n_q_heads); NAME(head_dim); NAME(dtype); NAME(rope_theta); NAME(cuda_stream); NAME(device_index);
     NAME(seg_base_k); NAME(anchor_base_k); NAME(anchor_len); NAME(base_k); NAME(base_v); NAME(anchor_dk); NAME(anchor_dv);
     NAME(anchor_dk8); NAME(anchor_dv8); NAME(scale_k); NAME(scale_v); NAME(weights); NAME(delta_pos); NAME(anchor_delta_pos);
     NAME(out_k); NAME(out_v);

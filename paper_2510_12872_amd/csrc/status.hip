@@ -13,4 +13,4 @@ extern "C" const char *kvcomm_status_string(int status)
     }
 }
 
-extern "C" int kvcomm_version(void) { return 201; }  // 0.2.1: kvcomm_align_kv_batch_beside
+extern "C" int kvcomm_version(void) { return 300; }  // 0.3.0: kvcomm_place_qkv, compact caches (kv4), sliding window

@@ -44,8 +44,7 @@
 // fp32 path: attn_f32.hip.
 #include <float.h>
 
-#include "attn_common.h"
-#include "attn_plan.h"
+#include "attn_host.h"
 
 namespace {
 
@@ -619,38 +618,13 @@ int suffix_attn(const kvcomm_model *model, kvcomm_tensor q, kvcomm_tensor cache_
                 int32_t tq, float softmax_scale, kvcomm_tensor out, float *lse_out, int32_t max_blocks, void *workspace,
                 size_t workspace_bytes, void *stream)
 {
-    int st = check_model(model);
-    if (st) return st;
-    if (tq <= 0 || n_ctx < 0) return KVCOMM_EINVAL;
-    const int dt = model->dtype;
-    if ((st = check_tensor(q, dt, true)) || (st = check_tensor(cache_k, dt, true)) ||
-        (st = check_tensor(cache_v, dt, true)) || (st = check_tensor(out, dt, true)))
-        return st;
-
     AttnParams p{};
-    p.q = q.ptr;
-    p.k = cache_k.ptr;
-    p.v = cache_v.ptr;
-    p.out = out.ptr;
-    p.lse = lse_out;
-    p.s_q = strides_of(q);
-    p.s_k = strides_of(cache_k);
-    p.s_v = strides_of(cache_v);
-    p.s_o = strides_of(out);
-    p.L = model->n_layers;
-    p.Hkv = model->n_kv_heads;
-    p.G = model->n_q_heads / model->n_kv_heads;
-    p.n_ctx = n_ctx;
-    p.tq = tq;
-    p.N = n_ctx + tq;
-    p.scale = softmax_scale > 0.f ? softmax_scale : (float)(1.0 / sqrt((double)model->head_dim));
-    p.scale_log2 = (float)((double)p.scale * 1.4426950408889634);
-    p.n_splits = 1;
-    p.groups_per_tile = 1;
+    int st = attn_params(model, q, n_ctx, tq, softmax_scale, out, lse_out, p);
+    if (st || (st = attn_cache(*model, cache_k, cache_v, p))) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int D = model->head_dim;
 
-    if (dt == KVCOMM_F32) {
+    if (model->dtype == KVCOMM_F32) {
         p.groups_per_tile = attn_f32_groups(*model, tq, max_blocks);
         const int rows = 16 * p.groups_per_tile;
         p.n_row_tiles = (int32_t)(((int64_t)p.G * tq + rows - 1) / rows);

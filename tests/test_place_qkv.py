@@ -1,0 +1,131 @@
+"""kvcomm_place_qkv against its definition in float64, and its refusals."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2510_12872_amd as kv
+from paper_2510_12872_amd import binding
+
+from plain64 import HALF_STEP, check, f64, placed
+
+# L, Hkv, G, D, dtype, n, first position, eps, layout of the inputs
+CASES = [(1, 8, 4, 128, torch.bfloat16, 1, 0, 0.0, "packed"),
+         (1, 8, 4, 128, torch.bfloat16, 1, 131071, 1e-6, "packed"),
+         (2, 4, 2, 64, torch.float32, 33, 4096, 1e-5, "packed"),
+         (3, 2, 1, 128, torch.bfloat16, 77, 12, 1e-6, "plain"),
+         (2, 1, 8, 256, torch.bfloat16, 9, -5, 1e-5, "packed"),
+         (1, 3, 5, 256, torch.float32, 2, 77, 1e-3, "plain"),
+         (2, 2, 3, 64, torch.bfloat16, 130, 2 ** 31 - 131, 0.0, "packed"),
+         (1, 1, 1, 128, torch.float32, 3, 1, 0.0, "plain"),
+         (4, 8, 4, 128, torch.bfloat16, 64, 2560, 1e-6, "packed")]
+
+
+def _inputs(L, Hkv, G, D, dtype, n, layout, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((L, n, (G + 2) * Hkv, D), generator=g).to(dtype).cuda()
+    parts = x.split([G * Hkv, Hkv, Hkv], 2)
+    q, k, v = (t.transpose(1, 2) for t in parts)
+    if layout == "plain":
+        q, k, v = (t.contiguous() for t in (q, k, v))
+    w = (1 + 0.2 * torch.randn((2, L, D), generator=g)).to(dtype).cuda()
+    return q, k, v, w[0], w[1]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", CASES, ids=lambda c: f"L{c[0]}-H{c[1]}x{c[2]}-D{c[3]}-{str(c[4])[6:]}-n{c[5]}-at{c[6]}-eps{c[7]}-{c[8]}")
+def test_against_float64(case):
+    L, Hkv, G, D, dtype, n, first, eps, layout = case
+    theta = 5e5
+    m = kv.Model(L, Hkv, G * Hkv, D, dtype, theta)
+    q, k, v, wq, wk = _inputs(L, Hkv, G, D, dtype, n, layout)
+    cache = torch.full((2, L, Hkv, n + 9, D), 3.0, dtype=dtype, device="cuda")
+    norm = dict(norm_eps=eps, q_weight=wq, k_weight=wk[0]) if eps else {}
+    qo, ko, vo = kv.kvcomm_place_qkv(m, q, k, v, first, k_out=cache[0, :, :, 5:5 + n], v_out=cache[1, :, :, 5:5 + n], **norm)
+    assert torch.equal(vo, v) and vo.data_ptr() == cache[1, :, :, 5:].data_ptr()
+    for got, x, w, what in ((qo, q, f64(wq), "q"), (ko, k, np.broadcast_to(f64(wk)[:1], (L, D)), "k")):
+        want, off = placed(f64(x), first, theta, eps, w)
+        check(got, want, off * (1 + HALF_STEP[dtype]) + HALF_STEP[dtype] * np.abs(want), what)
+    rest = torch.cat([cache[:, :, :, :5], cache[:, :, :, 5 + n:]], 3)
+    assert bool((rest == 3.0).all())   # the cache's other rows
+
+
+@pytest.mark.gpu
+def test_forms_of_a_call_give_the_same_bits():
+    L, Hkv, G, D, dtype, n = 2, 2, 4, 128, torch.bfloat16, 50
+    m = kv.Model(L, Hkv, G * Hkv, D, dtype, 1e4)
+    q, k, v, wq, wk = _inputs(L, Hkv, G, D, dtype, n, "plain")
+    norm = dict(norm_eps=1e-6, q_weight=wq, k_weight=wk)
+    want = kv.kvcomm_place_qkv(m, q, k, v, 40, **norm)
+    one = kv.kvcomm_place_qkv(m, None, k, None, 40, norm_eps=1e-6, k_weight=wk)
+    assert one[0] is None and one[2] is None and torch.equal(one[1], want[1])
+    for i in range(0, n, 7):   # in pieces
+        part = kv.kvcomm_place_qkv(m, q[:, :, i:i + 7], k[:, :, i:i + 7], v[:, :, i:i + 7], 40 + i, **norm)
+        assert all(torch.equal(a, b[:, :, i:i + 7]) for a, b in zip(part, want))
+    for l in range(L):         # a layer at a time
+        part = kv.kvcomm_place_qkv(kv.Model(1, Hkv, G * Hkv, D, dtype, 1e4), q[l:l + 1], k[l:l + 1], v[l:l + 1], 40, norm_eps=1e-6,
+                                   q_weight=wq[l], k_weight=wk[l:l + 1])
+        assert all(torch.equal(a, b[l:l + 1]) for a, b in zip(part, want))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    beside = kv.kvcomm_place_qkv(m, q, k, v, 40, stream=side, **norm)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(beside, want))
+    ones = torch.ones((D,), dtype=dtype, device="cuda")
+    assert all(torch.equal(a, b) for a, b in zip(kv.kvcomm_place_qkv(m, q, k, v, 40, norm_eps=1e-6),
+                                                 kv.kvcomm_place_qkv(m, q, k, v, 40, norm_eps=1e-6, q_weight=ones, k_weight=ones)))
+    kv.kvcomm_place_qkv(m, q, k, v, 40, q_out=q, k_out=k, v_out=v, **norm)   # in place
+    assert all(torch.equal(a, b) for a, b in zip((q, k, v), want))
+
+
+@pytest.mark.gpu
+def test_extreme_rows():
+    """A row of zeros under a norm, and squares that leave the range of fp32: what the formula gives there."""
+    m = kv.Model(1, 1, 1, 64, torch.float32, 1e4)
+    x = torch.zeros((1, 1, 3, 64), device="cuda")
+    x[0, 0, 1] = 1e-30
+    x[0, 0, 2] = 1e30
+    q, _, _ = kv.kvcomm_place_qkv(m, x, None, None, 0, norm_eps=1e-6)
+    assert bool((q[0, 0, 0] == 0).all())
+    want, off = placed(f64(x[:, :, 1:2]), 1, 1e4, 1e-6)
+    check(q[:, :, 1:2], want, off + 2.0 ** -24 * np.abs(want), "tiny")
+    assert bool((q[0, 0, 2] == 0).all())   # x / sqrt(inf), as the formula in fp32 gives
+
+
+@pytest.mark.gpu
+def test_refusals_of_the_binding():
+    m = kv.Model(2, 2, 4, 64, torch.bfloat16, 1e4)
+    t = lambda h, n=3, d=torch.bfloat16, D=64: torch.zeros((2, h, n, D), dtype=d, device="cuda")
+    q, k, v = t(4), t(2), t(2)
+    w = torch.ones((64,), dtype=torch.bfloat16, device="cuda")
+    bad = [dict(q=t(2)), dict(k=t(2, 4)), dict(v=t(2, d=torch.float32)), dict(k=t(2, D=32)), dict(q_out=t(4, 2)), dict(v=None, v_out=t(2)),
+           dict(q_weight=w), dict(norm_eps=-1.0), dict(norm_eps=float("nan")), dict(norm_eps=float("inf")), dict(norm_eps=1e-6, q_weight=w[:32]),
+           dict(norm_eps=1e-6, k_weight=w.float()), dict(norm_eps=1e-6, k_weight=w.cpu()), dict(q=q.cpu(), q_out=t(4)), dict(q=None, k=None, v=None),
+           dict(first_pos=2 ** 31 - 2), dict(k_out=q[:, :2]), dict(k_out=v), dict(norm_eps=1e-6, q_weight=w, q=None)]
+    for change in bad:
+        args = {**dict(q=q, k=k, v=v, first_pos=0), **change}
+        with pytest.raises(kv.KVCommError):
+            kv.kvcomm_place_qkv(m, args.pop("q"), args.pop("k"), args.pop("v"), args.pop("first_pos"), **args)
+    with pytest.raises(kv.KVCommError):
+        kv.kvcomm_place_qkv(m, t(4, 0), t(2, 0), t(2, 0), 0)
+
+
+def test_refusals_of_the_library():
+    """On the host, before anything is launched."""
+    lib = kv.load_library()
+    T = lambda ptr=0x10000, sl=1 << 20, sh=1 << 12, st=128: binding._CTensor(ptr, sl, sh, st)
+    none = binding._CTensor(None, 0, 0, 0)
+
+    def call(q=T(), k=T(0x8000000), v=T(0x9000000), n=4, first=0, wq=None, wk=None, sq=0, sk=0, eps=0.0, qo=T(0xa000000), ko=T(0xb000000),
+             vo=T(0xc000000), D=128, dtype=1):
+        m = binding._CModel(2, 2, 4, D, dtype, 1e4)
+        return lib.kvcomm_place_qkv(ctypes.byref(m), q, k, v, n, first, wq, wk, sq, sk, eps, qo, ko, vo, None)
+    inval = [dict(n=0), dict(n=-1), dict(first=2 ** 31 - 3), dict(eps=-1e-9), dict(eps=float("nan")), dict(eps=float("inf")), dict(wq=0x1000),
+             dict(wq=0x1008, eps=1e-6), dict(wk=0x1000, sk=4, eps=1e-6), dict(q=none), dict(ko=none), dict(q=none, qo=none, wq=0x1000, eps=1e-6),
+             dict(q=none, k=none, v=none, qo=none, ko=none, vo=none), dict(q=T(0x10008)), dict(k=T(0x8000000, st=4)), dict(vo=T(0xc000000, sh=-128)),
+             dict(qo=T(0x8000000)), dict(ko=T(0xa000000)), dict(qo=T(0x10000 + 256)), dict(ko=T(0x9000000)), dict(wk=0xb000000, eps=1e-6), dict(D=0)]
+    for change in inval:
+        assert call(**change) == -1, change
+    assert call(D=96) == -2
+    assert lib.kvcomm_place_qkv(None, T(), T(), T(), 1, 0, None, None, 0, 0, 0.0, T(), T(), T(), None) == -1
