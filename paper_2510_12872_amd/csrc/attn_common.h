@@ -26,12 +26,28 @@ struct AttnParams {
     int32_t n_splits;  // 1: results go straight to `out`
     int32_t groups_per_tile;  // groups of a row tile: bf16, of 32 rows (= wavefronts that own rows; one of 16 in a tile of 16 rows); fp32, of 16
     divisor_t by_G, by_Hkv, by_row_tiles, by_splits, by_groups;   // set_divisors()
-    // kvcomm_suffix_attn_window: token j is seen from position p iff j <= p and (j > p - window or j < n_sinks).  0: no window.
+    // kvcomm_suffix_attn_window: token j is seen from position p iff j <= p and (j > p - window or j < n_sinks); both <= N.  0: no window.
     int32_t window, n_sinks;
     // kvcomm_suffix_attn_kv4: k and v point at codes (strides in bytes), these at their scales.
     const uint8_t *k_scales, *v_scales;
     Strides s_ks, s_vs;
 };
+// What the keys of a launch are: a whole cache, or a cache of which a query sees its window and the sinks.
+enum class Keys { kAll, kWindow };
+
+// The units (of `unit` keys) that the queries imin ... imax of a tile see through their windows, in order: `sinks` of them from key 0 on, which end
+// before the first unit of the windows, then those; unit u begins at key unit * (u + (u < sinks ? 0 : gap)).
+struct WindowUnits {
+    int sinks, gap, count;
+};
+template <class P>
+__device__ __forceinline__ WindowUnits window_units(const P &p, int imin, int imax, int unit)   // unit: a literal power of two
+{
+    const int first = max(0, p.n_ctx + imin + 1 - p.window) / unit, end = (p.n_ctx + imax) / unit + 1;
+    const int sinks = min((p.n_sinks + unit - 1) / unit, first);
+    return WindowUnits{sinks, first - sinks, sinks + end - first};
+}
+
 __device__ __forceinline__ void await_attn_args(const AttnParams &p)
 {
     await_args(arg_word(&p), arg_word(&p.s_q.token), arg_word(&p.s_v), arg_word(&p.L));
@@ -183,5 +199,10 @@ __device__ __forceinline__ float query_sum(float x)
     const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
+
+// Does a row's state say that its block has to be computed again by attn_exact_rows()?  `zero`: a sum of 0 times everything in it, NaN if
+// anything is not finite.  A row that has a reference has the exponential of its maximum in its sum, which is 1 up to the rounding of reference * scale:
+// scores so large (beyond 2^24) that this rounding reaches the exponent leave a sum of 0, or infinity.
+__device__ __forceinline__ bool state_is_odd(float zero, float m, float sum) { return !(zero == 0.f) || !(sum >= 0.5f || m == -INFINITY); }
 
 }  // namespace kvc

@@ -15,11 +15,12 @@ template <typename T>
 struct CacheRows {
     const T *base;
     int64_t token;
-    __device__ __forceinline__ CacheRows(const AttnParams &p, bool values, int l, int hkv)
+    template <class P>
+    __device__ __forceinline__ CacheRows(const P &p, bool values, int l, int hkv)
     {
-        const Strides s = values ? p.s_v : p.s_k;
-        base = static_cast<const T *>(values ? p.v : p.k) + l * s.layer + hkv * s.head;
-        token = s.token;
+        const int64_t layer = values ? p.s_v.layer : p.s_k.layer, head = values ? p.s_v.head : p.s_k.head;
+        base = static_cast<const T *>(values ? p.v : p.k) + l * layer + hkv * head;
+        token = values ? p.s_v.token : p.s_k.token;
     }
     __device__ __forceinline__ void load8(int key, int c, float (&out)[8]) const
     {
@@ -37,13 +38,14 @@ template <>
 struct CacheRows<fp4_t> {
     const uint8_t *base, *scales;
     int64_t token, s_token;
-    __device__ __forceinline__ CacheRows(const AttnParams &p, bool values, int l, int hkv)
+    template <class P>
+    __device__ __forceinline__ CacheRows(const P &p, bool values, int l, int hkv)
     {
-        const Strides s = values ? p.s_v : p.s_k, ss = values ? p.s_vs : p.s_ks;
-        base = static_cast<const uint8_t *>(values ? p.v : p.k) + l * s.layer + hkv * s.head;
-        scales = (values ? p.v_scales : p.k_scales) + l * ss.layer + hkv * ss.head;
-        token = s.token;
-        s_token = ss.token;
+        const int64_t layer = values ? p.s_v.layer : p.s_k.layer, head = values ? p.s_v.head : p.s_k.head;
+        base = static_cast<const uint8_t *>(values ? p.v : p.k) + l * layer + hkv * head;
+        scales = (values ? p.v_scales : p.k_scales) + l * (values ? p.s_vs.layer : p.s_ks.layer) + hkv * (values ? p.s_vs.head : p.s_ks.head);
+        token = values ? p.s_v.token : p.s_k.token;
+        s_token = values ? p.s_vs.token : p.s_ks.token;
     }
     __device__ __forceinline__ void load8(int key, int c, float (&out)[8]) const
     {
@@ -62,8 +64,8 @@ struct KeyRanges {
 
 // Rows [row0, row0 + n_rows) of the packed (query, head) axis of (layer, kv head) lh: wavefront `wave` of n_waves takes every n_waves-th.
 // Results go to `out`, or, where the keys are cut, to the partial results of run `split` (groups of group_rows rows).
-template <typename T, typename Q, int D>
-__device__ __forceinline__ void attn_exact_rows(const AttnParams &p, int lh, int row0, int n_rows, KeyRanges keys, int split, int group_rows, int wave,
+template <typename T, typename Q, int D, class P>   // P: AttnParams, in any address space
+__device__ __forceinline__ void attn_exact_rows(const P &p, int lh, int row0, int n_rows, KeyRanges keys, int split, int group_rows, int wave,
                                                 int n_waves, int lane)
 {
     constexpr int CL = D / 8;           // lanes that hold the 8 channels c = 8 * lane of an output row

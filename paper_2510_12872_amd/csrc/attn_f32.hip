@@ -1,4 +1,5 @@
 // fp32 suffix attention: fp32 MFMA (exact fp32 products and sums) with expf and an online softmax, fp32 throughout.
+#include "attn_exact.h"
 #include "attn_plan.h"
 
 namespace {
@@ -85,9 +86,12 @@ __global__ __launch_bounds__(256) void attn_f32_row_kernel(const AttnParams p)
 // K and V operand.  us before (32 rows and 32 keys on 32x32x2 MFMAs, K loads of 64 lines) and now: 2 layers x 4 heads x 64 rows, 224
 // keys, D = 64 10.3 -> 7.7; 4 x 8, G = 8, one token, 1025 keys, D = 128 54.8 -> 29.6, 256 96 -> 58; 4 x 8, G = 4, Tq 128, 1152 keys, D = 64 60.5 -> 55.5,
 // 128 118 -> 105, 256 195 -> 193; one layer, Tq 512, 3072 keys, D = 128 272 -> 243 (97 TFLOP/s; back to back, as all of these).
-template <int D, int RH>
+// KEYS = kWindow: the sub-steps of the sinks, then those of the windows (window_units()); values at the edges are multiplied as they are, and a block whose
+// results are not all finite computes its rows again by attn_exact_rows().
+template <int D, int RH, Keys KEYS>
 __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   // item: one row tile of a (layer, kv head)
 {
+    constexpr bool kWindow = KEYS == Keys::kWindow;
     constexpr int NW = kF32Waves;
     constexpr int NJ = D / 16, NT = D / 64;                 // 16-byte pieces of a K row in a lane, loads of a V row
     constexpr int NP = D == 256 ? 2 : 1, PJ = NJ / NP;         // parts of a K row (32 registers at most), pieces of a part
@@ -105,7 +109,10 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
     const int l = div_by(lh, p.by_Hkv), hkv = lh - l * p.Hkv;
     const int row0 = rt * 16 * RH;
     const int imax = min(p.tq - 1, div_by(row0 + 16 * RH - 1, p.by_G)), imin = min(p.tq - 1, div_by(row0, p.by_G));
-    const int units = (p.n_ctx + imax + 16) / 16;   // sub-steps that some query of the tile sees
+    WindowUnits wu = {0, 0, (p.n_ctx + imax + 16) / 16};   // sub-steps that some query of the tile sees
+    if constexpr (kWindow) wu = window_units(p, imin, imax, 16);
+    const int units = wu.count;
+    auto first_key = [&](int u) __attribute__((always_inline)) -> int { return 16 * (kWindow && u >= wu.sinks ? u + wu.gap : u); };
 
     const float *kb = static_cast<const float *>(p.k) + l * p.s_k.layer + hkv * p.s_k.head;
     const float *vb = static_cast<const float *>(p.v) + l * p.s_v.layer + hkv * p.s_v.head;
@@ -120,14 +127,14 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
     f32x4 k[HOLD][PJ], v[VR][NT];
     // Rows past the cache end re-read the last one; they are always masked.
     auto load_k = [&](int u, int part) __attribute__((always_inline)) {
-        const float *kr = kb + (int64_t)min(16 * u + n, p.N - 1) * p.s_k.token + 16 * PJ * part + 4 * g;
+        const float *kr = kb + (int64_t)min(first_key(u) + n, p.N - 1) * p.s_k.token + 16 * PJ * part + 4 * g;
 #pragma unroll
         for (int j = 0; j < PJ; ++j) k[part % HOLD][j] = *reinterpret_cast<const f32x4 *>(kr + 16 * j);
     };
     auto load_v = [&](int u, int r0) __attribute__((always_inline)) {   // score r of this lane is key 4 * g + r
 #pragma unroll
         for (int r = 0; r < VR; ++r) {
-            const float *vr = vb + (int64_t)min(16 * u + 4 * g + r0 + r, p.N - 1) * p.s_v.token + 4 * n;
+            const float *vr = vb + (int64_t)min(first_key(u) + 4 * g + r0 + r, p.N - 1) * p.s_v.token + 4 * n;
 #pragma unroll
             for (int t = 0; t < NT; ++t) v[r][t] = *reinterpret_cast<const f32x4 *>(vr + 64 * t);
         }
@@ -203,12 +210,14 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
         }
 #pragma unroll
         for (int h = 0; h < RH; ++h) {
-            const int limit = p.n_ctx + qi[h] - 16 * u - 4 * g;     // last visible one of this lane's keys
+            const int limit = p.n_ctx + qi[h] - first_key(u) - 4 * g;     // last visible one of this lane's keys
+            const int sinks = kWindow ? p.n_sinks - first_key(u) - 4 * g : 0;
             float mx = -INFINITY;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 s[h][r] *= p.scale;
                 if (EDGE && r > limit) s[h][r] = -INFINITY;
+                if (EDGE && kWindow && r <= limit - p.window && r >= sinks) s[h][r] = -INFINITY;
                 mx = fmaxf(mx, s[h][r]);
             }
             mx = query_max(mx);
@@ -247,7 +256,7 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         float x = v[r][t][c];
-                        if (EDGE) {
+                        if (EDGE && !kWindow) {
                             const bool fin = fabsf(x) < INFINITY;
                             odd |= !fin;
                             x = fin ? x : 0.f;
@@ -261,11 +270,32 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
     };
     // Two loops: with a branch inside one, V selected in place, the compiler gave other values the registers of rows that were still to
     // be multiplied.
-    const int u_edge = (p.n_ctx + imin + 1) / 16;   // first sub-step with a hidden key
+    int u_edge = (p.n_ctx + imin + 1) / 16;   // first sub-step with a hidden key
     int u = wave;
+    if constexpr (kWindow) {   // (of the windows; those before u_whole have keys that some query's window has left)
+        u_edge -= wu.gap;
+        const int left = p.n_ctx + imax - p.window;
+        const int u_whole = max(wu.sinks, left < 0 ? 0 : left / 16 + 1 - wu.gap);
+        for (; u < min(u_whole, units); u += NW) sub_step(u, std::true_type{});
+    }
     for (; u < min(u_edge, units); u += NW) sub_step(u, std::false_type{});
     for (; u < units; u += NW) sub_step(u, std::true_type{});
 
+    if constexpr (kWindow) {
+        bool odd_state = false;
+#pragma unroll
+        for (int h = 0; h < RH; ++h) {
+            float zero = lsum[h] * 0.f;
+#pragma unroll
+            for (int i = 0; i < 16 * NT; ++i) zero = fmaf(o[h][i / 16][i / 4 % 4][i % 4], 0.f, zero);
+            odd_state |= state_is_odd(zero, m[h], query_sum(lsum[h]));
+        }
+        if (__syncthreads_or(odd_state)) {
+            const KeyRanges keys = {0, 16 * wu.sinks, 16 * (wu.sinks + wu.gap), p.N};
+            attn_exact_rows<float, float, D>(p, lh, row0, 16 * RH, keys, 0, 16, wave, NW, lane);
+            return;
+        }
+    }
     // ---- join the wavefronts' states and store.  Lane (n, g) holds channels 64 * t + 16 * g + 4 * r + c of query rows n (and 16 + n).
 #pragma unroll
     for (int h = 0; h < RH; ++h) {
@@ -309,7 +339,7 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
     }
 
     // Rare: values left out at the causal edge, for the queries that see them (thread: one query, every 4 * NW-th channel).
-    if (__syncthreads_or(odd)) {
+    if (!kWindow && __syncthreads_or(odd)) {
 #pragma unroll 1
         for (int h = 0; h < RH; ++h) {   // (all of it formed again: nothing is kept for this across the loop)
             const int r_row = row0 + 16 * h + n, i_row = div_by(r_row, p.by_G);
@@ -341,15 +371,15 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
 
 // PERSIST: a grid of fewer blocks than items, each walking every gridDim.x-th one.  Two blocks of D = 64 fit a compute unit.  (One group at D = 128 held to
 // two as well spilled up to 24 registers: one token, 1025 keys, 4 layers x 8 heads, G = 8 on 16 blocks 60.7 us instead of 54.9; in one round the same 28.6.)
-template <int D, int RH, bool PERSIST>
+template <int D, int RH, bool PERSIST, Keys KEYS>
 __global__ __launch_bounds__(64 * kF32Waves, D == 64 ? 4 : 2) void attn_f32_kernel(const AttnParams p)
 {
     await_attn_args(p);
     if constexpr (!PERSIST) {
-        attn_f32_item<D, RH>(p, blockIdx.x);
+        attn_f32_item<D, RH, KEYS>(p, blockIdx.x);
     } else {
         for (int item = blockIdx.x; item < p.n_items; item += gridDim.x) {
-            attn_f32_item<D, RH>(p, item);
+            attn_f32_item<D, RH, KEYS>(p, item);
             __syncthreads();   // the joined states have been read: LDS becomes the next item's
         }
     }
@@ -358,8 +388,9 @@ __global__ __launch_bounds__(64 * kF32Waves, D == 64 ? 4 : 2) void attn_f32_kern
 template <int D>
 int launch_f32(const AttnParams &p, bool persist, unsigned n_blocks, hipStream_t stream)
 {
-    const auto one = persist ? attn_f32_kernel<D, 1, true> : attn_f32_kernel<D, 1, false>;
-    const auto two = persist ? attn_f32_kernel<D, 2, true> : attn_f32_kernel<D, 2, false>;
+    constexpr Keys A = Keys::kAll, W = Keys::kWindow;
+    const auto one = p.window ? attn_f32_kernel<D, 1, false, W> : persist ? attn_f32_kernel<D, 1, true, A> : attn_f32_kernel<D, 1, false, A>;
+    const auto two = p.window ? attn_f32_kernel<D, 2, false, W> : persist ? attn_f32_kernel<D, 2, true, A> : attn_f32_kernel<D, 2, false, A>;
     return launch(p.groups_per_tile == 1 ? one : two, dim3(n_blocks), dim3(64 * kF32Waves), 0, stream, p);
 }
 
@@ -369,7 +400,7 @@ namespace kvc {
 
 int launch_attn_f32(const AttnParams &p, int D, unsigned n_blocks, hipStream_t stream)
 {
-    if (p.N <= f32_row_keys(D)) {
+    if (p.N <= f32_row_keys(D) && !p.window) {
         const dim3 grid((unsigned)(((int64_t)p.L * p.Hkv * p.G * p.tq + 3) / 4)), block(256);
         switch (D) {
             case 64: return launch(attn_f32_row_kernel<64>, grid, block, 0, stream, p);
@@ -380,6 +411,7 @@ int launch_attn_f32(const AttnParams &p, int D, unsigned n_blocks, hipStream_t s
     }
     n_blocks = std::min<unsigned>(n_blocks, (1u << 23) - 1);   // a launch holds fewer than 2^32 threads
     const bool persist = n_blocks < (unsigned)p.n_items;
+    if (persist && p.window) return KVCOMM_EUNSUPPORTED;   // (millions of blocks)
     switch (D) {
         case 64: return launch_f32<64>(p, persist, n_blocks, stream);
         case 128: return launch_f32<128>(p, persist, n_blocks, stream);

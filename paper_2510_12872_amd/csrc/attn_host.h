@@ -44,6 +44,27 @@ static inline int attn_cache(const kvcomm_model &model, const kvcomm_tensor &k, 
     return KVCOMM_OK;
 }
 
+// The kernels' direct loads address a row group as a 64-bit scalar base plus an unsigned 32-bit per-lane byte
+// offset that spans up to 64 * 8 / D rows: the token stride has to leave that offset below 2^32.
+static inline bool direct_loads_reach(const Strides &cache, int D)
+{
+    const int64_t rows_per_load = 64 * 8 / D;
+    return cache.token < ((int64_t)1 << 31) / (2 * rows_per_load);
+}
+
+// fp32: row tiles of `groups` * 16 packed rows.
+static inline int launch_f32(AttnParams &p, int D, int groups, int max_blocks, hipStream_t s)
+{
+    p.groups_per_tile = groups;
+    const int rows = 16 * groups;
+    p.n_row_tiles = (int32_t)(((int64_t)p.G * p.tq + rows - 1) / rows);
+    const int64_t n_items = (int64_t)p.L * p.Hkv * p.n_row_tiles;
+    if (n_items > 0x7fffffff) return KVCOMM_EUNSUPPORTED;
+    p.n_items = (int32_t)n_items;
+    set_divisors(p);
+    return launch_attn_f32(p, D, (unsigned)(max_blocks > 0 ? std::min(max_blocks, p.n_items) : p.n_items), s);
+}
+
 // The same in 4 bits.
 static inline int attn_cache4(const kvcomm_model &model, const kvcomm_tensor4 &k, const kvcomm_tensor4 &v, AttnParams &p)
 {
@@ -60,7 +81,11 @@ static inline int attn_cache4(const kvcomm_model &model, const kvcomm_tensor4 &k
     return KVCOMM_OK;
 }
 
-// Tokens of a cache whose tiles the kernels count and address with 32-bit integers.
+// Tokens of a cache whose tiles the kernels count with 32-bit integers; a launch holds fewer than 2^32 threads, of 512 in a block (at most 16 runs of 16 rows).
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;
+static inline bool fits_a_launch(const AttnParams &p)
+{
+    return (int64_t)p.n_ctx + p.tq <= kMaxTokens && (double)p.L * p.Hkv * ((double)p.G * p.tq / 16 + 1) < (1 << 23);
+}
 
 }  // namespace kvc

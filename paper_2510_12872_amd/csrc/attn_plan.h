@@ -60,10 +60,10 @@ static inline double attn_tiles_us(const kvcomm_model &m, int64_t items, int til
 // Cuts of the rows kernel pay when they take off more than the combine launch (4 us, its gap and its launch on the
 // host), and only up to one round of blocks.  One decoded token, 3100 keys, in one run / 13: D 64 15.4 / 12.3 us, D 128 20 / 13,
 // D 256 55 / 19.
-static inline AttnPlan attn_plan(const kvcomm_model &m, int n_ctx, int tq, bool may_split)
+static inline AttnPlan attn_plan_keys(const kvcomm_model &m, int64_t N, int tq, bool may_split)   // N: keys that a query sees
 {
     const int G = m.n_q_heads / m.n_kv_heads, D = m.head_dim;
-    const int64_t rows = (int64_t)G * tq, LH = (int64_t)m.n_layers * m.n_kv_heads, N = (int64_t)n_ctx + tq;
+    const int64_t rows = (int64_t)G * tq, LH = (int64_t)m.n_layers * m.n_kv_heads;
 
     const int tile_rows = D == 256 ? 128 : 32 * kAttnWaves;
     const int64_t tile_items = LH * ((rows + tile_rows - 1) / tile_rows), tiles = (N + 63) / 64;
@@ -121,6 +121,18 @@ static inline AttnPlan attn_plan(const kvcomm_model &m, int n_ctx, int tq, bool 
     return pl;
 }
 
+static inline AttnPlan attn_plan(const kvcomm_model &m, int n_ctx, int tq, bool may_split)
+{
+    return attn_plan_keys(m, (int64_t)n_ctx + tq, tq, may_split);
+}
+
+// The same for a window: what a tile of queries walks is their windows and the sinks (a 256-row tile of G = 4 heads has 64 queries).
+static inline AttnPlan attn_plan_window(const kvcomm_model &m, int n_ctx, int tq, int window, int n_sinks, bool may_split)
+{
+    const int64_t N = (int64_t)n_ctx + tq;
+    return attn_plan_keys(m, std::min<int64_t>(N, (int64_t)window + n_sinks + std::min(tq, 64)), tq, may_split);
+}
+
 // (row group, split) pairs of a launch.
 static inline size_t attn_parts(const kvcomm_model &m, const AttnPlan &pl)
 {
@@ -146,6 +158,9 @@ static inline int attn_f32_groups(const kvcomm_model &m, int tq, int max_blocks)
     return (int64_t)m.n_layers * m.n_kv_heads * ((rows + 15) / 16) <= at_once ? 1 : 2;
 }
 
+// Launches a bf16 attention as `plan` says (`uncut` where the scratch does not hold the partial results of its runs).  max_blocks: 0, or as in
+// kvcomm_suffix_attn_confined.
+int launch_attn(const kvcomm_model &m, AttnParams &p, AttnPlan plan, const AttnPlan &uncut, int max_blocks, void *workspace, size_t workspace_bytes, hipStream_t stream);
 int launch_attn_rows(const AttnParams &p, int D, int rows, unsigned n_blocks, hipStream_t stream);
 int launch_attn_f32(const AttnParams &p, int D, unsigned n_blocks, hipStream_t stream);
 int launch_attn_combine(const AttnParams &p, int D, int rows, hipStream_t stream);   // rows: of a group of partial results

@@ -1,5 +1,6 @@
 // bf16 suffix attention for few query rows (decoded tokens, very short suffixes), and the kernel that joins the
 // partial results of a launch that splits the key axis.
+#include "attn_exact.h"
 #include "attn_plan.h"
 
 namespace {
@@ -54,9 +55,13 @@ __device__ __forceinline__ void load_half(const unsigned char *bytes, int64_t to
 // 6.4 TB/s): K and V of a sub-step go global -> LDS into the wavefront's own buffers (no block barrier in the loop),
 // K of the next sub-step is requested as soon as its operands are in registers and V likewise, so a wavefront
 // always has 8 ... 16 KB in flight (D = 128).  Eight wavefronts measured 10 % better than two blocks of four.
-template <int D, bool NT, bool PERSIST>
+// KEYS = kWindow: the sub-steps of the sinks, then those of the windows (window_units()); a block whose results are not all finite computes its rows again by
+// attn_exact_rows(), because a hidden key's value may have been multiplied by its probability 0.
+template <int D, bool NT, bool PERSIST, Keys KEYS>
 __global__ __launch_bounds__(64 * rows_waves(D), D == 256 ? 1 : 2) void attn_rows_kernel(const AttnParams p)
 {
+    constexpr bool kWindow = KEYS == Keys::kWindow;
+    static_assert(!(PERSIST && kWindow), "");
     constexpr int NW = rows_waves(D);
     constexpr int NKS = D / 16, NDB = D / 32, KCH = D / 8, ROWB = D * 2, HALFB = 32 * ROWB;
     constexpr int RPL = 64 / KCH;    // key rows filled by one wavefront-wide direct load
@@ -97,7 +102,10 @@ __global__ __launch_bounds__(64 * rows_waves(D), D == 256 ? 1 : 2) void attn_row
         const int qi = min(i_row, p.tq - 1);
         const int hq = hkv * p.G + r_row - i_row * p.G;
         const int imax = min(p.tq - 1, div_by(rt * 32 + 31, p.by_G)), imin = min(p.tq - 1, div_by(rt * 32, p.by_G));
-        const int units = (p.n_ctx + imax + 32) / 32;   // sub-steps that some query of the tile sees
+        WindowUnits wu = {0, 0, (p.n_ctx + imax + 32) / 32};   // sub-steps that some query of the tile sees
+        if constexpr (kWindow) wu = window_units(p, imin, imax, 32);
+        const int units = wu.count;
+        auto first_key = [&](int u) __attribute__((always_inline)) -> int { return 32 * (kWindow && u >= wu.sinks ? u + wu.gap : u); };
         // split_bound() without a causal edge: s * units / n_splits (<= 2^30: see there)
         const int u0 = div_by(split * units, p.by_splits), u1 = div_by((split + 1) * units, p.by_splits);
 
@@ -106,8 +114,8 @@ __global__ __launch_bounds__(64 * rows_waves(D), D == 256 ? 1 : 2) void attn_row
         uint32_t k_in[KD], v_in[VD];
         lane_offsets<D>(k_in, lane, p.s_k.token, k_swz);
         lane_offsets<D>(v_in, lane, p.s_v.token, v_swz);
-        auto load_k = [&](int u) __attribute__((always_inline)) { load_half<D, NT>(kbytes, p.s_k.token, 32 * u, p.N, k_in, lane, k_swz, kbuf); };
-        auto load_v = [&](int u) __attribute__((always_inline)) { load_half<D, NT>(vbytes, p.s_v.token, 32 * u, p.N, v_in, lane, v_swz, vbuf); };
+        auto load_k = [&](int u) __attribute__((always_inline)) { load_half<D, NT>(kbytes, p.s_k.token, first_key(u), p.N, k_in, lane, k_swz, kbuf); };
+        auto load_v = [&](int u) __attribute__((always_inline)) { load_half<D, NT>(vbytes, p.s_v.token, first_key(u), p.N, v_in, lane, v_swz, vbuf); };
         int u = u0 + wave;
         bf16x8 qf[NKS];
         const bf16_t *qrow = static_cast<const bf16_t *>(p.q) + l * p.s_q.layer + (int64_t)hq * p.s_q.head + (int64_t)qi * p.s_q.token;
@@ -153,7 +161,16 @@ __global__ __launch_bounds__(64 * rows_waves(D), D == 256 ? 1 : 2) void attn_row
 #pragma unroll
             for (int ks = 0; ks < NKS; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], qf[ks], s, 0, 0, 0);
 
-            if (32 * u + 31 > p.n_ctx + imin) {   // some key is hidden from some query
+            if constexpr (kWindow) {
+                const int first = first_key(u), limit = p.n_ctx + qi - first;
+                if (first + 31 > p.n_ctx + imin || first <= p.n_ctx + imax - p.window) {   // some key is hidden from some query
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const int row = 8 * (j >> 2) + 4 * hg + (j & 3);
+                        if (row > limit || (row <= limit - p.window && row >= p.n_sinks - first)) s[j] = -INFINITY;
+                    }
+                }
+            } else if (32 * u + 31 > p.n_ctx + imin) {   // some key is hidden from some query
                 const int limit = p.n_ctx + qi - 32 * u;
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
@@ -210,6 +227,17 @@ __global__ __launch_bounds__(64 * rows_waves(D), D == 256 ? 1 : 2) void attn_row
             for (int i = 0; i < 2 * NDB; ++i) o[i % NDB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[i], pf[i / NDB], o[i % NDB], 0, 0, 0);
         }
 
+        if constexpr (kWindow) {
+            float zero = lsum * 0.f;
+#pragma unroll
+            for (int i = 0; i < 16 * NDB; ++i) zero = fmaf(o[i / 16][i % 16], 0.f, zero);
+            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(lsum), __float_as_uint(lsum), false, false);
+            if (__syncthreads_or(state_is_odd(zero, m, __uint_as_float(sw[0]) + __uint_as_float(sw[1])))) {
+                const KeyRanges keys = {32 * u0, 32 * min(u1, wu.sinks), 32 * (max(u0, wu.sinks) + wu.gap), min(32 * (u1 + wu.gap), p.N)};
+                attn_exact_rows<bf16_t, bf16_t, D>(p, lh, rt * 32, 32, keys, split, 32, wave, NW, lane);
+                return;
+            }
+        }
         // ---- join the wavefronts' states: outputs as they are go over the wavefront's own K / V buffers (no other wavefront
         // reads those), so one barrier does; a thread then owns whole slots (its own n and hg) and sums them over
         // the wavefronts with their factors against the common maximum.
@@ -281,9 +309,11 @@ __global__ __launch_bounds__(64 * rows_waves(D), D == 256 ? 1 : 2) void attn_row
 // the two tiles may begin a sub-step apart).  For confined launches of more tiles than blocks.  us on 160 / 64 / 8 blocks one by one, two at a time (and as tiles
 // of 32 rows on 32x32x16 MFMAs, whose sums are others): 2 layers x 8 heads, G = 4, Tq 64, 364 keys 10.8 / 19.5 / 136, 8.8 / 15.3 / 103 (8.1 / 13.9 / 95);
 // D = 64, one layer, Tq 128, 2128 keys 16.1 / 29.2 / 220, 12.7 / 22.7 / 165 (11.2 / 19.6 / 139); 4 layers, Tq 16, 516 keys on 64 / 8 12.5 / 82, 9.7 / 63 (8.8 / 57).
-template <int D, bool NT, bool PERSIST, int RH>
+template <int D, bool NT, bool PERSIST, int RH, Keys KEYS>
 __global__ __launch_bounds__(64 * rows_waves(D), D == 256 ? 1 : 2) void attn_rows_kernel16(const AttnParams p)
 {
+    constexpr bool kWindow = KEYS == Keys::kWindow;
+    static_assert(!kWindow || (RH == 1 && !PERSIST), "");
     constexpr int NW = rows_waves(D), ROWS = 16;   // rows of a tile
     constexpr int NF = D / 16, KCH = D / 8, ROWB = D * 2, HALFB = 32 * ROWB;
     constexpr int RPL = 64 / KCH;                    // key rows filled by one wavefront-wide direct load
@@ -323,6 +353,8 @@ __global__ __launch_bounds__(64 * rows_waves(D), D == 256 ? 1 : 2) void attn_row
 
         int qi[RH], hq[RH], imin[RH], u0[RH], u1[RH];
         bool valid[RH];
+        WindowUnits wu = {0, 0, 0};
+        int left = 0;   // last key that some query's window has left
 #pragma unroll
         for (int h = 0; h < RH; ++h) {
             const int r_row = (rt0 + h) * ROWS + n, i_row = div_by(r_row, p.by_G);   // (also the row that this thread joins: tid % ROWS == n)
@@ -331,12 +363,18 @@ __global__ __launch_bounds__(64 * rows_waves(D), D == 256 ? 1 : 2) void attn_row
             hq[h] = hkv * p.G + r_row - i_row * p.G;
             const int imax = min(p.tq - 1, div_by((rt0 + h) * ROWS + ROWS - 1, p.by_G));
             imin[h] = min(p.tq - 1, div_by((rt0 + h) * ROWS, p.by_G));
-            const int units = (p.n_ctx + imax + 32) / 32;   // sub-steps that some query of the tile sees
+            int units = (p.n_ctx + imax + 32) / 32;   // sub-steps that some query of the tile sees
+            if constexpr (kWindow) {
+                wu = window_units(p, imin[h], imax, 32);
+                units = wu.count;
+                left = p.n_ctx + imax - p.window;
+            }
             // split_bound() without a causal edge: s * units / n_splits (<= 2^30: see there)
             u0[h] = div_by(split * units, p.by_splits), u1[h] = div_by((split + 1) * units, p.by_splits);
         }
         if (RH == 2 && rt0 + 1 == n_tiles) u0[RH - 1] = u1[RH - 1] = u0[0];   // there is no second tile
         const int u_end = RH == 2 ? max(u1[0], u1[RH - 1]) : u1[0];
+        auto first_key = [&](int u) __attribute__((always_inline)) -> int { return 32 * (kWindow && u >= wu.sinks ? u + wu.gap : u); };
         // 0 or 1, and so the ends: the tiles' last queries are at most 16 keys apart.  1: a wavefront's sub-steps belong to one tile and the other in turn.
         const int apart = u0[RH - 1] - u0[0];
         const int u_end0 = apart ? u1[0] : u_end;   // of turn 0 (that of turn 1 is u_end)
@@ -346,8 +384,8 @@ __global__ __launch_bounds__(64 * rows_waves(D), D == 256 ? 1 : 2) void attn_row
         uint32_t k_in[KD], v_in[VD];
         lane_offsets<D>(k_in, lane, p.s_k.token, k_swz);
         lane_offsets<D>(v_in, lane, p.s_v.token, v_swz);
-        auto load_k = [&](int u) __attribute__((always_inline)) { load_half<D, NT>(kbytes, p.s_k.token, 32 * u, p.N, k_in, lane, k_swz, kbuf); };
-        auto load_v = [&](int u) __attribute__((always_inline)) { load_half<D, NT>(vbytes, p.s_v.token, 32 * u, p.N, v_in, lane, v_swz, vbuf); };
+        auto load_k = [&](int u) __attribute__((always_inline)) { load_half<D, NT>(kbytes, p.s_k.token, first_key(u), p.N, k_in, lane, k_swz, kbuf); };
+        auto load_v = [&](int u) __attribute__((always_inline)) { load_half<D, NT>(vbytes, p.s_v.token, first_key(u), p.N, v_in, lane, v_swz, vbuf); };
         int u = u0[0] + wave, turn = 0;
         bf16x8 qf[RH][NF / 2];
 #pragma unroll
@@ -401,7 +439,17 @@ __global__ __launch_bounds__(64 * rows_waves(D), D == 256 ? 1 : 2) void attn_row
                 for (int h = H0; h < H1; ++h)
                     s[h][i & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[i], qf[h][i >> 1], i < 2 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[h][i & 1], 0, 0, 0);
 
-            if (32 * u + 31 > p.n_ctx + imin[H0]) {   // some key is hidden from some query (imin grows from tile to tile)
+            if constexpr (kWindow) {
+                const int first = first_key(u);
+                if (first + 31 > p.n_ctx + imin[0] || first <= left) {   // some key is hidden from some query
+                    const int limit = p.n_ctx + qi[0] - first - 4 * g, sinks = p.n_sinks - first - 4 * g;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int row = 16 * (j >> 2) + (j & 3);
+                        if (row > limit || (row <= limit - p.window && row >= sinks)) s[0][j >> 2][j & 3] = -INFINITY;
+                    }
+                }
+            } else if (32 * u + 31 > p.n_ctx + imin[H0]) {   // some key is hidden from some query (imin grows from tile to tile)
 #pragma unroll
                 for (int h = H0; h < H1; ++h) {
                     const int limit = p.n_ctx + qi[h] - 32 * u - 4 * g;
@@ -481,6 +529,16 @@ __global__ __launch_bounds__(64 * rows_waves(D), D == 256 ? 1 : 2) void attn_row
             }
         }
 
+        if constexpr (kWindow) {
+            float zero = lsum[0] * 0.f;
+#pragma unroll
+            for (int i = 0; i < 4 * NF; ++i) zero = fmaf(o[0][i / 4][i % 4], 0.f, zero);
+            if (__syncthreads_or(state_is_odd(zero, m[0], query_sum(lsum[0])))) {
+                const KeyRanges keys = {32 * u0[0], 32 * min(u1[0], wu.sinks), 32 * (max(u0[0], wu.sinks) + wu.gap), min(32 * (u1[0] + wu.gap), p.N)};
+                attn_exact_rows<bf16_t, bf16_t, D>(p, lh, rt0 * ROWS, ROWS, keys, split, ROWS, wave, NW, lane);
+                return;
+            }
+        }
         // ---- join the wavefronts' states as in attn_rows_kernel.  Lane (n, g) holds channels 16 * db + 4 * g ... + 3 of row n: slot
         // (4 * db + g, n).
         f32x4 *join = reinterpret_cast<f32x4 *>(smem);
@@ -727,13 +785,17 @@ int launch_rows(const AttnParams &p, int rows, bool nt, bool persist, unsigned n
         pairs.n_row_tiles = (p.n_row_tiles + 1) / 2;
         pairs.by_row_tiles = make_divisor((uint32_t)pairs.n_row_tiles);
         pairs.n_items = p.n_items / p.n_row_tiles * pairs.n_row_tiles;
-        return launch(attn_rows_kernel16<D, false, true, 2>, dim3(std::min(n_blocks, (unsigned)pairs.n_items)), block, 0, stream, pairs);
+        return launch(attn_rows_kernel16<D, false, true, 2, Keys::kAll>, dim3(std::min(n_blocks, (unsigned)pairs.n_items)), block, 0, stream, pairs);
     }
     const dim3 grid(n_blocks);
-    const auto rows16 = persist ? (nt ? attn_rows_kernel16<D, true, true, 1> : attn_rows_kernel16<D, false, true, 1>)
-                                : (nt ? attn_rows_kernel16<D, true, false, 1> : attn_rows_kernel16<D, false, false, 1>);
-    const auto rows32 = persist ? (nt ? attn_rows_kernel<D, true, true> : attn_rows_kernel<D, false, true>)
-                                : (nt ? attn_rows_kernel<D, true, false> : attn_rows_kernel<D, false, false>);
+    constexpr Keys A = Keys::kAll, W = Keys::kWindow;
+    const bool window = p.window != 0;
+    const auto rows16 = window    ? (nt ? attn_rows_kernel16<D, true, false, 1, W> : attn_rows_kernel16<D, false, false, 1, W>)
+                        : persist ? (nt ? attn_rows_kernel16<D, true, true, 1, A> : attn_rows_kernel16<D, false, true, 1, A>)
+                                  : (nt ? attn_rows_kernel16<D, true, false, 1, A> : attn_rows_kernel16<D, false, false, 1, A>);
+    const auto rows32 = window    ? (nt ? attn_rows_kernel<D, true, false, W> : attn_rows_kernel<D, false, false, W>)
+                        : persist ? (nt ? attn_rows_kernel<D, true, true, A> : attn_rows_kernel<D, false, true, A>)
+                                  : (nt ? attn_rows_kernel<D, true, false, A> : attn_rows_kernel<D, false, false, A>);
     return launch(rows == 16 ? rows16 : rows32, grid, block, 0, stream, p);
 }
 
@@ -745,7 +807,8 @@ int launch_attn_rows(const AttnParams &p, int D, int rows, unsigned n_blocks, hi
 {
     // Non-temporal K / V only where they cannot stay in the last-level cache and no other block reads them: 32 layers
     // of 3100 keys (407 MB) take 64 us with it and 72 us without, 4 layers (51 MB, read again for the next token) 33 and 26.
-    const bool nt = p.n_row_tiles == 1 && (int64_t)p.L * p.Hkv * p.N * D * 4 > kLastLevelCache;
+    const int64_t keys = p.window ? std::min<int64_t>(p.N, (int64_t)p.window + p.n_sinks) : p.N;
+    const bool nt = p.n_row_tiles == 1 && (int64_t)p.L * p.Hkv * keys * D * 4 > kLastLevelCache;
     const bool persist = n_blocks < (unsigned)p.n_items;
     switch (D) {
         case 64: return launch_rows<64>(p, rows, nt, persist, n_blocks, stream);

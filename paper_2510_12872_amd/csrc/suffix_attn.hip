@@ -44,11 +44,39 @@
 // fp32 path: attn_f32.hip.
 #include <float.h>
 
+#include "attn_exact.h"
 #include "attn_host.h"
 
 namespace {
 
 using namespace kvc;
+
+// The whole work item of a block by attn_exact_rows().  All that it needs is formed again from the parameters, read through an opaque pointer to the
+// kernel-argument segment: the tile loops then hold nothing for it.
+template <int D, int NW, bool SPLIT>
+__device__ __forceinline__ void exact_tile()
+{
+    typedef const __attribute__((address_space(4))) AttnParams ParamT;
+    ParamT *ptr = (ParamT *)__builtin_amdgcn_kernarg_segment_ptr();
+    int block = blockIdx.x, tid = threadIdx.x;
+    asm volatile("" : "+s"(ptr));
+    asm volatile("" : "+s"(block));
+    ParamT &p = *ptr;
+    constexpr int BM = 32 * NW;
+    const int x_id = block & 7;
+    int logical = x_id * (p.n_items >> 3) + min(x_id, p.n_items & 7) + (block >> 3), split = 0;
+    if (SPLIT) {
+        const int rest = div_by(logical, p.by_splits);
+        split = logical - rest * p.n_splits;
+        logical = rest;
+    }
+    const int lh = div_by(logical, p.by_row_tiles), rt = p.n_row_tiles - 1 - (logical - lh * p.n_row_tiles);
+    const int imin = min(p.tq - 1, div_by(rt * BM, p.by_G)), imax = min(p.tq - 1, div_by(rt * BM + BM - 1, p.by_G));
+    const WindowUnits wu = window_units(p, imin, imax, 64);
+    const int begin = SPLIT ? div_by(split * wu.count, p.by_splits) : 0, end = SPLIT && split + 1 < p.n_splits ? div_by((split + 1) * wu.count, p.by_splits) : wu.count;
+    const KeyRanges keys = {64 * begin, 64 * min(end, wu.sinks), 64 * (max(begin, wu.sinks) + wu.gap), min(64 * (end + wu.gap), p.N)};
+    attn_exact_rows<bf16_t, bf16_t, D>(p, lh, rt * BM, BM, keys, split, 32, __builtin_amdgcn_readfirstlane(tid >> 6), NW, tid & 63);
+}
 
 // ------------------------------------------------------------------------------- bf16 MFMA
 // PERSIST: the grid is smaller than the number of (layer, kv head, row tile) items and every block walks a
@@ -58,8 +86,13 @@ using namespace kvc;
 // SPLIT: an item is one run of key tiles of a row tile.  The block works on the cache as if it began at the run's
 // first key (which all its queries see) and leaves unnormalised outputs, references and row sums in the workspace;
 // attn_combine_kernel joins them.
-template <int D, int NW, int WPE, bool PERSIST, bool SPLIT>
-__global__ __launch_bounds__(64 * NW, WPE) void attn_mfma_kernel(const AttnParams p_arg)
+// KEYS = kWindow: the block walks the tiles of the sinks, then those of its queries' windows (window_units()), as if they lay behind each other.  The
+// first pairs of tiles, where some query does not see some key, are masked like the last; a block whose results are not all finite computes its
+// rows again by attn_exact_rows(), because a hidden key's value may have been multiplied by its probability 0.
+// FORM: wavefronts per SIMD + form(KEYS) (one argument for both: a whole cache's kernels keep the names that the profiles have).
+constexpr int form(Keys keys) { return 16 * (int)keys; }
+template <int D, int NW, int FORM, bool PERSIST, bool SPLIT>
+__global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const AttnParams p_arg)
 {
     // PERSIST reads the parameters through an opaque pointer to the kernel-argument segment, once per item:
     // they are then re-loaded (scalar loads) for every item instead of being held in scalar registers for the
@@ -71,6 +104,9 @@ __global__ __launch_bounds__(64 * NW, WPE) void attn_mfma_kernel(const AttnParam
     else
         p_ptr = &p_arg;
     ParamT &p0 = *p_ptr;
+    constexpr Keys KEYS = (Keys)(FORM / 16);
+    constexpr bool kWindow = KEYS == Keys::kWindow;
+    static_assert(!(PERSIST && kWindow), "the persistent form reads its parameters in its own way");
     constexpr int NF = D / 16;       // K operands of a sub-step (contraction step, key half), V^T operands (16 channels)
     constexpr int BM = 32 * NW;      // query rows per block (32 per wavefront)
     constexpr int RW = 64 / NW;      // key rows of a 64-key group that one wavefront loads
@@ -138,8 +174,15 @@ __global__ __launch_bounds__(64 * NW, WPE) void attn_mfma_kernel(const AttnParam
     const int wg_imin = min(p.tq - 1, div_by(rt * BM, p.by_G));
     const int all_tiles = (p.n_ctx + wg_imax + 1 + 63) / 64;
     const int first_hidden = (p.n_ctx + wg_imin) / 64 + 1;
-    const int tile0 = SPLIT ? split_bound(split, p.n_splits, all_tiles, first_hidden) : 0;
-    const int n_tiles = SPLIT ? split_bound(split + 1, p.n_splits, all_tiles, first_hidden) - tile0 : all_tiles;
+    WindowUnits wu = {0, 0, all_tiles};
+    if constexpr (kWindow) wu = window_units(p, wg_imin, wg_imax, 64);
+    // (a run of a window may begin with keys that some query does not see: the reference of such a row is set later)
+    auto bound = [&](int s) __attribute__((always_inline)) -> int {
+        return kWindow ? div_by(s * wu.count, p.by_splits) : split_bound(s, p.n_splits, all_tiles, first_hidden);
+    };
+    const int tile0 = SPLIT ? bound(split) : 0;
+    const int n_tiles = SPLIT ? bound(split + 1) - tile0 : wu.count;
+    const int sink_tiles = kWindow ? max(0, wu.sinks - tile0) : 0;   // of this run
     if constexpr (SPLIT) {
         if (n_tiles <= 0) {   // the whole block: this run is empty
             if (lane < 32 && div_by(rt * BM + wave * 32 + lane, p.by_G) < p.tq) {
@@ -151,13 +194,18 @@ __global__ __launch_bounds__(64 * NW, WPE) void attn_mfma_kernel(const AttnParam
             item += x_blocks;
             continue;
         }
-        kb_ += (int64_t)(64 * tile0) * p.s_k.token;
-        vb_ += (int64_t)(64 * tile0) * p.s_v.token;
     }
-    // Context length and cache length counted from the run's first key (n_ctx_() may be negative; every query of
+    // Tile t of the run begins at key 64 * (t + origin); a tile of the sinks lies 64 * gap keys before that.
+    const int origin = tile0 + wu.gap;
+    if constexpr (SPLIT || kWindow) {
+        kb_ += (int64_t)(64 * origin) * p.s_k.token;
+        vb_ += (int64_t)(64 * origin) * p.s_v.token;
+    }
+    auto tile_shift = [&](int t) __attribute__((always_inline)) -> int { return kWindow && t < sink_tiles ? -64 * wu.gap : 0; };
+    // Context length and cache length counted from key 64 * origin (n_ctx_() may be negative; without a window every query of
     // the tile still sees key 0 of the run).
-    auto n_ctx_ = [&]() __attribute__((always_inline)) -> int { return SPLIT ? p.n_ctx - 64 * tile0 : p.n_ctx; };
-    auto N_ = [&]() __attribute__((always_inline)) -> int { return SPLIT ? p.N - 64 * tile0 : p.N; };
+    auto n_ctx_ = [&]() __attribute__((always_inline)) -> int { return SPLIT || kWindow ? p.n_ctx - 64 * origin : p.n_ctx; };
+    auto N_ = [&]() __attribute__((always_inline)) -> int { return SPLIT || kWindow ? p.N - 64 * origin : p.N; };
     const int n_sub = 2 * n_tiles;
     const int sub_unmasked = (n_ctx_() + wg_imin + 1) / 32;  // sub-steps [0, sub_unmasked) are visible to all queries
 
@@ -209,14 +257,14 @@ __global__ __launch_bounds__(64 * NW, WPE) void attn_mfma_kernel(const AttnParam
         const int rbase = (wave % (NW / 2)) * RW;
 #pragma unroll
         for (int it = 0; it < LPT; ++it)
-            load_rows(kbytes, p.s_k.token, k_row_bytes, 32 * h + rbase + it * RPL, ld_koff[it],
+            load_rows(kbytes, p.s_k.token, k_row_bytes, 32 * h + tile_shift(h >> 1) + rbase + it * RPL, ld_koff[it],
                       kring + (h & 3) * HALFB + (rbase + it * RPL) * ROWB);
     };
     auto load_v64 = [&](int tile) __attribute__((always_inline)) {
         if (tile >= n_tiles) return;
 #pragma unroll
         for (int it = 0; it < LPT; ++it)
-            load_rows(vbytes, p.s_v.token, v_row_bytes, 64 * tile + wave * RW + it * RPL, ld_voff[it],
+            load_rows(vbytes, p.s_v.token, v_row_bytes, 64 * tile + tile_shift(tile) + wave * RW + it * RPL, ld_voff[it],
                       vbuf + (tile & 1) * TILEB + (wave * RW + it * RPL) * ROWB);
     };
     // The first tiles are requested before anything else is set up: their latency is the block's start-up time.
@@ -241,10 +289,13 @@ __global__ __launch_bounds__(64 * NW, WPE) void attn_mfma_kernel(const AttnParam
     // so that a load costs one 64-bit scalar add instead of a 64-bit multiply, and with M0 formed from
     // a per-wavefront LDS base plus a literal.  kp / vp point at this wavefront's next row to load:
     // during tile t the K halves 2t+4, 2t+5 (keys 64t+128 ...) and V tile t+1.
+    // First tile (even) of those pairs, which have no tile of the sinks and whose exponentials, of sub-steps from 2t+1 on, are of keys that no window has left.
+    const int left = kWindow ? n_ctx_() + wg_imax - p.window : -1;   // last key that some query has left
+    const int t_plain0 = kWindow ? (max(sink_tiles, left < 0 ? 0 : (left / 32 + 1) / 2) + 1) & ~1 : 0;
     const int64_t k_rpl = (int64_t)RPL * p.s_k.token * 2, v_rpl = (int64_t)RPL * p.s_v.token * 2;
     const int64_t k_adv = (int64_t)(64 - LPT * RPL) * p.s_k.token * 2, v_adv = (int64_t)(64 - LPT * RPL) * p.s_v.token * 2;
-    const unsigned char *kp = kbytes + (int64_t)(128 + 32 * (wave / (NW / 2)) + (wave % (NW / 2)) * RW) * p.s_k.token * 2;
-    const unsigned char *vp = vbytes + (int64_t)(64 + wave * RW) * p.s_v.token * 2;
+    const unsigned char *kp = kbytes + (int64_t)(64 * t_plain0 + 128 + 32 * (wave / (NW / 2)) + (wave % (NW / 2)) * RW) * p.s_k.token * 2;
+    const unsigned char *vp = vbytes + (int64_t)(64 * t_plain0 + 64 + wave * RW) * p.s_v.token * 2;
     const uint32_t lds0 = (uint32_t)(uintptr_t)kring;
     const uint32_t k_rows = lds0 + (wave % (NW / 2)) * RW * ROWB;
     // t even: halves 2t+4, 2t+5 live in slots 0, 1; t odd: in slots 2, 3
@@ -306,8 +357,8 @@ __global__ __launch_bounds__(64 * NW, WPE) void attn_mfma_kernel(const AttnParam
     // what its own slot produced: element j is scaled in slot b-2, exponentiated in slot b-1 and
     // summed / packed in slot b = j * NS / 16 (slots -2 and -1 precede the first MFMA).  A wavefront issues in
     // order, so a dependent chain inside one slot would hold back the next MFMA for its whole latency.
-    // Element j is key row 16 * kh + 4 * g4 + r of the sub-step for query half j / 8, kh = j / 4 % 2, r = j % 4; `limit`
-    // plus the query's index is its last visible key.
+    // Element j is key row 16 * kh + 4 * g4 + r of the sub-step for query half j / 8, kh = j / 4 % 2, r = j % 4; `limit.last`
+    // plus the query's index is its last visible key, rows before `limit.sinks` are sinks.
     // Row sums are plain fp32 additions of the unrounded exponentials: v_dot2 on the rounded pairs
     // would agree with the numerator to the last bit, but it shares a pipeline with the MFMAs and costs four
     // times as much next to them; the difference is a relative 2^-9 / sqrt(keys) of the denominator.
@@ -315,11 +366,22 @@ __global__ __launch_bounds__(64 * NW, WPE) void attn_mfma_kernel(const AttnParam
         float x[16], e[16], rs[2];
     };
     typedef f32x4 Scores[2][2];
-    auto score = [&](const Scores &s, int j, int limit, bool masked) __attribute__((always_inline)) -> float {
-        const int h = j >> 3, kh = (j >> 2) & 1, r = j & 3;
-        return masked && 16 * kh + 4 * g4 + r > limit + qi[h] ? -INFINITY : s[kh][h][r];
+    struct Limit {
+        int last, sinks;
     };
-    auto exp_slot = [&](const Scores &s, u32x4 (&pk)[2], ExpState &st, int limit, bool masked, int t, int NS)
+    auto limit_of = [&](int u) __attribute__((always_inline)) -> Limit {   // of sub-step u
+        const int first = 32 * u + tile_shift(u >> 1);
+        return Limit{n_ctx_() - first, kWindow ? p.n_sinks - first - 64 * origin : 0};
+    };
+    auto score = [&](const Scores &s, int j, Limit limit, bool masked) __attribute__((always_inline)) -> float {
+        const int h = j >> 3, kh = (j >> 2) & 1, r = j & 3;
+        if constexpr (kWindow) {
+            const int row = 16 * kh + 4 * g4 + r, last = limit.last + qi[h];
+            return masked && (row > last || (row <= last - p.window && row >= limit.sinks)) ? -INFINITY : s[kh][h][r];
+        }
+        return masked && 16 * kh + 4 * g4 + r > limit.last + qi[h] ? -INFINITY : s[kh][h][r];
+    };
+    auto exp_slot = [&](const Scores &s, u32x4 (&pk)[2], ExpState &st, Limit limit, bool masked, int t, int NS)
                         __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
@@ -339,7 +401,7 @@ __global__ __launch_bounds__(64 * NW, WPE) void attn_mfma_kernel(const AttnParam
     // A row whose exponentials left the safe range (or the first sub-step, whose reference is still -inf): take
     // the true maximum of the sub-step as the new reference if it is larger, rescale what has been accumulated,
     // and form the exponentials again.  Rare: the reference only ever moves by more than log2(kOverflow).
-    auto rereference = [&](const Scores &s, u32x4 (&pk)[2], ExpState &st, int limit, bool masked) __attribute__((always_inline)) {
+    auto rereference = [&](const Scores &s, u32x4 (&pk)[2], ExpState &st, Limit limit, bool masked) __attribute__((always_inline)) {
         if (kAccO || !masked) mfma_settle<kAccO>(o);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -372,13 +434,14 @@ __global__ __launch_bounds__(64 * NW, WPE) void attn_mfma_kernel(const AttnParam
         constexpr bool DO_QK = decltype(do_qk_c)::value, DO_EXP = decltype(do_exp_c)::value, MASKED = decltype(masked_c)::value;
         constexpr int NS = 4 * NF;   // slots: the MFMAs of both products
         // The compiler copies operands right before the MFMAs of masked sub-steps, and moves scores of D = 256 between register files.
+        // (Through windows at D = 256 it also copies results right behind them: no inline assembly there.)
         constexpr Mfma HOW_S = !MASKED && !kAccO ? Mfma::kInPlace : Mfma::kBuiltin;
-        constexpr Mfma HOW_O = !MASKED ? Mfma::kInPlace : kAccO ? Mfma::kGuarded : Mfma::kBuiltin;
+        constexpr Mfma HOW_O = kAccO && kWindow ? Mfma::kBuiltin : !MASKED ? Mfma::kInPlace : kAccO ? Mfma::kGuarded : Mfma::kBuiltin;
         Scores &s_acc = sbuf[U4 & 1];
         const Scores &s_exp = sbuf[(U4 + 1) & 1];
         const lds_byte *kl = kring + ((U4 + 2) & 3) * HALFB;
         const lds_byte *vl = vbuf + ((U4 >> 1) & 1) * TILEB + (U4 & 1) * HALFB;
-        const int limit = n_ctx_() - 32 * (u + 1);  // last key of S(u+1), relative to its sub-step, that query 0 sees
+        const Limit limit = limit_of(u + 1);
         bf16x8 ka[NF], va[NF], pf[2];
         pf[0] = as_bf16x8(pbuf[U4 & 1][0]);
         pf[1] = as_bf16x8(pbuf[U4 & 1][1]);
@@ -453,7 +516,7 @@ __global__ __launch_bounds__(64 * NW, WPE) void attn_mfma_kernel(const AttnParam
             }
         }
         ExpState st;
-        rereference(sbuf[0], pbuf[0], st, n_ctx_(), true);
+        rereference(sbuf[0], pbuf[0], st, limit_of(0), true);
         lsum[0] = st.rs[0];
         lsum[1] = st.rs[1];
     }
@@ -491,6 +554,10 @@ __global__ __launch_bounds__(64 * NW, WPE) void attn_mfma_kernel(const AttnParam
         tile_barrier();
     };
     int t = 0;
+    if constexpr (kWindow) {
+        for (; t < t_plain0 && t + 2 <= t_last; t += 2) tile_pair(t, F_{});
+        mfma_settle<kAccO>(o);
+    }
     for (; t + 2 <= t_plain; t += 2) tile_pair(t, T_{});
     mfma_settle<kAccO>(o);
     for (; t + 2 <= t_last; t += 2) tile_pair(t, F_{});
@@ -509,6 +576,20 @@ __global__ __launch_bounds__(64 * NW, WPE) void attn_mfma_kernel(const AttnParam
     }
 
     if (kAccO) mfma_settle<kAccO>(o);
+    if constexpr (kWindow) {
+        bool odd = false;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float zero = lsum[h] * 0.f;
+#pragma unroll
+            for (int i = 0; i < 4 * NF; ++i) zero = fmaf(o[h][i / 4][i % 4], 0.f, zero);
+            odd |= state_is_odd(zero, m[h], query_sum(lsum[h]));
+        }
+        if (__syncthreads_or(odd)) {
+            exact_tile<D, NW, SPLIT>();
+            return;
+        }
+    }
     if constexpr (SPLIT) {
         // ---- epilogue of a split: accumulators as they are (256-byte runs per store), reference and row sum.
         const int64_t part = ((int64_t)(lh * p.n_row_tiles + rt) * NW + wave) * p.n_splits + split;
@@ -603,6 +684,9 @@ template <int D, int NW, int WPE>
 int launch_mfma(const AttnParams &p, unsigned n_blocks, bool persist, hipStream_t s)
 {
     const dim3 grid(n_blocks), block(64 * NW);
+    if (p.window)
+        return p.n_splits > 1 ? launch(attn_mfma_kernel<D, NW, WPE + form(Keys::kWindow), false, true>, grid, block, 0, s, p)
+                              : launch(attn_mfma_kernel<D, NW, WPE + form(Keys::kWindow), false, false>, grid, block, 0, s, p);
     if (p.n_splits > 1)
         return persist ? launch(attn_mfma_kernel<D, NW, WPE, true, true>, grid, block, 0, s, p)
                        : launch(attn_mfma_kernel<D, NW, WPE, false, true>, grid, block, 0, s, p);
@@ -624,40 +708,32 @@ int suffix_attn(const kvcomm_model *model, kvcomm_tensor q, kvcomm_tensor cache_
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int D = model->head_dim;
 
-    if (model->dtype == KVCOMM_F32) {
-        p.groups_per_tile = attn_f32_groups(*model, tq, max_blocks);
-        const int rows = 16 * p.groups_per_tile;
-        p.n_row_tiles = (int32_t)(((int64_t)p.G * tq + rows - 1) / rows);
-        const int64_t n_items = (int64_t)p.L * p.Hkv * p.n_row_tiles;
-        if (n_items > 0x7fffffff) return KVCOMM_EUNSUPPORTED;
-        p.n_items = (int32_t)n_items;
-        set_divisors(p);
-        return launch_attn_f32(p, D, (unsigned)(max_blocks > 0 ? std::min(max_blocks, p.n_items) : p.n_items), s);
-    }
+    if (model->dtype == KVCOMM_F32) return launch_f32(p, D, attn_f32_groups(*model, tq, max_blocks), max_blocks, s);
+    if (!direct_loads_reach(p.s_k, D) || !direct_loads_reach(p.s_v, D)) return KVCOMM_EUNSUPPORTED;
+    return launch_attn(*model, p, attn_plan(*model, n_ctx, tq, true), attn_plan(*model, n_ctx, tq, false), max_blocks, workspace, workspace_bytes, s);
+}
 
-    // The direct loads address a row group as a 64-bit scalar base plus an unsigned 32-bit per-lane byte
-    // offset that spans up to 64 * 8 / D rows: the token stride has to leave that offset below 2^32.
-    const int64_t rows_per_load = 64 * 8 / D;
-    const int64_t max_tok = ((int64_t)1 << 31) / (2 * rows_per_load);
-    if (cache_k.stride_token >= max_tok || cache_v.stride_token >= max_tok) return KVCOMM_EUNSUPPORTED;
+}  // namespace
 
-    AttnPlan plan = attn_plan(*model, n_ctx, tq, true);
-    size_t need = attn_workspace(*model, plan);
-    if (plan.n_splits > 1 && (!workspace || workspace_bytes < need || !aligned16(workspace))) {
-        plan = attn_plan(*model, n_ctx, tq, false);
-        need = 0;
-    }
+namespace kvc {
+
+int launch_attn(const kvcomm_model &m, AttnParams &p, AttnPlan plan, const AttnPlan &uncut, int max_blocks, void *workspace, size_t workspace_bytes, hipStream_t s)
+{
+    const int D = m.head_dim;
+    const size_t need = attn_workspace(m, plan);
+    if (plan.n_splits > 1 && (!workspace || workspace_bytes < need || !aligned16(workspace))) plan = uncut;
     p.n_row_tiles = plan.n_row_tiles;
     p.n_splits = plan.n_splits;
     p.groups_per_tile = plan.tile_rows / plan.group_rows;
     p.n_items = p.L * p.Hkv * p.n_row_tiles * p.n_splits;
     if (p.n_splits > 1) {
         p.part_o = static_cast<float *>(workspace);
-        p.part_ml = p.part_o + attn_parts(*model, plan) * (size_t)(plan.group_rows * D);
+        p.part_ml = p.part_o + attn_parts(m, plan) * (size_t)(plan.group_rows * D);
     }
     set_divisors(p);
     const bool persist = max_blocks > 0 && max_blocks < p.n_items;
     const unsigned n_blocks = persist ? (unsigned)max_blocks : (unsigned)p.n_items;
+    int st;
     if (plan.rows_kernel) {
         st = launch_attn_rows(p, D, plan.tile_rows, n_blocks, s);
     } else {
@@ -671,7 +747,7 @@ int suffix_attn(const kvcomm_model *model, kvcomm_tensor q, kvcomm_tensor cache_
     return launch_attn_combine(p, D, plan.group_rows, s);
 }
 
-}  // namespace
+}  // namespace kvc
 
 extern "C" int kvcomm_suffix_attn(const kvcomm_model *model, kvcomm_tensor q, kvcomm_tensor cache_k,
                                   kvcomm_tensor cache_v, int32_t n_ctx, int32_t tq, float softmax_scale,
