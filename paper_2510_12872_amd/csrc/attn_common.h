@@ -32,8 +32,8 @@ struct AttnParams {
     const uint8_t *k_scales, *v_scales;
     Strides s_ks, s_vs;
 };
-// What the keys of a launch are: a whole cache, or a cache of which a query sees its window and the sinks.
-enum class Keys { kAll, kWindow };
+// What the keys of a launch are: a whole cache, a cache of which a query sees its window and the sinks, a whole cache in 4 bits.
+enum class Keys { kAll, kWindow, kFp4 };
 
 // The units (of `unit` keys) that the queries imin ... imax of a tile see through their windows, in order: `sinks` of them from key 0 on, which end
 // before the first unit of the windows, then those; unit u begins at key unit * (u + (u < sinks ? 0 : gap)).

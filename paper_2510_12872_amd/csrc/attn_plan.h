@@ -162,6 +162,7 @@ static inline int attn_f32_groups(const kvcomm_model &m, int tq, int max_blocks)
 // kvcomm_suffix_attn_confined.
 int launch_attn(const kvcomm_model &m, AttnParams &p, AttnPlan plan, const AttnPlan &uncut, int max_blocks, void *workspace, size_t workspace_bytes, hipStream_t stream);
 int launch_attn_rows(const AttnParams &p, int D, int rows, unsigned n_blocks, hipStream_t stream);
+int launch_attn_kv4_rows(const AttnParams &p, int D, unsigned n_blocks, hipStream_t stream);
 int launch_attn_f32(const AttnParams &p, int D, unsigned n_blocks, hipStream_t stream);
 int launch_attn_combine(const AttnParams &p, int D, int rows, hipStream_t stream);   // rows: of a group of partial results
 

@@ -51,9 +51,13 @@ namespace {
 
 using namespace kvc;
 
+// First unit of run s of `units`, cut evenly.
+template <class P>
+__device__ __forceinline__ int even_bound(int s, const P &p, int units) { return div_by(s * units, p.by_splits); }   // (at most 16 * 2^24)
+
 // The whole work item of a block by attn_exact_rows().  All that it needs is formed again from the parameters, read through an opaque pointer to the
 // kernel-argument segment: the tile loops then hold nothing for it.
-template <int D, int NW, bool SPLIT>
+template <int D, int NW, bool SPLIT, Keys KEYS>
 __device__ __forceinline__ void exact_tile()
 {
     typedef const __attribute__((address_space(4))) AttnParams ParamT;
@@ -72,10 +76,11 @@ __device__ __forceinline__ void exact_tile()
     }
     const int lh = div_by(logical, p.by_row_tiles), rt = p.n_row_tiles - 1 - (logical - lh * p.n_row_tiles);
     const int imin = min(p.tq - 1, div_by(rt * BM, p.by_G)), imax = min(p.tq - 1, div_by(rt * BM + BM - 1, p.by_G));
-    const WindowUnits wu = window_units(p, imin, imax, 64);
-    const int begin = SPLIT ? div_by(split * wu.count, p.by_splits) : 0, end = SPLIT && split + 1 < p.n_splits ? div_by((split + 1) * wu.count, p.by_splits) : wu.count;
+    WindowUnits wu = {0, 0, (p.n_ctx + imax) / 64 + 1};
+    if (KEYS == Keys::kWindow) wu = window_units(p, imin, imax, 64);
+    const int begin = SPLIT ? even_bound(split, p, wu.count) : 0, end = SPLIT ? even_bound(split + 1, p, wu.count) : wu.count;
     const KeyRanges keys = {64 * begin, 64 * min(end, wu.sinks), 64 * (max(begin, wu.sinks) + wu.gap), min(64 * (end + wu.gap), p.N)};
-    attn_exact_rows<bf16_t, bf16_t, D>(p, lh, rt * BM, BM, keys, split, 32, __builtin_amdgcn_readfirstlane(tid >> 6), NW, tid & 63);
+    attn_exact_rows<std::conditional_t<KEYS == Keys::kFp4, fp4_t, bf16_t>, bf16_t, D>(p, lh, rt * BM, BM, keys, split, 32, __builtin_amdgcn_readfirstlane(tid >> 6), NW, tid & 63);
 }
 
 // ------------------------------------------------------------------------------- bf16 MFMA
@@ -106,7 +111,10 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     ParamT &p0 = *p_ptr;
     constexpr Keys KEYS = (Keys)(FORM / 16);
     constexpr bool kWindow = KEYS == Keys::kWindow;
-    static_assert(!(PERSIST && kWindow), "the persistent form reads its parameters in its own way");
+    constexpr bool kFp4 = KEYS == Keys::kFp4;
+    constexpr bool kChecked = kWindow || kFp4;   // blocks whose results are not all finite compute their rows again
+    static_assert(!(PERSIST && kChecked), "the persistent form reads its parameters in its own way");
+    using Cache = std::conditional_t<kFp4, uint8_t, bf16_t>;
     constexpr int NF = D / 16;       // K operands of a sub-step (contraction step, key half), V^T operands (16 channels)
     constexpr int BM = 32 * NW;      // query rows per block (32 per wavefront)
     constexpr int RW = 64 / NW;      // key rows of a 64-key group that one wavefront loads
@@ -165,8 +173,8 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     const int rt = p.n_row_tiles - 1 - (logical - lh * p.n_row_tiles);  // longest rows first
     const int l = div_by(lh, p.by_Hkv), hkv = lh - l * p.Hkv;
 
-    const bf16_t *kb_ = static_cast<const bf16_t *>(p.k) + l * p.s_k.layer + hkv * p.s_k.head;
-    const bf16_t *vb_ = static_cast<const bf16_t *>(p.v) + l * p.s_v.layer + hkv * p.s_v.head;
+    const Cache *kb_ = static_cast<const Cache *>(p.k) + l * p.s_k.layer + hkv * p.s_k.head;
+    const Cache *vb_ = static_cast<const Cache *>(p.v) + l * p.s_v.layer + hkv * p.s_v.head;
 
     // Every wavefront of the block walks the same tiles (one barrier per 64-key tile); the causal
     // mask is applied from the first 32-key sub-step that is partly hidden from some query of the block.
@@ -176,9 +184,9 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     const int first_hidden = (p.n_ctx + wg_imin) / 64 + 1;
     WindowUnits wu = {0, 0, all_tiles};
     if constexpr (kWindow) wu = window_units(p, wg_imin, wg_imax, 64);
-    // (a run of a window may begin with keys that some query does not see: the reference of such a row is set later)
+    // (a run cut evenly may begin with keys that some query does not see: the reference of such a row is set later)
     auto bound = [&](int s) __attribute__((always_inline)) -> int {
-        return kWindow ? div_by(s * wu.count, p.by_splits) : split_bound(s, p.n_splits, all_tiles, first_hidden);
+        return kChecked ? even_bound(s, p, wu.count) : split_bound(s, p.n_splits, all_tiles, first_hidden);
     };
     const int tile0 = SPLIT ? bound(split) : 0;
     const int n_tiles = SPLIT ? bound(split + 1) - tile0 : wu.count;
@@ -267,10 +275,78 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
             load_rows(vbytes, p.s_v.token, v_row_bytes, 64 * tile + tile_shift(tile) + wave * RW + it * RPL, ld_voff[it],
                       vbuf + (tile & 1) * TILEB + (wave * RW + it * RPL) * ROWB);
     };
+    // ---- 4-bit caches: a thread holds the codes of CT channels of one row of a 64-key tile (NW threads a row) and their scales, requested a tile ahead
+    // of their turn, decodes them at the start of a tile and stores them where the direct loads would have put them.
+    constexpr int CT = D / NW, CW = CT / 8, NSB = CT > 32 ? CT / 32 : 1;   // channels, words of codes, scales
+    struct Held {
+        uint32_t code[CW], scale[NSB];
+    };
+    [[maybe_unused]] Held held_k = {}, held_v = {};
+    [[maybe_unused]] const int f_row = tid / NW, f_part = tid % NW;
+    [[maybe_unused]] const uint8_t *k_sc = nullptr, *v_sc = nullptr;
+    if constexpr (kFp4) {
+        k_sc = p.k_scales + l * p.s_ks.layer + hkv * p.s_ks.head + (int64_t)(64 * origin) * p.s_ks.token + f_part * CT / 32;
+        v_sc = p.v_scales + l * p.s_vs.layer + hkv * p.s_vs.head + (int64_t)(64 * origin) * p.s_vs.token + f_part * CT / 32;
+    }
+    auto request = [&](bool values, int tile, Held &to) __attribute__((always_inline)) {
+        if (tile >= n_tiles) return;   // wavefront-uniform; what is held then is stored, but never read
+        const uint32_t tok = (uint32_t)(values ? p.s_v.token : p.s_k.token), s_tok = (uint32_t)(values ? p.s_vs.token : p.s_ks.token);
+        const uint32_t row = (uint32_t)min(f_row, N_() - 1 - 64 * tile);   // rows past the cache end re-read the last row; they are never unmasked
+        const unsigned char *src = (values ? vbytes : kbytes) + (int64_t)(64 * tile) * tok + (row * tok + (uint32_t)(f_part * CT / 2));
+        const uint8_t *sc = (values ? v_sc : k_sc) + (int64_t)(64 * tile) * s_tok + row * s_tok;
+#pragma unroll
+        for (int i = 0; i < NSB; ++i) to.scale[i] = sc[i];
+        if constexpr (CW == 1) {
+            to.code[0] = *reinterpret_cast<const uint32_t *>(src);
+        } else if constexpr (CW == 2) {
+            const u32x2 w = *reinterpret_cast<const u32x2 *>(src);
+            to.code[0] = w[0], to.code[1] = w[1];
+        } else {
+#pragma unroll
+            for (int i = 0; i < CW; i += 4) {
+                const u32x4 w = load16(src + 4 * i);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) to.code[i + j] = w[j];
+            }
+        }
+    };
+    auto unpack_rows = [&](lds_byte *row, int swz, const Held &from) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < CW; ++i) {
+            u32x4 raw[1];
+            fp4_decode8(from.code[i], fp4_scale(from.scale[i / 4]), raw);
+            *(__attribute__((address_space(3))) u32x4 *)(row + ((f_part * CW + i) ^ swz) * 16) = raw[0];
+        }
+    };
+    auto store_k = [&](int odd, const Held &from) __attribute__((always_inline)) {   // a tile of that parity
+        unpack_rows(kring + (2 * odd + (f_row >> 5)) * HALFB + (f_row & 31) * ROWB, k_swz(f_row & 31), from);
+    };
+    auto store_v = [&](int odd, const Held &from) __attribute__((always_inline)) {
+        unpack_rows(vbuf + odd * TILEB + f_row * ROWB, v_swz(f_row & 31), from);
+    };
+    auto next_rows = [&](int t, int odd) __attribute__((always_inline)) {   // at the start of tile t: K tile t+2, V tile t+1
+        store_k(odd, held_k);
+        store_v(1 - odd, held_v);
+        request(false, t + 3, held_k);
+        request(true, t + 2, held_v);
+    };
+
     // The first tiles are requested before anything else is set up: their latency is the block's start-up time.
+    if constexpr (kFp4) {
+        Held k0 = {}, k1 = {}, v0 = {};
+        request(false, 0, k0);
+        request(false, 1, k1);
+        request(true, 0, v0);
+        request(false, 2, held_k);
+        request(true, 1, held_v);
+        store_k(0, k0);
+        store_k(1, k1);
+        store_v(0, v0);
+    } else {
     load_k64(0);    // halves 0, 1
     load_k64(64);   // halves 2, 3
     load_v64(0);
+    }
     // This lane's two query columns, n and 16 + n of the wavefront's 32: row r = i * G + g of the (layer, kv head) group.
     int qi[2];
     bf16x8 qf[2][NF / 2];
@@ -434,9 +510,9 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
         constexpr bool DO_QK = decltype(do_qk_c)::value, DO_EXP = decltype(do_exp_c)::value, MASKED = decltype(masked_c)::value;
         constexpr int NS = 4 * NF;   // slots: the MFMAs of both products
         // The compiler copies operands right before the MFMAs of masked sub-steps, and moves scores of D = 256 between register files.
-        // (Through windows at D = 256 it also copies results right behind them: no inline assembly there.)
+        // (Through windows and in 4 bits at D = 256 it also copies results right behind them: no inline assembly there.)
         constexpr Mfma HOW_S = !MASKED && !kAccO ? Mfma::kInPlace : Mfma::kBuiltin;
-        constexpr Mfma HOW_O = kAccO && kWindow ? Mfma::kBuiltin : !MASKED ? Mfma::kInPlace : kAccO ? Mfma::kGuarded : Mfma::kBuiltin;
+        constexpr Mfma HOW_O = kAccO && kChecked ? Mfma::kBuiltin : !MASKED ? Mfma::kInPlace : kAccO ? Mfma::kGuarded : Mfma::kBuiltin;
         Scores &s_acc = sbuf[U4 & 1];
         const Scores &s_exp = sbuf[(U4 + 1) & 1];
         const lds_byte *kl = kring + ((U4 + 2) & 3) * HALFB;
@@ -490,7 +566,7 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
         }
     };
     const auto tile_barrier = [&]() __attribute__((always_inline)) {
-        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wavefront's direct loads have landed in LDS
+        if (!kFp4) __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wavefront's direct loads have landed in LDS
         __syncthreads();                     // ... and everybody else's; what was read in this tile is free
     };
     using T_ = std::true_type;
@@ -534,7 +610,9 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     auto tile_pair = [&](int t, auto plain) __attribute__((always_inline)) {
         constexpr bool PLAIN = decltype(plain)::value;
         using M_ = std::integral_constant<bool, !PLAIN>;
-        if (PLAIN) {
+        if constexpr (kFp4) {
+            next_rows(t, 0);
+        } else if (PLAIN) {
             load_kv_next(kdst_a, template_int<1>{});  // K halves 2t+4, 2t+5, V tile t+1
         } else {
             load_k64(64 * t + 128);
@@ -543,7 +621,9 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
         step(2 * t, u0, T_{}, T_{}, M_{});
         step(2 * t + 1, u1, T_{}, T_{}, M_{});
         tile_barrier();
-        if (PLAIN) {
+        if constexpr (kFp4) {
+            next_rows(t + 1, 1);
+        } else if (PLAIN) {
             load_kv_next(kdst_b, template_int<0>{});  // K halves 2t+6, 2t+7, V tile t+2
         } else {
             load_k64(64 * t + 192);
@@ -562,8 +642,12 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     mfma_settle<kAccO>(o);
     for (; t + 2 <= t_last; t += 2) tile_pair(t, F_{});
     if (t < t_last) {  // two tiles left (t is even): a whole one, then the last
+        if constexpr (kFp4) {
+            next_rows(t, 0);
+        } else {
         load_k64(64 * t + 128);
         load_v64(t + 1);
+        }
         step(2 * t, u0, T_{}, T_{}, T_{});
         step(2 * t + 1, u1, T_{}, T_{}, T_{});
         tile_barrier();
@@ -576,7 +660,7 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     }
 
     if (kAccO) mfma_settle<kAccO>(o);
-    if constexpr (kWindow) {
+    if constexpr (kChecked) {
         bool odd = false;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -586,7 +670,7 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
             odd |= state_is_odd(zero, m[h], query_sum(lsum[h]));
         }
         if (__syncthreads_or(odd)) {
-            exact_tile<D, NW, SPLIT>();
+            exact_tile<D, NW, SPLIT, KEYS>();
             return;
         }
     }
@@ -684,6 +768,9 @@ template <int D, int NW, int WPE>
 int launch_mfma(const AttnParams &p, unsigned n_blocks, bool persist, hipStream_t s)
 {
     const dim3 grid(n_blocks), block(64 * NW);
+    if (p.k_scales)
+        return p.n_splits > 1 ? launch(attn_mfma_kernel<D, NW, WPE + form(Keys::kFp4), false, true>, grid, block, 0, s, p)
+                              : launch(attn_mfma_kernel<D, NW, WPE + form(Keys::kFp4), false, false>, grid, block, 0, s, p);
     if (p.window)
         return p.n_splits > 1 ? launch(attn_mfma_kernel<D, NW, WPE + form(Keys::kWindow), false, true>, grid, block, 0, s, p)
                               : launch(attn_mfma_kernel<D, NW, WPE + form(Keys::kWindow), false, false>, grid, block, 0, s, p);
@@ -735,7 +822,7 @@ int launch_attn(const kvcomm_model &m, AttnParams &p, AttnPlan plan, const AttnP
     const unsigned n_blocks = persist ? (unsigned)max_blocks : (unsigned)p.n_items;
     int st;
     if (plan.rows_kernel) {
-        st = launch_attn_rows(p, D, plan.tile_rows, n_blocks, s);
+        st = p.k_scales ? launch_attn_kv4_rows(p, D, n_blocks, s) : launch_attn_rows(p, D, plan.tile_rows, n_blocks, s);
     } else {
         switch (D) {
             case 64: st = launch_mfma<64, kAttnWaves, 2>(p, n_blocks, persist, s); break;
