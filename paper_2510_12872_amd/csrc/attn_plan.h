@@ -126,11 +126,34 @@ static inline AttnPlan attn_plan(const kvcomm_model &m, int n_ctx, int tq, bool 
     return attn_plan_keys(m, (int64_t)n_ctx + tq, tq, may_split);
 }
 
-// The same for a window: what a tile of queries walks is their windows and the sinks (a 256-row tile of G = 4 heads has 64 queries).
+// Microseconds of a launch of the tiles kernel in blocks of 128 rows (four wavefronts), two of which share a compute unit, over `tiles` 64-key tiles.  Walks
+// through windows are short, and a block's start and end (9 us with 256 rows, alone on its unit) weigh: with two, one's fall under the other's products; half the
+// queries also see fewer tiles together.  512 queries of 8 kv heads, G = 4, 4 sinks, us in 256 rows / 128:
+//   32 layers, window 64 / 256 / 1024 / 4096   D 64  91 / 66, 121 / 92, 210 / 178, 608 / 556     D 128  141 / 119, 176 / 165, 336 / 323, 956 / 971
+//   2 layers, window 256 / 1024 / 4096         D 64  17.2 / 14.0, 28.1 / 21.4, 70.9 / 49.8      D 128  21.1 / 17.2, 37.0 / 28.8, 94.7 / 72.8
+//   32 layers, D 128, G = 8, window 256 / 1024 333 / 305, 645 / 637; G = 1 65 / 55, 106 / 93
+static inline double attn_tiles128_us(const kvcomm_model &m, int64_t items, int64_t tiles, int ns)
+{
+    const double x = (double)items * ns / kChipCUs, t = (double)((tiles + ns - 1) / ns), rounds = attn_rounds(0.5 * x);
+    const double one = m.head_dim == 64 ? 10.0 + 0.6 * t : 11.0 + 0.9 * t;   // a block per unit
+    const double two = m.head_dim == 64 ? 5.0 + rounds * (5.0 + 0.98 * t) : rounds * (9.5 + 1.73 * t);
+    return (x <= 1 ? one : std::max(one, two)) + (ns > 1 ? 3.5 + (double)items * 128 * m.head_dim * 8 * ns / 8e6 : 0.0);
+}
+
+// The same for a window.  What a tile of rows walks is the windows of its queries and the sinks.
 static inline AttnPlan attn_plan_window(const kvcomm_model &m, int n_ctx, int tq, int window, int n_sinks, bool may_split)
 {
-    const int64_t N = (int64_t)n_ctx + tq;
-    return attn_plan_keys(m, std::min<int64_t>(N, (int64_t)window + n_sinks + std::min(tq, 64)), tq, may_split);
+    const int64_t N = (int64_t)n_ctx + tq, G = m.n_q_heads / m.n_kv_heads, rows = G * tq, LH = (int64_t)m.n_layers * m.n_kv_heads;
+    auto keys = [&](int64_t tile_rows) { return std::min(N, window + std::min<int64_t>(tq, (tile_rows + G - 1) / G) + n_sinks); };
+    AttnPlan pl = attn_plan_keys(m, keys(256), tq, may_split);
+    if (pl.rows_kernel || m.head_dim == 256) return pl;
+    double best = attn_tiles_us(m, LH * pl.n_row_tiles, pl.tile_rows, (keys(256) + 63) / 64, pl.n_splits);
+    const int64_t items = LH * ((rows + 127) / 128), tiles = (keys(128) + 63) / 64;
+    for (int ns = 1; ns == 1 || (may_split && keys(256) >= kMinSplitKeys && ns <= kTileMaxSplits && ns * kMinRunTiles <= tiles && items * ns <= 2 * kChipCUs); ++ns) {
+        const double t = attn_tiles128_us(m, items, tiles, ns);
+        if (t < best) best = t, pl = {false, 128, (int)((rows + 127) / 128), ns, 32};
+    }
+    return pl;
 }
 
 // (row group, split) pairs of a launch.

@@ -765,15 +765,20 @@ extern "C" size_t kvcomm_suffix_attn_workspace(const kvcomm_model *model, int32_
 namespace {
 
 template <int D, int NW, int WPE>
+int launch_window(const AttnParams &p, unsigned n_blocks, hipStream_t s)
+{
+    return launch(p.n_splits > 1 ? attn_mfma_kernel<D, NW, WPE + form(Keys::kWindow), false, true> : attn_mfma_kernel<D, NW, WPE + form(Keys::kWindow), false, false>,
+                  dim3(n_blocks), dim3(64 * NW), 0, s, p);
+}
+
+template <int D, int NW, int WPE>
 int launch_mfma(const AttnParams &p, unsigned n_blocks, bool persist, hipStream_t s)
 {
     const dim3 grid(n_blocks), block(64 * NW);
     if (p.k_scales)
         return p.n_splits > 1 ? launch(attn_mfma_kernel<D, NW, WPE + form(Keys::kFp4), false, true>, grid, block, 0, s, p)
                               : launch(attn_mfma_kernel<D, NW, WPE + form(Keys::kFp4), false, false>, grid, block, 0, s, p);
-    if (p.window)
-        return p.n_splits > 1 ? launch(attn_mfma_kernel<D, NW, WPE + form(Keys::kWindow), false, true>, grid, block, 0, s, p)
-                              : launch(attn_mfma_kernel<D, NW, WPE + form(Keys::kWindow), false, false>, grid, block, 0, s, p);
+    if (p.window) return p.groups_per_tile == 4 ? launch_window<D, 4, D == 256 ? 1 : 2>(p, n_blocks, s) : launch_window<D, NW, WPE>(p, n_blocks, s);
     if (p.n_splits > 1)
         return persist ? launch(attn_mfma_kernel<D, NW, WPE, true, true>, grid, block, 0, s, p)
                        : launch(attn_mfma_kernel<D, NW, WPE, false, true>, grid, block, 0, s, p);
