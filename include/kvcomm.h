@@ -470,9 +470,10 @@ int kvcomm_dequantize_kv4(const kvcomm_model *model, kvcomm_tensor4 k, kvcomm_te
 
 /* --------------------------------------------------------------------------------------
  * kvcomm_suffix_attn over a compact cache: cache_k / cache_v hold the n_ctx + tq tokens in 4 bits, q and out are of the model's
- * type, bf16 (f32 models: KVCOMM_EUNSUPPORTED).  Decoded values are exact in bf16; from there on the arithmetic is that of
- * kvcomm_suffix_attn's bf16 path.  lse_out, softmax_scale, workspace (kvcomm_suffix_attn_kv4_workspace() bytes, 16-byte aligned,
- * or none) and errors as there.  A key that a query does not see has no influence on it, whatever it holds.        */
+ * type.  Decoded values are exact in either type; from there on the arithmetic is that of
+ * kvcomm_suffix_attn.  lse_out, softmax_scale, workspace (kvcomm_suffix_attn_kv4_workspace() bytes, 16-byte aligned,
+ * or none) and errors as there; KVCOMM_EUNSUPPORTED for bf16 models and token strides of 2^26 bytes or more (a tile's rows are addressed by
+ * 32-bit offsets).  A key that a query does not see has no influence on it, whatever it holds.        */
 size_t kvcomm_suffix_attn_kv4_workspace(const kvcomm_model *model, int32_t n_ctx, int32_t tq);
 
 int kvcomm_suffix_attn_kv4(const kvcomm_model *model, kvcomm_tensor q,

@@ -86,12 +86,15 @@ __global__ __launch_bounds__(256) void attn_f32_row_kernel(const AttnParams p)
 // K and V operand.  us before (32 rows and 32 keys on 32x32x2 MFMAs, K loads of 64 lines) and now: 2 layers x 4 heads x 64 rows, 224
 // keys, D = 64 10.3 -> 7.7; 4 x 8, G = 8, one token, 1025 keys, D = 128 54.8 -> 29.6, 256 96 -> 58; 4 x 8, G = 4, Tq 128, 1152 keys, D = 64 60.5 -> 55.5,
 // 128 118 -> 105, 256 195 -> 193; one layer, Tq 512, 3072 keys, D = 128 272 -> 243 (97 TFLOP/s; back to back, as all of these).
-// KEYS = kWindow: the sub-steps of the sinks, then those of the windows (window_units()); values at the edges are multiplied as they are, and a block whose
-// results are not all finite computes its rows again by attn_exact_rows().
+// KEYS = kWindow: the sub-steps of the sinks, then those of the windows (window_units()).  KEYS = kFp4: pieces are held as codes and a scale, and decoded where they
+// are multiplied.  With both, values at the edges are multiplied as they are, and a block whose results are not all finite computes its rows again by
+// attn_exact_rows().
 template <int D, int RH, Keys KEYS>
 __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   // item: one row tile of a (layer, kv head)
 {
-    constexpr bool kWindow = KEYS == Keys::kWindow;
+    constexpr bool kWindow = KEYS == Keys::kWindow, kFp4 = KEYS == Keys::kFp4;
+    constexpr bool kChecked = kWindow || kFp4;   // a block whose results are not all finite computes its rows again
+    using Cache = std::conditional_t<kFp4, uint8_t, float>;
     constexpr int NW = kF32Waves;
     constexpr int NJ = D / 16, NT = D / 64;                 // 16-byte pieces of a K row in a lane, loads of a V row
     constexpr int NP = D == 256 ? 2 : 1, PJ = NJ / NP;         // parts of a K row (32 registers at most), pieces of a part
@@ -114,8 +117,13 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
     const int units = wu.count;
     auto first_key = [&](int u) __attribute__((always_inline)) -> int { return 16 * (kWindow && u >= wu.sinks ? u + wu.gap : u); };
 
-    const float *kb = static_cast<const float *>(p.k) + l * p.s_k.layer + hkv * p.s_k.head;
-    const float *vb = static_cast<const float *>(p.v) + l * p.s_v.layer + hkv * p.s_v.head;
+    const Cache *kb = static_cast<const Cache *>(p.k) + l * p.s_k.layer + hkv * p.s_k.head;
+    const Cache *vb = static_cast<const Cache *>(p.v) + l * p.s_v.layer + hkv * p.s_v.head;
+    const uint8_t *ksb = nullptr, *vsb = nullptr;
+    if constexpr (kFp4) {
+        ksb = p.k_scales + l * p.s_ks.layer + hkv * p.s_ks.head;
+        vsb = p.v_scales + l * p.s_vs.layer + hkv * p.s_vs.head;
+    }
     int qi[RH];
     const float *qrow[RH];
 #pragma unroll
@@ -124,19 +132,46 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
         qi[h] = min(i_row, p.tq - 1);
         qrow[h] = static_cast<const float *>(p.q) + l * p.s_q.layer + (int64_t)head * p.s_q.head + (int64_t)qi[h] * p.s_q.token;
     }
-    f32x4 k[HOLD][PJ], v[VR][NT];
+    struct Codes {   // four channels: two bytes
+        uint32_t code, scale;
+    };
+    using Piece = std::conditional_t<kFp4, Codes, f32x4>;
+    auto value = [](const Piece &x) __attribute__((always_inline)) -> f32x4 {
+        if constexpr (kFp4) {
+            const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x.code, fp4_scale(x.scale), 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x.code, fp4_scale(x.scale), 1);
+            return f32x4{a[0], a[1], b[0], b[1]};
+        } else {
+            return x;
+        }
+    };
+    auto codes_at = [](const uint8_t *row, const uint8_t *scales, int c) __attribute__((always_inline)) -> Codes {
+        return Codes{*reinterpret_cast<const uint16_t *>(row + c / 2), scales[c / 32]};
+    };
+    Piece k[HOLD][PJ], v[VR][NT];
     // Rows past the cache end re-read the last one; they are always masked.
     auto load_k = [&](int u, int part) __attribute__((always_inline)) {
-        const float *kr = kb + (int64_t)min(first_key(u) + n, p.N - 1) * p.s_k.token + 16 * PJ * part + 4 * g;
+        if constexpr (kFp4) {
+            const int64_t key = min(first_key(u) + n, p.N - 1);
 #pragma unroll
-        for (int j = 0; j < PJ; ++j) k[part % HOLD][j] = *reinterpret_cast<const f32x4 *>(kr + 16 * j);
+            for (int j = 0; j < PJ; ++j) k[part % HOLD][j] = codes_at(kb + key * p.s_k.token, ksb + key * p.s_ks.token, 16 * (PJ * part + j) + 4 * g);
+        } else {
+            const float *kr = kb + (int64_t)min(first_key(u) + n, p.N - 1) * p.s_k.token + 16 * PJ * part + 4 * g;
+#pragma unroll
+            for (int j = 0; j < PJ; ++j) k[part % HOLD][j] = *reinterpret_cast<const f32x4 *>(kr + 16 * j);
+        }
     };
     auto load_v = [&](int u, int r0) __attribute__((always_inline)) {   // score r of this lane is key 4 * g + r
 #pragma unroll
         for (int r = 0; r < VR; ++r) {
-            const float *vr = vb + (int64_t)min(first_key(u) + 4 * g + r0 + r, p.N - 1) * p.s_v.token + 4 * n;
+            if constexpr (kFp4) {
+                const int64_t key = min(first_key(u) + 4 * g + r0 + r, p.N - 1);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) v[r][t] = *reinterpret_cast<const f32x4 *>(vr + 64 * t);
+                for (int t = 0; t < NT; ++t) v[r][t] = codes_at(vb + key * p.s_v.token, vsb + key * p.s_vs.token, 64 * t + 4 * n);
+            } else {
+                const float *vr = vb + (int64_t)min(first_key(u) + 4 * g + r0 + r, p.N - 1) * p.s_v.token + 4 * n;
+#pragma unroll
+                for (int t = 0; t < NT; ++t) v[r][t] = *reinterpret_cast<const f32x4 *>(vr + 64 * t);
+            }
         }
     };
     f32x4 qf[RH][kQInRegs ? NJ : 1];
@@ -162,11 +197,11 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
 #pragma unroll
         for (int part = 0; part < HOLD; ++part)
 #pragma unroll
-            for (int j = 0; j < PJ; ++j) k[part][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < PJ; ++j) k[part][j] = Piece{};
 #pragma unroll
         for (int r = 0; r < VR; ++r)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) v[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int t = 0; t < NT; ++t) v[r][t] = Piece{};
     }
     if constexpr (!kQInRegs) __syncthreads();
 
@@ -196,10 +231,11 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
                 f32x4 q[RH];
 #pragma unroll
                 for (int h = 0; h < RH; ++h) q[h] = kQInRegs ? qf[h][kQInRegs ? j : 0] : smem[(h * NJ + part * PJ + j) * 64 + lane];
+                const f32x4 kj = value(k[part % HOLD][j]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
 #pragma unroll
-                    for (int h = 0; h < RH; ++h) s[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[part % HOLD][j][e], q[h][e], s[h], 0, 0, 0);
+                    for (int h = 0; h < RH; ++h) s[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(kj[e], q[h][e], s[h], 0, 0, 0);
                 if (D == 256 || !kQInRegs) __builtin_amdgcn_sched_barrier(0);   // (all of Q would be read first, into registers that do not exist)
             }
             if (HOLD < NP && part + 1 < NP) load_k(u, part + 1);
@@ -252,11 +288,12 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
 #pragma unroll
             for (int r = 0; r < VR; ++r)
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                for (int t = 0; t < NT; ++t) {
+                    const f32x4 vt = value(v[r][t]);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        float x = v[r][t][c];
-                        if (EDGE && !kWindow) {
+                        float x = vt[c];
+                        if (EDGE && !kChecked) {
                             const bool fin = fabsf(x) < INFINITY;
                             odd |= !fin;
                             x = fin ? x : 0.f;
@@ -265,6 +302,7 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
                         for (int h = 0; h < RH; ++h)
                             o[h][t][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, s[h][r0 + r], o[h][t][c], 0, 0, 0);
                     }
+                }
         }
         if (more) load_v(u + NW, 0);
     };
@@ -281,7 +319,7 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
     for (; u < min(u_edge, units); u += NW) sub_step(u, std::false_type{});
     for (; u < units; u += NW) sub_step(u, std::true_type{});
 
-    if constexpr (kWindow) {
+    if constexpr (kChecked) {
         bool odd_state = false;
 #pragma unroll
         for (int h = 0; h < RH; ++h) {
@@ -292,7 +330,7 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
         }
         if (__syncthreads_or(odd_state)) {
             const KeyRanges keys = {0, 16 * wu.sinks, 16 * (wu.sinks + wu.gap), p.N};
-            attn_exact_rows<float, float, D>(p, lh, row0, 16 * RH, keys, 0, 16, wave, NW, lane);
+            attn_exact_rows<std::conditional_t<kFp4, fp4_t, float>, float, D>(p, lh, row0, 16 * RH, keys, 0, 16, wave, NW, lane);
             return;
         }
     }
@@ -339,30 +377,32 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
     }
 
     // Rare: values left out at the causal edge, for the queries that see them (thread: one query, every 4 * NW-th channel).
-    if (!kWindow && __syncthreads_or(odd)) {
+    if constexpr (!kChecked) {
+        if (__syncthreads_or(odd)) {
 #pragma unroll 1
-        for (int h = 0; h < RH; ++h) {   // (all of it formed again: nothing is kept for this across the loop)
-            const int r_row = row0 + 16 * h + n, i_row = div_by(r_row, p.by_G);
-            if (i_row >= p.tq) continue;
-            const int head = hkv * p.G + r_row - i_row * p.G;
-            const float *qr = static_cast<const float *>(p.q) + l * p.s_q.layer + (int64_t)head * p.s_q.head + (int64_t)i_row * p.s_q.token;
-            float *orow = static_cast<float *>(p.out) + l * p.s_o.layer + (int64_t)head * p.s_o.head + (int64_t)i_row * p.s_o.token;
-            float M = ms[16 * h + n][0], ltot = 0.f;
-            for (int w = 1; w < NW; ++w) M = fmaxf(M, ms[16 * h + n][w]);
-            for (int w = 0; w < NW; ++w) ltot += ls[16 * h + n][w];
-            for (int key = (p.n_ctx + imin + 1) & ~15; key <= p.n_ctx + i_row; ++key) {
-                const float *vr = vb + (int64_t)key * p.s_v.token;
-                float pk = -1.f;
-                for (int c = 4 * wave + g; c < D; c += 4 * NW) {
-                    const float x = vr[c];
-                    if (fabsf(x) < INFINITY) continue;
-                    if (pk < 0.f) {
-                        const float *kr = kb + (int64_t)key * p.s_k.token;
-                        float dot = 0.f;
-                        for (int i = 0; i < D; ++i) dot = fmaf(qr[i], kr[i], dot);
-                        pk = expf(dot * p.scale - M) / ltot;
+            for (int h = 0; h < RH; ++h) {   // (all of it formed again: nothing is kept for this across the loop)
+                const int r_row = row0 + 16 * h + n, i_row = div_by(r_row, p.by_G);
+                if (i_row >= p.tq) continue;
+                const int head = hkv * p.G + r_row - i_row * p.G;
+                const float *qr = static_cast<const float *>(p.q) + l * p.s_q.layer + (int64_t)head * p.s_q.head + (int64_t)i_row * p.s_q.token;
+                float *orow = static_cast<float *>(p.out) + l * p.s_o.layer + (int64_t)head * p.s_o.head + (int64_t)i_row * p.s_o.token;
+                float M = ms[16 * h + n][0], ltot = 0.f;
+                for (int w = 1; w < NW; ++w) M = fmaxf(M, ms[16 * h + n][w]);
+                for (int w = 0; w < NW; ++w) ltot += ls[16 * h + n][w];
+                for (int key = (p.n_ctx + imin + 1) & ~15; key <= p.n_ctx + i_row; ++key) {
+                    const float *vr = vb + (int64_t)key * p.s_v.token;
+                    float pk = -1.f;
+                    for (int c = 4 * wave + g; c < D; c += 4 * NW) {
+                        const float x = vr[c];
+                        if (fabsf(x) < INFINITY) continue;
+                        if (pk < 0.f) {
+                            const float *kr = kb + (int64_t)key * p.s_k.token;
+                            float dot = 0.f;
+                            for (int i = 0; i < D; ++i) dot = fmaf(qr[i], kr[i], dot);
+                            pk = expf(dot * p.scale - M) / ltot;
+                        }
+                        orow[c] += pk * x;
                     }
-                    orow[c] += pk * x;
                 }
             }
         }
@@ -388,9 +428,9 @@ __global__ __launch_bounds__(64 * kF32Waves, D == 64 ? 4 : 2) void attn_f32_kern
 template <int D>
 int launch_f32(const AttnParams &p, bool persist, unsigned n_blocks, hipStream_t stream)
 {
-    constexpr Keys A = Keys::kAll, W = Keys::kWindow;
-    const auto one = p.window ? attn_f32_kernel<D, 1, false, W> : persist ? attn_f32_kernel<D, 1, true, A> : attn_f32_kernel<D, 1, false, A>;
-    const auto two = p.window ? attn_f32_kernel<D, 2, false, W> : persist ? attn_f32_kernel<D, 2, true, A> : attn_f32_kernel<D, 2, false, A>;
+    constexpr Keys A = Keys::kAll, W = Keys::kWindow, Q = Keys::kFp4;
+    const auto one = p.k_scales ? attn_f32_kernel<D, 1, false, Q> : p.window ? attn_f32_kernel<D, 1, false, W> : persist ? attn_f32_kernel<D, 1, true, A> : attn_f32_kernel<D, 1, false, A>;
+    const auto two = p.k_scales ? attn_f32_kernel<D, 2, false, Q> : p.window ? attn_f32_kernel<D, 2, false, W> : persist ? attn_f32_kernel<D, 2, true, A> : attn_f32_kernel<D, 2, false, A>;
     return launch(p.groups_per_tile == 1 ? one : two, dim3(n_blocks), dim3(64 * kF32Waves), 0, stream, p);
 }
 
@@ -400,7 +440,8 @@ namespace kvc {
 
 int launch_attn_f32(const AttnParams &p, int D, unsigned n_blocks, hipStream_t stream)
 {
-    if (p.N <= f32_row_keys(D) && !p.window) {
+    const bool whole = !p.window && !p.k_scales;   // a whole cache of this type
+    if (p.N <= f32_row_keys(D) && whole) {
         const dim3 grid((unsigned)(((int64_t)p.L * p.Hkv * p.G * p.tq + 3) / 4)), block(256);
         switch (D) {
             case 64: return launch(attn_f32_row_kernel<64>, grid, block, 0, stream, p);
@@ -411,7 +452,7 @@ int launch_attn_f32(const AttnParams &p, int D, unsigned n_blocks, hipStream_t s
     }
     n_blocks = std::min<unsigned>(n_blocks, (1u << 23) - 1);   // a launch holds fewer than 2^32 threads
     const bool persist = n_blocks < (unsigned)p.n_items;
-    if (persist && p.window) return KVCOMM_EUNSUPPORTED;   // (millions of blocks)
+    if (persist && !whole) return KVCOMM_EUNSUPPORTED;   // (millions of blocks)
     switch (D) {
         case 64: return launch_f32<64>(p, persist, n_blocks, stream);
         case 128: return launch_f32<128>(p, persist, n_blocks, stream);

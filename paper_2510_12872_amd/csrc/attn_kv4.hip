@@ -1,5 +1,5 @@
 // kvcomm_suffix_attn_kv4: suffix attention over a cache held in 4 bits per value (fp4.h).  Many query rows: attn_mfma_kernel, which decodes
-// every tile into LDS once per block of 256 (128) rows.  Few query rows: attn_kv4_rows_kernel.
+// every tile into LDS once per block of 256 (128) rows.  Few query rows: attn_kv4_rows_kernel.  f32 models: attn_f32_kernel.
 #include "attn_exact.h"
 #include "attn_host.h"
 
@@ -338,7 +338,8 @@ extern "C" int kvcomm_suffix_attn_kv4(const kvcomm_model *model, kvcomm_tensor q
     AttnParams p{};
     int st = attn_params(model, q, n_ctx, tq, softmax_scale, out, lse_out, p);
     if (st || (st = attn_cache4(*model, cache_k, cache_v, p))) return st;
-    if (model->dtype != KVCOMM_BF16 || !fits_a_launch(p)) return KVCOMM_EUNSUPPORTED;
+    if (!fits_a_launch(p)) return KVCOMM_EUNSUPPORTED;
+    if (model->dtype == KVCOMM_F32) return launch_f32(p, model->head_dim, attn_f32_groups(*model, tq, 0), 0, static_cast<hipStream_t>(stream));
     // Rows of a 64-key tile are addressed by a 32-bit offset from the first.
     for (const Strides &t : {p.s_k, p.s_v, p.s_ks, p.s_vs})
         if (t.token >= 1 << 26) return KVCOMM_EUNSUPPORTED;

@@ -20,8 +20,9 @@ WINDOWS = [(1, 1, 1, 64, BF16, 0, 1, 1, 0), (1, 2, 4, 128, BF16, 0, 5, 2, 1), (2
            (1, 1, 2, 128, F32, 100, 50, 33, 1), (1, 2, 1, 256, F32, 40, 17, 16, 40), (1, 1, 4, 64, F32, 513, 1, 129, 2), (1, 1, 1, 64, F32, 0, 90, 40, 0),
            (1, 1, 4, 128, BF16, 0, 300, 64, 1), (1, 1, 4, 128, BF16, 63, 260, 191, 64), (1, 1, 2, 64, BF16, 4000, 130, 2500, 130), (1, 8, 4, 128, BF16, 1500, 2, 700, 4),
            (1, 1, 8, 128, BF16, 1000, 600, 400, 100), (1, 1, 4, 256, BF16, 900, 300, 500, 10)]
-# L, Hkv, G, D, n_ctx, tq
-COMPACT = [(1, 1, 1, 64, 0, 1), (1, 2, 4, 128, 0, 5), (2, 1, 2, 64, 31, 1), (1, 2, 4, 128, 700, 1), (1, 8, 4, 128, 3100, 1), (1, 1, 8, 256, 1200, 2), (1, 2, 4, 128, 90, 33),
+# L, Hkv, G, D, n_ctx, tq(, dtype)
+COMPACT = [(1, 1, 1, 64, 0, 1, F32), (2, 2, 4, 64, 77, 5, F32), (1, 1, 2, 128, 300, 40, F32), (1, 2, 1, 256, 130, 17, F32), (1, 4, 8, 64, 500, 64, F32),
+           (1, 1, 4, 256, 33, 90, F32), (1, 1, 1, 64, 0, 1), (1, 2, 4, 128, 0, 5), (2, 1, 2, 64, 31, 1), (1, 2, 4, 128, 700, 1), (1, 8, 4, 128, 3100, 1), (1, 1, 8, 256, 1200, 2), (1, 2, 4, 128, 90, 33),
            (1, 1, 2, 64, 500, 90), (1, 1, 3, 128, 640, 100), (1, 1, 1, 256, 70, 200), (1, 1, 4, 128, 0, 300), (1, 1, 4, 64, 2100, 260), (2, 2, 1, 128, 64, 64),
            (1, 1, 8, 128, 1000, 600), (1, 1, 4, 256, 900, 300), (4, 8, 1, 128, 1023, 1)]
 name = lambda c: "-".join(str(x).replace("torch.", "") for x in c)
@@ -91,14 +92,15 @@ def test_what_a_query_does_not_see_has_no_influence(case):
 @pytest.mark.gpu
 @pytest.mark.parametrize("case", COMPACT, ids=name)
 def test_compact_against_float64(case):
-    L, Hkv, G, D, n_ctx, tq = case
-    m = kv.Model(L, Hkv, Hkv * G, D, BF16, 1e4)
+    L, Hkv, G, D, n_ctx, tq = case[:6]
+    dtype = case[6] if len(case) > 6 else BF16
+    m = kv.Model(L, Hkv, Hkv * G, D, dtype, 1e4)
     g = torch.Generator().manual_seed(2)
-    q = _rand((L, Hkv * G, tq, D), BF16, g)
+    q = _rand((L, Hkv * G, tq, D), dtype, g)
     k4, v4 = _codes((L, Hkv, n_ctx + tq, D), g), _codes((L, Hkv, n_ctx + tq, D), g)
     k, v = (decode4(c.numpy(), s.numpy()) for c, s in (k4, v4))
     dev = lambda pair: tuple(t.cuda() for t in pair)
-    want, lse, tol, tol_lse = attention(f64(q), k, v, n_ctx, BF16)
+    want, lse, tol, tol_lse = attention(f64(q), k, v, n_ctx, dtype)
     for kw in (dict(), dict(workspace=_no_scratch())):
         out, got_lse = kv.kvcomm_suffix_attn_kv4(m, q.cuda(), dev(k4), dev(v4), n_ctx, want_lse=True, **kw)
         check(out, want, tol, "out")
@@ -107,7 +109,7 @@ def test_compact_against_float64(case):
         v4[1][:, :, -2, 0] = 255
         k4[1][:, :, -1, 1] = 255
         k, v = (decode4(c.numpy(), s.numpy()) for c, s in (k4, v4))
-        want, lse, tol, tol_lse = attention(f64(q), k, v, n_ctx, BF16)
+        want, lse, tol, tol_lse = attention(f64(q), k, v, n_ctx, dtype)
         for kw in (dict(), dict(workspace=_no_scratch())):
             out, got_lse = kv.kvcomm_suffix_attn_kv4(m, q.cuda(), dev(k4), dev(v4), n_ctx, want_lse=True, **kw)
             check(out, want, tol, "out with NaN")
@@ -240,8 +242,6 @@ def test_refusals_of_the_binding():
         a = {**dict(q=q, k=c(), v=c(), n_ctx=7), **bad}
         with pytest.raises(kv.KVCommError):
             kv.kvcomm_suffix_attn_kv4(m, a.pop("q"), a.pop("k"), a.pop("v"), a.pop("n_ctx"), **a)
-    with pytest.raises(kv.KVCommError):
-        kv.kvcomm_suffix_attn_kv4(kv.Model(1, 2, 4, 64, F32, 1e4), t(4, 3, F32), c(), c(), 7)
 
 
 def test_refusals_of_the_library():
@@ -262,7 +262,7 @@ def test_refusals_of_the_library():
         return lib.kvcomm_suffix_attn_kv4(m, q, k, v, n_ctx, tq, 0.0, out, None, None, 0, None)
     for bad in (dict(tq=0), dict(n_ctx=-1), dict(q=none), dict(k=c4(None)), dict(v=c4(0x100008)), dict(k=c4(st=40)), dict(v=c4(ss=2)), dict(out=none), dict(m=None)):
         assert compact(**bad) == -1, bad
-    assert compact(n_ctx=2 ** 30) == -2 and compact(m=model(D=80)) == -2 and compact(m=model(dtype=0)) == -2
+    assert compact(n_ctx=2 ** 30) == -2 and compact(m=model(D=80)) == -2 and compact(k=c4(st=1 << 26)) == -2 and compact(v=c4(ss=1 << 26)) == -2
     for need in (lib.kvcomm_suffix_attn_window_workspace(model(), 100, 0, 3, 0), lib.kvcomm_suffix_attn_window_workspace(model(), 100, 1, 0, 0),
                  lib.kvcomm_suffix_attn_kv4_workspace(model(), -1, 1), lib.kvcomm_suffix_attn_kv4_workspace(None, 5, 1)):
         assert need == 0
