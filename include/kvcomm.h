@@ -433,8 +433,8 @@ int kvcomm_align_kv_q8_batch(const kvcomm_model *model, int32_t gran, kvcomm_ten
  *   q_weight, k_weight   DEVICE [L, D] of the model's type, or NULL (ones); layer l's begins at element l * stride
  *                        (0: one for all layers; pointer and stride aligned like a tensor's).  Only with a norm and its pair.
  * An output may be exactly its own input (same pointer and strides); any other sharing of bytes between an output and
- * another tensor of the call returns KVCOMM_EINVAL (whole (layer, head) blocks are compared, first to last token: queries that lie
- * token by token beside the keys cannot be rotated in place).
+ * another tensor of the call returns KVCOMM_EINVAL (tensors that lie token by token beside each other, as in a projection, are told
+ * apart; of others whole (layer, head) blocks are compared, first to last token).
  * Errors: KVCOMM_EINVAL / KVCOMM_EUNSUPPORTED as above; KVCOMM_EINVAL for n_tokens <= 0, positions beyond INT32_MAX,
  * norm_eps negative, infinite or NaN, a weight without a norm or without its tensor.       */
 int kvcomm_place_qkv(const kvcomm_model *model, kvcomm_tensor q, kvcomm_tensor k, kvcomm_tensor v,

@@ -177,6 +177,18 @@ int launch_place(PlaceParams &p, int L, hipStream_t s)
     return launch(p.heads_per_group == at_once ? one : two, dim3((unsigned)blocks), dim3(kBlock), 0, s, p);
 }
 
+// Tensors that lie token by token beside each other, as the parts of a projection do: the same distance st from token to token, layers whole numbers of tokens apart,
+// and all heads of each within its own piece of every st bytes.
+bool beside_each_other(const kvcomm_tensor &a, int Ha, const kvcomm_tensor &b, int Hb, int L, int D, int es)
+{
+    const int64_t st = a.stride_token;
+    if (st <= 0 || b.stride_token != st || (L > 1 && (a.stride_layer % st || b.stride_layer % st))) return false;
+    const int64_t piece_a = (Ha - 1) * a.stride_head + D, piece_b = (Hb - 1) * b.stride_head + D;
+    int64_t gap = (int64_t)(reinterpret_cast<uintptr_t>(b.ptr) - reinterpret_cast<uintptr_t>(a.ptr)) % (st * es);   // of b's piece behind a's begin
+    if (gap < 0) gap += st * es;
+    return gap >= piece_a * es && gap + piece_b * es <= st * es;
+}
+
 }  // namespace
 
 extern "C" int kvcomm_place_qkv(const kvcomm_model *model, kvcomm_tensor q, kvcomm_tensor k, kvcomm_tensor v, int32_t n_tokens, int32_t first_pos,
@@ -194,7 +206,7 @@ extern "C" int kvcomm_place_qkv(const kvcomm_model *model, kvcomm_tensor q, kvco
     const int64_t w_stride[2] = {q_weight_stride, k_weight_stride};
     PlaceParams p{};
     Extent from[5], to[3];
-    int n_from = 0, n_to = 0;
+    int n_from = 0, n_to = 0, is[3];
     for (int i = 0; i < 3; ++i) {
         if (!in[i].ptr && !out[i].ptr) continue;
         if ((st = check_tensor(in[i], dt, true)) || (st = check_tensor(out[i], dt, true))) return st;
@@ -204,6 +216,7 @@ extern "C" int kvcomm_place_qkv(const kvcomm_model *model, kvcomm_tensor q, kvco
         p.s_out[i] = strides_of(out[i]);
         p.heads[i] = heads[i];
         from[n_from++] = extent_of(in[i], L, heads[i], n_tokens, D, es);
+        is[n_to] = i;
         to[n_to++] = extent_of(out[i], L, heads[i], n_tokens, D, es);
     }
     if (n_to == 0) return KVCOMM_EINVAL;
@@ -217,11 +230,14 @@ extern "C" int kvcomm_place_qkv(const kvcomm_model *model, kvcomm_tensor q, kvco
         p.s_weight[i] = w_stride[i];
         from[n_from++] = extent_of(w, L, 1, 1, D, es);
     }
+    auto apart = [&](int i, int j, const kvcomm_tensor &y) { return beside_each_other(out[is[i]], heads[is[i]], y, heads[is[j]], L, D, es); };
     for (int i = 0; i < n_to; ++i) {
-        for (int j = 0; j < n_from; ++j)
-            if (!(i == j && j < n_pairs && same_extent(to[i], from[j])) && extents_overlap(to[i], from[j])) return KVCOMM_EINVAL;
+        for (int j = 0; j < n_from; ++j) {
+            const bool pair = j < n_pairs;
+            if (!(i == j && pair && same_extent(to[i], from[j])) && extents_overlap(to[i], from[j]) && !(pair && apart(i, j, in[is[j]]))) return KVCOMM_EINVAL;
+        }
         for (int j = 0; j < i; ++j)
-            if (extents_overlap(to[i], to[j])) return KVCOMM_EINVAL;
+            if (extents_overlap(to[i], to[j]) && !apart(i, j, out[is[j]])) return KVCOMM_EINVAL;
     }
     p.n = n_tokens;
     p.first_pos = first_pos;

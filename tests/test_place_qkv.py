@@ -75,8 +75,11 @@ def test_forms_of_a_call_give_the_same_bits():
     ones = torch.ones((D,), dtype=dtype, device="cuda")
     assert all(torch.equal(a, b) for a, b in zip(kv.kvcomm_place_qkv(m, q, k, v, 40, norm_eps=1e-6),
                                                  kv.kvcomm_place_qkv(m, q, k, v, 40, norm_eps=1e-6, q_weight=ones, k_weight=ones)))
-    kv.kvcomm_place_qkv(m, q, k, v, 40, q_out=q, k_out=k, v_out=v, **norm)   # in place
-    assert all(torch.equal(a, b) for a, b in zip((q, k, v), want))
+    packed = _inputs(L, Hkv, G, D, dtype, n, "packed")[:3]
+    assert all(torch.equal(a, b) for a, b in zip(packed, (q, k, v)))
+    for x in ((q, k, v), packed):   # in place, each by itself and side by side in one projection
+        kv.kvcomm_place_qkv(m, *x, 40, q_out=x[0], k_out=x[1], v_out=x[2], **norm)
+        assert all(torch.equal(a, b) for a, b in zip(x, want))
 
 
 @pytest.mark.gpu
@@ -127,5 +130,11 @@ def test_refusals_of_the_library():
              dict(qo=T(0x8000000)), dict(ko=T(0xa000000)), dict(qo=T(0x10000 + 256)), dict(ko=T(0x9000000)), dict(wk=0xb000000, eps=1e-6), dict(D=0)]
     for change in inval:
         assert call(**change) == -1, change
+    # parts of a projection [token, 4 + 2 + 2 heads, 128]: a head further on they meet
+    row, at = 8 * 128, lambda head: 0x10000 + 2 * 128 * head
+    part = lambda head: T(at(head), 4 * row, 128, row)
+    assert call(q=part(0), k=part(4), v=part(6), qo=part(0), ko=part(5), vo=T(0xc000000)) == -1
+    assert call(q=part(0), k=part(4), v=part(6), qo=part(0), ko=part(4), vo=part(7)) == -1   # (reaches into the next token's queries)
+    assert call(q=part(0), k=part(4), v=T(0x9000000), qo=T(at(0), 4 * row + 8, 128, row)) == -1
     assert call(D=96) == -2
     assert lib.kvcomm_place_qkv(None, T(), T(), T(), 1, 0, None, None, 0, 0, 0.0, T(), T(), T(), None) == -1
