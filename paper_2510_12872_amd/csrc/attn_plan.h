@@ -147,7 +147,7 @@ static inline AttnPlan attn_plan_window(const kvcomm_model &m, int n_ctx, int tq
     auto keys = [&](int64_t tile_rows) { return std::min(N, window + std::min<int64_t>(tq, (tile_rows + G - 1) / G) + n_sinks); };
     AttnPlan pl = attn_plan_keys(m, keys(256), tq, may_split);
     if (pl.rows_kernel || m.head_dim == 256) return pl;
-    double best = attn_tiles_us(m, LH * pl.n_row_tiles, pl.tile_rows, (keys(256) + 63) / 64, pl.n_splits);
+    double best = m.head_dim == 64 ? INFINITY : attn_tiles_us(m, LH * pl.n_row_tiles, pl.tile_rows, (keys(256) + 63) / 64, pl.n_splits);   // (D = 64: always 128 rows)
     const int64_t items = LH * ((rows + 127) / 128), tiles = (keys(128) + 63) / 64;
     for (int ns = 1; ns == 1 || (may_split && keys(256) >= kMinSplitKeys && ns <= kTileMaxSplits && ns * kMinRunTiles <= tiles && items * ns <= 2 * kChipCUs); ++ns) {
         const double t = attn_tiles128_us(m, items, tiles, ns);

@@ -778,7 +778,11 @@ int launch_mfma(const AttnParams &p, unsigned n_blocks, bool persist, hipStream_
     if (p.k_scales)
         return p.n_splits > 1 ? launch(attn_mfma_kernel<D, NW, WPE + form(Keys::kFp4), false, true>, grid, block, 0, s, p)
                               : launch(attn_mfma_kernel<D, NW, WPE + form(Keys::kFp4), false, false>, grid, block, 0, s, p);
-    if (p.window) return p.groups_per_tile == 4 ? launch_window<D, 4, D == 256 ? 1 : 2>(p, n_blocks, s) : launch_window<D, NW, WPE>(p, n_blocks, s);
+    if (p.window) {   // blocks of 128 or, at D = 128, of 256 rows
+        if constexpr (D == 128)
+            if (p.groups_per_tile == NW) return launch_window<D, NW, WPE>(p, n_blocks, s);
+        return launch_window<D, 4, WPE>(p, n_blocks, s);
+    }
     if (p.n_splits > 1)
         return persist ? launch(attn_mfma_kernel<D, NW, WPE, true, true>, grid, block, 0, s, p)
                        : launch(attn_mfma_kernel<D, NW, WPE, false, true>, grid, block, 0, s, p);

@@ -19,7 +19,7 @@ WINDOWS = [(1, 1, 1, 64, BF16, 0, 1, 1, 0), (1, 2, 4, 128, BF16, 0, 5, 2, 1), (2
            (1, 1, 3, 128, BF16, 640, 100, 300, 4), (1, 1, 4, 64, BF16, 1100, 80, 1, 0), (1, 1, 4, 128, BF16, 1100, 70, 5000, 2), (2, 1, 1, 256, BF16, 70, 200, 50, 64),
            (1, 1, 2, 128, F32, 100, 50, 33, 1), (1, 2, 1, 256, F32, 40, 17, 16, 40), (1, 1, 4, 64, F32, 513, 1, 129, 2), (1, 1, 1, 64, F32, 0, 90, 40, 0),
            (1, 1, 4, 128, BF16, 0, 300, 64, 1), (1, 1, 4, 128, BF16, 63, 260, 191, 64), (1, 1, 2, 64, BF16, 4000, 130, 2500, 130), (1, 8, 4, 128, BF16, 1500, 2, 700, 4),
-           (1, 1, 8, 128, BF16, 1000, 600, 400, 100), (1, 1, 4, 256, BF16, 900, 300, 500, 10)]
+           (1, 1, 8, 128, BF16, 1000, 600, 400, 100), (1, 1, 4, 256, BF16, 900, 300, 500, 10), (1, 1, 1, 256, BF16, 900, 60, 700, 70)]
 # L, Hkv, G, D, n_ctx, tq(, dtype)
 COMPACT = [(1, 1, 1, 64, 0, 1, F32), (2, 2, 4, 64, 77, 5, F32), (1, 1, 2, 128, 300, 40, F32), (1, 2, 1, 256, 130, 17, F32), (1, 4, 8, 64, 500, 64, F32),
            (1, 1, 4, 256, 33, 90, F32), (1, 1, 1, 64, 0, 1), (1, 2, 4, 128, 0, 5), (2, 1, 2, 64, 31, 1), (1, 2, 4, 128, 700, 1), (1, 8, 4, 128, 3100, 1), (1, 1, 8, 256, 1200, 2), (1, 2, 4, 128, 90, 33),

@@ -1,0 +1,140 @@
+"""Larger launches of kvcomm_suffix_attn_window and kvcomm_suffix_attn_kv4, those that go to the tiles kernel (tests/test_window_kv4_launches.py holds that
+they do), against masked attention in float64 on the GPU; with hidden infinities and NaN too."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2510_12872_amd as kv
+
+from plain64 import HALF_STEP, decode4
+
+BF16 = torch.bfloat16
+NAN, INF = float("nan"), float("inf")
+
+# L, Hkv, G, D, n_ctx, tq, window, sinks
+WINDOW_TILES = [(1, 8, 8, 64, 0, 130, 100, 3), (1, 8, 8, 64, 900, 130, 1024, 70), (4, 8, 2, 128, 70, 130, 100, 3), (1, 8, 8, 128, 900, 130, 1024, 70),
+                (1, 8, 8, 128, 70, 130, 100, 3), (1, 4, 4, 128, 2000, 700, 2048, 4), (1, 8, 8, 256, 70, 130, 100, 3), (1, 1, 4, 256, 1500, 700, 2500, 4),
+                (2, 8, 4, 128, 0, 1000, 300, 200), (1, 8, 1, 128, 33, 2100, 64, 1), (1, 4, 8, 128, 777, 555, 1, 0), (1, 8, 4, 128, 2000, 515, 129, 900),
+                (2, 8, 4, 64, 700, 333, 511, 64), (1, 8, 4, 256, 640, 321, 257, 65), (4, 8, 4, 128, 5000, 260, 2048, 0), (1, 8, 4, 128, 8000, 512, 4096, 4),
+                (1, 4, 8, 256, 1500, 130, 2500, 4), (32, 8, 4, 128, 2600, 1, 2200, 4)]
+# L, Hkv, G, D, n_ctx, tq
+COMPACT_TILES = [(4, 8, 8, 64, 0, 130), (1, 4, 4, 64, 900, 700), (1, 8, 8, 128, 0, 260), (1, 4, 8, 128, 900, 400), (1, 4, 1, 128, 70, 2000), (2, 8, 8, 256, 70, 130),
+                 (1, 2, 8, 256, 3000, 130), (4, 8, 4, 128, 1000, 321), (1, 8, 4, 128, 4000, 256), (2, 8, 4, 64, 2049, 513), (32, 8, 4, 128, 8300, 1)]
+name = lambda c: "-".join(map(str, c))
+
+
+def attention64(q, k, v, n_ctx, window=None, sinks=0):
+    """(out, lse, bounds of their errors) in float64 on the device, a (layer, kv head) at a time; bounds as in plain64.attention."""
+    L, Hq, tq, D = q.shape
+    Hkv, N = k.shape[1], k.shape[2]
+    G, scale, u = Hq // Hkv, D ** -0.5, HALF_STEP[BF16]
+    out, lse = torch.empty(q.shape, dtype=torch.float64, device=q.device), torch.empty(q.shape[:3], dtype=torch.float64, device=q.device)
+    tol, tol_lse = torch.empty_like(out), torch.empty_like(lse)
+    j, p = torch.arange(N, device=q.device), n_ctx + torch.arange(tq, device=q.device)[:, None]
+    seen = j <= p
+    if window is not None:
+        seen = seen & ((j > p - window) | (j < sinks))
+    for l in range(L):
+        for h in range(Hkv):
+            kk, vv = k[l, h].double(), v[l, h].double()
+            at = (l, slice(h * G, h * G + G))
+            x = q[at].double()
+            s = torch.matmul(x, kk.T.contiguous()) * scale
+            bad = (torch.isnan(s) & seen).any(-1)                       # a score that is not a number: nor is the row
+            s = torch.where(seen, torch.nan_to_num(s, nan=0.0), -INF)
+            lse[at] = torch.where(bad, NAN, torch.logsumexp(s, -1))
+            w = torch.softmax(s, -1)
+            finite = torch.isfinite(vv)
+            v0 = torch.where(finite, vv, 0.0)
+            o = torch.matmul(w, v0)
+            see = lambda what: torch.matmul(seen.double(), what.double()) > 0
+            nan, up, down = see(torch.isnan(vv)), see(vv == INF), see(vv == -INF)
+            o = torch.where(nan | (up & down), NAN, torch.where(up, INF, torch.where(down, -INF, o)))
+            out[at] = torch.where(bad[..., None], NAN, o)
+            ds = (D + 4) * 2.0 ** -24 * torch.where(seen, torch.matmul(x.abs(), torch.nan_to_num(kk, nan=0.0).abs().T.contiguous()), 0.0).amax(-1) * scale
+            n = seen.sum(-1)
+            rel = 2 * ds + (n + 32) * 2.0 ** -24 + u
+            tol[at] = 1.01 * (rel[..., None] * torch.matmul(w, v0.abs()) + u * torch.nan_to_num(o, nan=0.0, posinf=0.0, neginf=0.0).abs()) + 2.0 ** -120
+            tol_lse[at] = ds + (n + 32) * 2.0 ** -24 * torch.clamp(torch.nan_to_num(lse[at], nan=0.0).abs(), min=1.0)
+    return out, lse, tol, tol_lse
+
+
+def check(got, want, tol, what):
+    got = got.double()
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), f"{what}: NaN in other places"
+    fine = torch.isfinite(want)
+    assert torch.equal(got[~fine & ~torch.isnan(want)], want[~fine & ~torch.isnan(want)]), f"{what}: infinities"
+    off = torch.where(fine, (got - want).abs() - tol, -1.0)
+    assert float(off.max()) <= 0, f"{what}: {int((off > 0).sum())} of {off.numel()} values, worst by {float(off.max()):.3e}"
+
+
+def _rand(shape, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.randn(shape, generator=g, device="cuda").to(BF16)
+
+
+def _no_scratch():
+    return torch.empty((1,), dtype=torch.uint8, device="cuda")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hidden", [False, True])
+@pytest.mark.parametrize("case", WINDOW_TILES, ids=name)
+def test_windows(case, hidden):
+    L, Hkv, G, D, n_ctx, tq, window, sinks = case
+    N = n_ctx + tq
+    m = kv.Model(L, Hkv, Hkv * G, D, BF16, 1e4)
+    q, k, v = _rand((L, Hkv * G, tq, D), 1), _rand((L, Hkv, N, D), 2), _rand((L, Hkv, N, D), 3)
+    if hidden:   # NaN where no query looks; values that only the last or the first queries see
+        unseen = torch.arange(sinks, max(sinks, n_ctx + 1 - window), device="cuda")
+        k[:, :, unseen], v[:, :, unseen] = NAN, NAN
+        v[:, 0, N - 3, 3], k[-1, -1, N - 2, 5] = -INF, NAN
+        if n_ctx + 1 - window >= sinks:
+            v[:, -1, n_ctx + 1 - window, 7] = NAN
+    want = attention64(q, k, v, n_ctx, window, sinks)
+    for kw in (dict(), dict(workspace=_no_scratch())):
+        out, lse = kv.kvcomm_suffix_attn_window(m, q, k, v, n_ctx, window, sinks, want_lse=True, **kw)
+        check(out, want[0], want[2], "out")
+        check(lse, want[1], want[3], "lse")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hidden", [False, True])
+@pytest.mark.parametrize("case", COMPACT_TILES, ids=name)
+def test_compact_caches(case, hidden):
+    L, Hkv, G, D, n_ctx, tq = case
+    N = n_ctx + tq
+    m = kv.Model(L, Hkv, Hkv * G, D, BF16, 1e4)
+    q = _rand((L, Hkv * G, tq, D), 1)
+    k4, v4 = kv.kvcomm_quantize_kv4(m, _rand((L, Hkv, N, D), 2), _rand((L, Hkv, N, D), 3))
+    if hidden and tq > 1:
+        v4[1][:, 0, N - 2, 0] = 255
+        k4[1][-1, -1, N - 1, 1] = 255
+    k, v = (torch.from_numpy(decode4(*(t.cpu().numpy() for t in pair))).cuda() for pair in (k4, v4))
+    want = attention64(q, k, v, n_ctx)
+    for kw in (dict(), dict(workspace=_no_scratch())):
+        out, lse = kv.kvcomm_suffix_attn_kv4(m, q, k4, v4, n_ctx, want_lse=True, **kw)
+        check(out, want[0], want[2], "out")
+        check(lse, want[1], want[3], "lse")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("compact", [False, True])
+def test_scores_that_move_the_reference(compact):
+    """Scores of hundreds that grow along the keys: the tiles kernel sets its references again and again."""
+    L, Hkv, G, D, n_ctx, tq = 1, 8, 8, 128, 300, 260
+    N = n_ctx + tq
+    m = kv.Model(L, Hkv, Hkv * G, D, BF16, 1e4)
+    q, k, v = _rand((L, Hkv * G, tq, D), 1), _rand((L, Hkv, N, D), 2), _rand((L, Hkv, N, D), 3)
+    q[..., 0], k[..., 0] = 40.0, torch.linspace(-60, 60, N, device="cuda").to(BF16)
+    if compact:
+        k4, v4 = kv.kvcomm_quantize_kv4(m, k, v)
+        k, v = kv.kvcomm_dequantize_kv4(m, k4, v4)
+        out, lse = kv.kvcomm_suffix_attn_kv4(m, q, k4, v4, n_ctx, want_lse=True)
+        want = attention64(q, k, v, n_ctx)
+    else:
+        out, lse = kv.kvcomm_suffix_attn_window(m, q, k, v, n_ctx, 200, 5, want_lse=True)
+        want = attention64(q, k, v, n_ctx, 200, 5)
+    check(out, want[0], want[2], "out")
+    check(lse, want[1], want[3], "lse")
