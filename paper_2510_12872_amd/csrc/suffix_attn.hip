@@ -76,10 +76,11 @@ __device__ __forceinline__ void exact_tile()
     }
     const int lh = div_by(logical, p.by_row_tiles), rt = p.n_row_tiles - 1 - (logical - lh * p.n_row_tiles);
     const int imin = min(p.tq - 1, div_by(rt * BM, p.by_G)), imax = min(p.tq - 1, div_by(rt * BM + BM - 1, p.by_G));
-    WindowUnits wu = {0, 0, (p.n_ctx + imax) / 64 + 1};
-    if (KEYS == Keys::kWindow) wu = window_units(p, imin, imax, 64);
-    const int begin = SPLIT ? even_bound(split, p, wu.count) : 0, end = SPLIT ? even_bound(split + 1, p, wu.count) : wu.count;
-    const KeyRanges keys = {64 * begin, 64 * min(end, wu.sinks), 64 * (max(begin, wu.sinks) + wu.gap), min(64 * (end + wu.gap), p.N)};
+    WindowUnits wu = {0, 0, (p.n_ctx + imax) / 32 + 1};
+    if (KEYS == Keys::kWindow) wu = window_units(p, imin, imax, 32);
+    const int tiles = (wu.count + 1) / 2;
+    const int begin = SPLIT ? 2 * even_bound(split, p, tiles) : 0, end = 2 * (SPLIT ? even_bound(split + 1, p, tiles) : tiles);   // in halves of tiles
+    const KeyRanges keys = {32 * begin, 32 * min(end, wu.sinks), 32 * (max(begin, wu.sinks) + wu.gap), min(32 * (end + wu.gap), p.N)};
     attn_exact_rows<std::conditional_t<KEYS == Keys::kFp4, fp4_t, bf16_t>, bf16_t, D>(p, lh, rt * BM, BM, keys, split, 32, __builtin_amdgcn_readfirstlane(tid >> 6), NW, tid & 63);
 }
 
@@ -91,7 +92,7 @@ __device__ __forceinline__ void exact_tile()
 // SPLIT: an item is one run of key tiles of a row tile.  The block works on the cache as if it began at the run's
 // first key (which all its queries see) and leaves unnormalised outputs, references and row sums in the workspace;
 // attn_combine_kernel joins them.
-// KEYS = kWindow: the block walks the tiles of the sinks, then those of its queries' windows (window_units()), as if they lay behind each other.  The
+// KEYS = kWindow: the block walks the 32-key halves of the sinks, then those of its queries' windows (window_units()), as if they lay behind each other.  The
 // first pairs of tiles, where some query does not see some key, are masked like the last; a block whose results are not all finite computes its
 // rows again by attn_exact_rows(), because a hidden key's value may have been multiplied by its probability 0.
 // FORM: wavefronts per SIMD + form(KEYS) (one argument for both: a whole cache's kernels keep the names that the profiles have).
@@ -182,15 +183,16 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     const int wg_imin = min(p.tq - 1, div_by(rt * BM, p.by_G));
     const int all_tiles = (p.n_ctx + wg_imax + 1 + 63) / 64;
     const int first_hidden = (p.n_ctx + wg_imin) / 64 + 1;
-    WindowUnits wu = {0, 0, all_tiles};
-    if constexpr (kWindow) wu = window_units(p, wg_imin, wg_imax, 64);
+    WindowUnits wu = {0, 0, 2 * all_tiles};   // in halves of tiles
+    if constexpr (kWindow) wu = window_units(p, wg_imin, wg_imax, 32);
+    const int walk_tiles = kWindow ? (wu.count + 1) / 2 : all_tiles;   // (a half too many lies behind the last query)
     // (a run cut evenly may begin with keys that some query does not see: the reference of such a row is set later)
     auto bound = [&](int s) __attribute__((always_inline)) -> int {
-        return kChecked ? even_bound(s, p, wu.count) : split_bound(s, p.n_splits, all_tiles, first_hidden);
+        return kChecked ? even_bound(s, p, walk_tiles) : split_bound(s, p.n_splits, all_tiles, first_hidden);
     };
     const int tile0 = SPLIT ? bound(split) : 0;
-    const int n_tiles = SPLIT ? bound(split + 1) - tile0 : wu.count;
-    const int sink_tiles = kWindow ? max(0, wu.sinks - tile0) : 0;   // of this run
+    const int n_tiles = SPLIT ? bound(split + 1) - tile0 : walk_tiles;
+    const int sink_halves = kWindow ? max(0, wu.sinks - 2 * tile0) : 0;   // of this run
     if constexpr (SPLIT) {
         if (n_tiles <= 0) {   // the whole block: this run is empty
             if (lane < 32 && div_by(rt * BM + wave * 32 + lane, p.by_G) < p.tq) {
@@ -203,17 +205,17 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
             continue;
         }
     }
-    // Tile t of the run begins at key 64 * (t + origin); a tile of the sinks lies 64 * gap keys before that.
-    const int origin = tile0 + wu.gap;
+    // Half h of the run begins at key origin + 32 * h; a half of the sinks lies 32 * gap keys before that.
+    const int origin = 64 * tile0 + 32 * wu.gap;
     if constexpr (SPLIT || kWindow) {
-        kb_ += (int64_t)(64 * origin) * p.s_k.token;
-        vb_ += (int64_t)(64 * origin) * p.s_v.token;
+        kb_ += (int64_t)origin * p.s_k.token;
+        vb_ += (int64_t)origin * p.s_v.token;
     }
-    auto tile_shift = [&](int t) __attribute__((always_inline)) -> int { return kWindow && t < sink_tiles ? -64 * wu.gap : 0; };
-    // Context length and cache length counted from key 64 * origin (n_ctx_() may be negative; without a window every query of
+    auto half_shift = [&](int h) __attribute__((always_inline)) -> int { return kWindow && h < sink_halves ? -32 * wu.gap : 0; };
+    // Context length and cache length counted from key `origin` (n_ctx_() may be negative; without a window every query of
     // the tile still sees key 0 of the run).
-    auto n_ctx_ = [&]() __attribute__((always_inline)) -> int { return SPLIT || kWindow ? p.n_ctx - 64 * origin : p.n_ctx; };
-    auto N_ = [&]() __attribute__((always_inline)) -> int { return SPLIT || kWindow ? p.N - 64 * origin : p.N; };
+    auto n_ctx_ = [&]() __attribute__((always_inline)) -> int { return SPLIT || kWindow ? p.n_ctx - origin : p.n_ctx; };
+    auto N_ = [&]() __attribute__((always_inline)) -> int { return SPLIT || kWindow ? p.N - origin : p.N; };
     const int n_sub = 2 * n_tiles;
     const int sub_unmasked = (n_ctx_() + wg_imin + 1) / 32;  // sub-steps [0, sub_unmasked) are visible to all queries
 
@@ -265,14 +267,14 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
         const int rbase = (wave % (NW / 2)) * RW;
 #pragma unroll
         for (int it = 0; it < LPT; ++it)
-            load_rows(kbytes, p.s_k.token, k_row_bytes, 32 * h + tile_shift(h >> 1) + rbase + it * RPL, ld_koff[it],
+            load_rows(kbytes, p.s_k.token, k_row_bytes, 32 * h + half_shift(h) + rbase + it * RPL, ld_koff[it],
                       kring + (h & 3) * HALFB + (rbase + it * RPL) * ROWB);
     };
     auto load_v64 = [&](int tile) __attribute__((always_inline)) {
         if (tile >= n_tiles) return;
 #pragma unroll
         for (int it = 0; it < LPT; ++it)
-            load_rows(vbytes, p.s_v.token, v_row_bytes, 64 * tile + tile_shift(tile) + wave * RW + it * RPL, ld_voff[it],
+            load_rows(vbytes, p.s_v.token, v_row_bytes, 64 * tile + half_shift(2 * tile + wave / (NW / 2)) + wave * RW + it * RPL, ld_voff[it],
                       vbuf + (tile & 1) * TILEB + (wave * RW + it * RPL) * ROWB);
     };
     // ---- 4-bit caches: a thread holds the codes of CT channels of one row of a 64-key tile (NW threads a row) and their scales, requested a tile ahead
@@ -285,8 +287,8 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     [[maybe_unused]] const int f_row = tid / NW, f_part = tid % NW;
     [[maybe_unused]] const uint8_t *k_sc = nullptr, *v_sc = nullptr;
     if constexpr (kFp4) {
-        k_sc = p.k_scales + l * p.s_ks.layer + hkv * p.s_ks.head + (int64_t)(64 * origin) * p.s_ks.token + f_part * CT / 32;
-        v_sc = p.v_scales + l * p.s_vs.layer + hkv * p.s_vs.head + (int64_t)(64 * origin) * p.s_vs.token + f_part * CT / 32;
+        k_sc = p.k_scales + l * p.s_ks.layer + hkv * p.s_ks.head + (int64_t)origin * p.s_ks.token + f_part * CT / 32;
+        v_sc = p.v_scales + l * p.s_vs.layer + hkv * p.s_vs.head + (int64_t)origin * p.s_vs.token + f_part * CT / 32;
     }
     auto request = [&](bool values, int tile, Held &to) __attribute__((always_inline)) {
         if (tile >= n_tiles) return;   // wavefront-uniform; what is held then is stored, but never read
@@ -365,9 +367,9 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     // so that a load costs one 64-bit scalar add instead of a 64-bit multiply, and with M0 formed from
     // a per-wavefront LDS base plus a literal.  kp / vp point at this wavefront's next row to load:
     // during tile t the K halves 2t+4, 2t+5 (keys 64t+128 ...) and V tile t+1.
-    // First tile (even) of those pairs, which have no tile of the sinks and whose exponentials, of sub-steps from 2t+1 on, are of keys that no window has left.
+    // First tile (even) of those pairs, which have no half of the sinks and whose exponentials, of sub-steps from 2t+1 on, are of keys that no window has left.
     const int left = kWindow ? n_ctx_() + wg_imax - p.window : -1;   // last key that some query has left
-    const int t_plain0 = kWindow ? (max(sink_tiles, left < 0 ? 0 : (left / 32 + 1) / 2) + 1) & ~1 : 0;
+    const int t_plain0 = kWindow ? (max((sink_halves + 1) / 2, left < 0 ? 0 : (left / 32 + 1) / 2) + 1) & ~1 : 0;
     const int64_t k_rpl = (int64_t)RPL * p.s_k.token * 2, v_rpl = (int64_t)RPL * p.s_v.token * 2;
     const int64_t k_adv = (int64_t)(64 - LPT * RPL) * p.s_k.token * 2, v_adv = (int64_t)(64 - LPT * RPL) * p.s_v.token * 2;
     const unsigned char *kp = kbytes + (int64_t)(64 * t_plain0 + 128 + 32 * (wave / (NW / 2)) + (wave % (NW / 2)) * RW) * p.s_k.token * 2;
@@ -446,8 +448,8 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
         int last, sinks;
     };
     auto limit_of = [&](int u) __attribute__((always_inline)) -> Limit {   // of sub-step u
-        const int first = 32 * u + tile_shift(u >> 1);
-        return Limit{n_ctx_() - first, kWindow ? p.n_sinks - first - 64 * origin : 0};
+        const int first = 32 * u + half_shift(u);
+        return Limit{n_ctx_() - first, kWindow ? p.n_sinks - first - origin : 0};
     };
     auto score = [&](const Scores &s, int j, Limit limit, bool masked) __attribute__((always_inline)) -> float {
         const int h = j >> 3, kh = (j >> 2) & 1, r = j & 3;
