@@ -255,14 +255,14 @@ __global__ __launch_bounds__(512, D == 256 ? 2 : 4) void attn_kv4_rows_kernel(co
 }
 
 // Microseconds of a launch of the rows kernel with the keys of `items` (16-row tile, layer, kv head) triples cut into ns runs, `its` iterations (32 keys of every
-// wavefront) of a whole cache: 4 us, and per iteration 1.2 us when few units are busy, 1.5 with a block on each, 2.5 with two and 2.5 us more for their start (D = 256: one block
+// wavefront) of a whole cache: 4 us, and per iteration 1.2 us when few units are busy, 1.5 with a block on each, 2.5 with two and 2.5 us more for their start, 1.5 us for the start of every two that follow (D = 256: one block
 // per unit, in rounds); 3.5 us for the combine launch and the partial results at about 8 TB/s.
 double kv4_rows_us(const kvcomm_model &m, int64_t items, int64_t its, int64_t ns)
 {
     const double x = (double)(items * ns) / kChipCUs, run = (double)((its + ns - 1) / ns);
     const double one = 1.2 + 0.3 * std::min(1.0, x), two = x <= 1 ? one : x <= 2 ? 0.5 + x : 1.25 * x;
     const double us = m.head_dim == 256 ? attn_rounds(x) * (4.0 + 1.9 * one * run)
-                                        : 4.0 + 2.5 * std::min(1.0, std::max(0.0, x - 1)) + (m.head_dim == 64 ? 0.65 : 1.0) * two * run;
+                                        : 4.0 + 2.5 * std::min(1.0, std::max(0.0, x - 1)) + 0.75 * std::max(0.0, x - 2) + (m.head_dim == 64 ? 0.65 : 1.0) * two * run;
     return us + (ns > 1 ? 3.5 + (double)(items * ns) * 16 * m.head_dim * 8 / 8e6 : 0.0);
 }
 
@@ -272,6 +272,16 @@ double kv4_tiles_us(const kvcomm_model &m, int64_t items, int tile_rows, int64_t
     const double x = (double)(items * ns) / kChipCUs, scale = m.head_dim == 64 ? 0.68 : m.head_dim == 128 ? 1.0 : 1.7;
     return attn_rounds(x) * (9.0 + scale * (1.4 + 0.25 * std::min(1.0, x)) * (double)((tiles + ns - 1) / ns)) +
            (ns > 1 ? 3.5 + (double)(items * ns) * tile_rows * m.head_dim * 8 / 8e6 : 0.0);
+}
+
+// The same in blocks of 128 rows: 10 us and 1.13 us per tile with a block per unit at most (its wavefronts have a SIMD each); with two on a unit every tile is decoded twice
+// there, and at D = 128 the registers do not suffice.  us in 256 rows / 128, best cuts: one layer, 4000 keys, D 128, Tq 128 26.0 / 22.2, Tq 512 44.8 / 50.6, 32 layers, G = 1, Tq 128
+// 115 / 80; D 64: 19.3 / 15.2, 31.4 / 31.5, 77 / 51; 8 layers, 8704 keys, Tq 512, D 128 451 / 502, D 64 294 / 301.
+double kv4_tiles128_us(const kvcomm_model &m, int64_t items, int64_t tiles, int64_t ns)
+{
+    const double x = (double)(items * ns) / kChipCUs, t = (double)((tiles + ns - 1) / ns);
+    const double us = x <= 1 ? 10.0 + (m.head_dim == 64 ? 0.65 : 1.13) * t : attn_rounds(0.5 * x) * (10.0 + (m.head_dim == 64 ? 1.03 : 1.8) * t);
+    return us + (ns > 1 ? 3.5 + (double)(items * ns) * 128 * m.head_dim * 8 / 8e6 : 0.0);
 }
 
 // Which kernel, in how many runs of keys: the least by these times.  Measured, 8 kv heads, G = 4, D = 128, us: rows kernel in 1 / 2 / 4 / 8 / 16 runs and
@@ -296,9 +306,15 @@ AttnPlan plan_kv4(const kvcomm_model &m, int n_ctx, int tq, bool may_split)
         const double t = kv4_rows_us(m, items, its, ns);
         if (t < best) best = t, pl.n_splits = ns;
     }
-    for (int ns = 1; ns == 1 || (may_split && ns <= kTileMaxSplits && ns * kMinRunTiles <= tiles && tile_items * ns <= 2 * kChipCUs); ++ns) {
+    auto may_cut = [&](int64_t blocks, int ns) { return ns == 1 || (may_split && ns <= kTileMaxSplits && ns * kMinRunTiles <= tiles && blocks * ns <= 2 * kChipCUs); };
+    for (int ns = 1; may_cut(tile_items, ns); ++ns) {
         const double t = kv4_tiles_us(m, tile_items, tile_rows, tiles, ns);
         if (t < best) best = t, pl = {false, tile_rows, (int)((rows + tile_rows - 1) / tile_rows), ns, 32};
+    }
+    const int64_t items128 = LH * ((rows + 127) / 128);
+    for (int ns = 1; m.head_dim != 256 && may_cut(items128, ns); ++ns) {
+        const double t = kv4_tiles128_us(m, items128, tiles, ns);
+        if (t < best) best = t, pl = {false, 128, (int)((rows + 127) / 128), ns, 32};
     }
     return pl;
 }

@@ -766,10 +766,10 @@ extern "C" size_t kvcomm_suffix_attn_workspace(const kvcomm_model *model, int32_
 
 namespace {
 
-template <int D, int NW, int WPE>
-int launch_window(const AttnParams &p, unsigned n_blocks, hipStream_t s)
+template <int D, int NW, int WPE, Keys KEYS>
+int launch_checked(const AttnParams &p, unsigned n_blocks, hipStream_t s)
 {
-    return launch(p.n_splits > 1 ? attn_mfma_kernel<D, NW, WPE + form(Keys::kWindow), false, true> : attn_mfma_kernel<D, NW, WPE + form(Keys::kWindow), false, false>,
+    return launch(p.n_splits > 1 ? attn_mfma_kernel<D, NW, WPE + form(KEYS), false, true> : attn_mfma_kernel<D, NW, WPE + form(KEYS), false, false>,
                   dim3(n_blocks), dim3(64 * NW), 0, s, p);
 }
 
@@ -777,13 +777,11 @@ template <int D, int NW, int WPE>
 int launch_mfma(const AttnParams &p, unsigned n_blocks, bool persist, hipStream_t s)
 {
     const dim3 grid(n_blocks), block(64 * NW);
-    if (p.k_scales)
-        return p.n_splits > 1 ? launch(attn_mfma_kernel<D, NW, WPE + form(Keys::kFp4), false, true>, grid, block, 0, s, p)
-                              : launch(attn_mfma_kernel<D, NW, WPE + form(Keys::kFp4), false, false>, grid, block, 0, s, p);
+    if (p.k_scales) return D != 256 && p.groups_per_tile == 4 ? launch_checked<D, 4, WPE, Keys::kFp4>(p, n_blocks, s) : launch_checked<D, NW, WPE, Keys::kFp4>(p, n_blocks, s);
     if (p.window) {   // blocks of 128 or, at D = 128, of 256 rows
         if constexpr (D == 128)
-            if (p.groups_per_tile == NW) return launch_window<D, NW, WPE>(p, n_blocks, s);
-        return launch_window<D, 4, WPE>(p, n_blocks, s);
+            if (p.groups_per_tile == NW) return launch_checked<D, NW, WPE, Keys::kWindow>(p, n_blocks, s);
+        return launch_checked<D, 4, WPE, Keys::kWindow>(p, n_blocks, s);
     }
     if (p.n_splits > 1)
         return persist ? launch(attn_mfma_kernel<D, NW, WPE, true, true>, grid, block, 0, s, p)

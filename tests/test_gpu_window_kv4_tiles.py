@@ -19,7 +19,8 @@ WINDOW_TILES = [(1, 8, 8, 64, 0, 130, 100, 3), (1, 8, 8, 64, 900, 130, 1024, 70)
                 (1, 4, 8, 256, 1500, 130, 2500, 4), (32, 8, 4, 128, 2600, 1, 2200, 4)]
 # L, Hkv, G, D, n_ctx, tq
 COMPACT_TILES = [(4, 8, 8, 64, 0, 130), (1, 4, 4, 64, 900, 700), (1, 8, 8, 128, 0, 260), (1, 4, 8, 128, 900, 400), (1, 4, 1, 128, 70, 2000), (2, 8, 8, 256, 70, 130),
-                 (1, 2, 8, 256, 3000, 130), (4, 8, 4, 128, 1000, 321), (1, 8, 4, 128, 4000, 256), (2, 8, 4, 64, 2049, 513), (32, 8, 4, 128, 8300, 1)]
+                 (1, 2, 8, 256, 3000, 130), (4, 8, 4, 128, 1000, 321), (1, 8, 4, 128, 4000, 256), (2, 8, 4, 64, 2049, 513), (1, 8, 8, 64, 0, 260), (1, 4, 8, 64, 900, 400), (1, 4, 2, 128, 4000, 400), (4, 8, 8, 128, 33, 130),
+                 (32, 8, 4, 128, 8300, 1)]
 name = lambda c: "-".join(map(str, c))
 
 

@@ -79,6 +79,6 @@ def test_the_shapes_of_the_gpu_tests_reach_every_kernel(tmp_path):
     want |= {(False, "attn_mfma_kernel", D, 256, cut) for D in (64, 256) for cut in (False, True)}
     want |= {(c, "attn_f32_kernel", D, 512, False) for c in (False, True) for D in (64, 128, 256)}
     want |= {(True, "attn_kv4_rows_kernel", D, 512, cut) for D in (64, 128, 256) for cut in (False, True)}
-    want |= {(True, "attn_mfma_kernel", D, 256 if D == 256 else 512, cut) for D in (64, 128, 256) for cut in (False, True)}
+    want |= {(True, "attn_mfma_kernel", D, t, cut) for D in (64, 128, 256) for t in ((256,) if D == 256 else (256, 512)) for cut in (False, True)}
     want |= {(False, "attn_rows_kernel16", "non-temporal"), (True, "attn_kv4_rows_kernel", "non-temporal")}
     assert want <= seen, sorted(want - seen)
