@@ -846,13 +846,13 @@ def kvcomm_place_qkv(model, q, k, v, first_pos, q_out=None, k_out=None, v_out=No
     q_weight, k_weight [D] or [L, D]), rotation of token i to position first_pos + i, v copied.  k_out and v_out are normally views of the agent's
     cache; outputs that are not passed are made.  None in the place of q, k or v leaves it out."""
     lib = load_library()
-    ins, outs = [q, k, v], [q_out, k_out, v_out]
-    for i, x in enumerate(ins):
-        if x is not None and outs[i] is None:
-            with on_stream(stream):
-                outs[i] = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    if _done(_native.place_qkv(model, q, k, v, first_pos, q_weight, k_weight, norm_eps, outs[0], outs[1], outs[2], stream)):
-        return tuple(outs)
+    if (q_out is None and q is not None) or (k_out is None and k is not None) or (v_out is None and v is not None):
+        with on_stream(stream):
+            q_out, k_out, v_out = (torch.empty(x.shape, dtype=x.dtype, device=x.device) if y is None and x is not None else y
+                                   for x, y in ((q, q_out), (k, k_out), (v, v_out)))
+    if _done(_native.place_qkv(model, q, k, v, first_pos, q_weight, k_weight, norm_eps, q_out, k_out, v_out, stream)):
+        return q_out, k_out, v_out
+    ins, outs = (q, k, v), (q_out, k_out, v_out)
     n = next((x.shape[2] for x in ins if x is not None), 0)
     none = _CTensor(None, 0, 0, 0)
     cin, cout = [none] * 3, [none] * 3
@@ -870,7 +870,7 @@ def kvcomm_place_qkv(model, q, k, v, first_pos, q_out=None, k_out=None, v_out=No
         weights.append((None, 0) if w is None else (w.data_ptr(), w.stride(0) if w.dim() == 2 else 0))
     _check(lib.kvcomm_place_qkv(ctypes.byref(model.c()), *cin, n, int(first_pos), weights[0][0], weights[1][0], weights[0][1], weights[1][1],
                                 float(norm_eps), *cout, _on_stream_of((*ins, *outs, q_weight, k_weight), stream)))
-    return tuple(outs)
+    return outs
 
 
 def kvcomm_quantize_kv4(model, k, v, out_k=None, out_v=None, stream=None):
