@@ -1,6 +1,7 @@
 // Attention of single rows by the formula, key by key, in fp32: a key that a query does not see is not looked at.  The tiled kernels multiply
 // whole tiles, where a hidden key has probability 0: with an infinity or NaN among its values the product is NaN.  They check what they
-// computed at the end, and a block that holds anything that is not finite computes its rows again here.
+// computed at the end, and a block that holds anything that is not finite computes its rows again here (tens of times slower: a launch whose
+// every tile meets a NaN is a rare one, and should be right rather than fast).
 #pragma once
 
 #include "attn_common.h"
@@ -84,7 +85,7 @@ __device__ __forceinline__ void attn_exact_rows(const P &p, int lh, int row0, in
         for (int part = 0; part < 2; ++part) {
             const int begin = part ? keys.begin : keys.first, end = min(part ? keys.end : keys.first_end, pos + 1);
 #pragma unroll 1
-            for (int key0 = begin; key0 < end; key0 += 64) {   // a key per lane
+            for (int key0 = begin; key0 < end && sum == sum; key0 += 64) {   // a key per lane; a sum that is not a number stays so, and the row with it
                 const int key = key0 + lane;
                 const bool seen = key < end && (p.window == 0 || key > pos - p.window || key < p.n_sinks);
                 float s = -INFINITY;

@@ -415,6 +415,7 @@ template <int D, int RH, bool PERSIST, Keys KEYS>
 __global__ __launch_bounds__(64 * kF32Waves, D == 64 ? 4 : 2) void attn_f32_kernel(const AttnParams p)
 {
     await_attn_args(p);
+    if constexpr (KEYS != Keys::kAll) await_args(arg_word(&p.window), arg_word(&p.s_vs));
     if constexpr (!PERSIST) {
         attn_f32_item<D, RH, KEYS>(p, blockIdx.x);
     } else {

@@ -46,6 +46,7 @@ __global__ __launch_bounds__(512, D == 256 ? 2 : 4) void attn_kv4_rows_kernel(co
     __shared__ float ml[2][NW][ROWS];
 
     await_attn_args(p);
+    await_args(arg_word(&p.k_scales), arg_word(&p.s_vs));
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lane = tid & 63, n = lane & 15, g = lane >> 4;

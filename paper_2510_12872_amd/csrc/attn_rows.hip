@@ -78,6 +78,7 @@ __global__ __launch_bounds__(64 * rows_waves(D), D == 256 ? 1 : 2) void attn_row
     __shared__ float ml[2][NW][32];
 
     await_attn_args(p);
+    if constexpr (kWindow) await_args(arg_word(&p.window), arg_word(&p.n_sinks));
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lane = tid & 63, n = lane & 31, hg = lane >> 5;
@@ -331,6 +332,7 @@ __global__ __launch_bounds__(64 * rows_waves(D), D == 256 ? 1 : 2) void attn_row
     __shared__ float ml[2][NW][RH * ROWS];
 
     await_attn_args(p);
+    if constexpr (kWindow) await_args(arg_word(&p.window), arg_word(&p.n_sinks));
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lane = tid & 63, n = lane & 15, g = lane >> 4;

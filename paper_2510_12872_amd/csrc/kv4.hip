@@ -51,6 +51,8 @@ __global__ __launch_bounds__(kBlock) void quantize_kv4_kernel(const Kv4Params p)
 {
     constexpr int LPR = D / 8, RPB = kBlock / LPR;   // lanes of a row, rows of a block
     const int w = blockIdx.y;
+    await_args(arg_word(&p), arg_word(&p.s_x), arg_word(&p.s_codes), arg_word(&p.s_scales));
+    await_args(arg_word(&p.s_scales[1]), arg_word(&p.by_H));
     const int lh = div_by(blockIdx.x, p.by_tiles), tile = blockIdx.x - lh * p.n_tiles;
     const int l = div_by(lh, p.by_H), h = lh - l * p.H;
     const int t = tile * RPB + threadIdx.x / LPR, c = threadIdx.x % LPR;
@@ -71,6 +73,8 @@ __global__ __launch_bounds__(kBlock) void dequantize_kv4_kernel(const Kv4Params 
 {
     constexpr int LPR = D / 8, RPB = kBlock / LPR;
     const int w = blockIdx.y;
+    await_args(arg_word(&p), arg_word(&p.s_x), arg_word(&p.s_codes), arg_word(&p.s_scales));
+    await_args(arg_word(&p.s_scales[1]), arg_word(&p.by_H));
     const int lh = div_by(blockIdx.x, p.by_tiles), tile = blockIdx.x - lh * p.n_tiles;
     const int l = div_by(lh, p.by_H), h = lh - l * p.H;
     const int t = tile * RPB + threadIdx.x / LPR, c = threadIdx.x % LPR;

@@ -55,6 +55,11 @@ __global__ __launch_bounds__(kBlock) void place_kernel(const PlaceParams p)
 {
     constexpr int EPV = Elem<T>::EPV, LPR = D / 2 / EPV;   // channels of a 16-byte piece, lanes of a row
     const int c = threadIdx.x % LPR, slot = threadIdx.x / LPR;
+    double freq[EPV];   // the arguments lie in memory that no cache holds yet: all that is needed of them is requested first (one token 3.8 -> 3.6 us)
+#pragma unroll
+    for (int i = 0; i < EPV; ++i) freq[i] = p.inv_freq[c * EPV + i];
+    await_args(arg_word(&p), arg_word(&p.s_in[1]), arg_word(&p.s_out), arg_word(&p.s_out[2]));
+    await_args(arg_word(&p.heads), arg_word(&p.by_groups));
     const int rest = div_by(blockIdx.x, p.by_tiles), tile = blockIdx.x - rest * p.n_tiles;
     const int l = div_by(rest, p.by_groups), group = rest - l * p.group_end[2];
     const int which = group < p.group_end[0] ? 0 : group < p.group_end[1] ? 1 : 2;
@@ -104,7 +109,7 @@ __global__ __launch_bounds__(kBlock) void place_kernel(const PlaceParams p)
     float co[EPV], si[EPV];
 #pragma unroll
     for (int i = 0; i < EPV; ++i) {
-        const float2 cs = rope_cos_sin(p.first_pos + tt, p.inv_freq[c * EPV + i]);
+        const float2 cs = rope_cos_sin(p.first_pos + tt, freq[i]);
         co[i] = cs.x;
         si[i] = cs.y;
     }
