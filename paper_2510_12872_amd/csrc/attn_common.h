@@ -37,15 +37,17 @@ enum class Keys { kAll, kWindow, kFp4 };
 
 // The units (of `unit` keys) that the queries imin ... imax of a tile see through their windows, in order: `sinks` of them from key 0 on, which end
 // before the first unit of the windows, then those; unit u begins at key unit * (u + (u < sinks ? 0 : gap)).
+// Rows that no query sees are not read, as far as sinks and windows lie apart (gap > 0): loads of the first units stay before `sink_end`, the others' at
+// `oldest` and behind it.
 struct WindowUnits {
-    int sinks, gap, count;
+    int sinks, gap, count, oldest, sink_end;
 };
 template <class P>
 __device__ __forceinline__ WindowUnits window_units(const P &p, int imin, int imax, int unit)   // unit: a literal power of two
 {
-    const int first = max(0, p.n_ctx + imin + 1 - p.window) / unit, end = (p.n_ctx + imax) / unit + 1;
-    const int sinks = min((p.n_sinks + unit - 1) / unit, first);
-    return WindowUnits{sinks, first - sinks, sinks + end - first};
+    const int oldest = max(0, p.n_ctx + imin + 1 - p.window), first = oldest / unit, end = (p.n_ctx + imax) / unit + 1;
+    const int sinks = min((p.n_sinks + unit - 1) / unit, first), gap = first - sinks;
+    return WindowUnits{sinks, gap, sinks + end - first, gap > 0 ? oldest : 0, gap > 0 ? p.n_sinks : p.N};
 }
 
 __device__ __forceinline__ void await_attn_args(const AttnParams &p)

@@ -112,9 +112,17 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
     const int l = div_by(lh, p.by_Hkv), hkv = lh - l * p.Hkv;
     const int row0 = rt * 16 * RH;
     const int imax = min(p.tq - 1, div_by(row0 + 16 * RH - 1, p.by_G)), imin = min(p.tq - 1, div_by(row0, p.by_G));
-    WindowUnits wu = {0, 0, (p.n_ctx + imax + 16) / 16};   // sub-steps that some query of the tile sees
+    WindowUnits wu = {0, 0, (p.n_ctx + imax + 16) / 16, 0, 0};   // sub-steps that some query of the tile sees
     if constexpr (kWindow) wu = window_units(p, imin, imax, 16);
     const int units = wu.count;
+    // Row r of sub-step u.  Rows past the cache end re-read the last one, rows that no query's window or sinks hold the nearest that one does; they are always masked.
+    auto row_of = [&](int u, int r) __attribute__((always_inline)) -> int {
+        if constexpr (kWindow) {
+            const bool sink = u < wu.sinks;
+            return max(sink ? 0 : wu.oldest, min(16 * (sink ? u : u + wu.gap) + r, (sink ? wu.sink_end : p.N) - 1));
+        }
+        return min(16 * u + r, p.N - 1);
+    };
     auto first_key = [&](int u) __attribute__((always_inline)) -> int { return 16 * (kWindow && u >= wu.sinks ? u + wu.gap : u); };
 
     const Cache *kb = static_cast<const Cache *>(p.k) + l * p.s_k.layer + hkv * p.s_k.head;
@@ -148,14 +156,13 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
         return Codes{*reinterpret_cast<const uint16_t *>(row + c / 2), scales[c / 32]};
     };
     Piece k[HOLD][PJ], v[VR][NT];
-    // Rows past the cache end re-read the last one; they are always masked.
     auto load_k = [&](int u, int part) __attribute__((always_inline)) {
         if constexpr (kFp4) {
-            const int64_t key = min(first_key(u) + n, p.N - 1);
+            const int64_t key = row_of(u, n);
 #pragma unroll
             for (int j = 0; j < PJ; ++j) k[part % HOLD][j] = codes_at(kb + key * p.s_k.token, ksb + key * p.s_ks.token, 16 * (PJ * part + j) + 4 * g);
         } else {
-            const float *kr = kb + (int64_t)min(first_key(u) + n, p.N - 1) * p.s_k.token + 16 * PJ * part + 4 * g;
+            const float *kr = kb + (int64_t)row_of(u, n) * p.s_k.token + 16 * PJ * part + 4 * g;
 #pragma unroll
             for (int j = 0; j < PJ; ++j) k[part % HOLD][j] = *reinterpret_cast<const f32x4 *>(kr + 16 * j);
         }
@@ -164,11 +171,11 @@ __device__ __forceinline__ void attn_f32_item(const AttnParams &p, int item)   /
 #pragma unroll
         for (int r = 0; r < VR; ++r) {
             if constexpr (kFp4) {
-                const int64_t key = min(first_key(u) + 4 * g + r0 + r, p.N - 1);
+                const int64_t key = row_of(u, 4 * g + r0 + r);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) v[r][t] = codes_at(vb + key * p.s_v.token, vsb + key * p.s_vs.token, 64 * t + 4 * n);
             } else {
-                const float *vr = vb + (int64_t)min(first_key(u) + 4 * g + r0 + r, p.N - 1) * p.s_v.token + 4 * n;
+                const float *vr = vb + (int64_t)row_of(u, 4 * g + r0 + r) * p.s_v.token + 4 * n;
 #pragma unroll
                 for (int t = 0; t < NT; ++t) v[r][t] = *reinterpret_cast<const f32x4 *>(vr + 64 * t);
             }

@@ -46,6 +46,23 @@ __device__ __forceinline__ void load_half(const unsigned char *bytes, int64_t to
     }
 }
 
+// The same of a window's rows: those outside [lo, hi] (wavefront-uniform), which are always masked, re-read the nearest one inside.
+template <int D, bool NT, int NIN, class Swz>
+__device__ __forceinline__ void load_half_between(const unsigned char *bytes, int64_t tok, int key0, int lo, int hi, const uint32_t (&in)[NIN], int lane, Swz swz,
+                                                  lds_byte *dst)
+{
+    constexpr int KCH = D / 8, ROWB = D * 2, RPL = 64 / KCH, LPT = 32 / RPL;
+    if (key0 >= lo && key0 + 31 <= hi) return load_half<D, NT>(bytes, tok, key0, hi + 1, in, lane, swz, dst);
+    const int lq = lane / KCH;
+#pragma unroll 1
+    for (int it = 0; it < LPT; ++it) {
+        const int row0 = max(lo, min(key0 + it * RPL, hi));
+        const int row = max(0, min(key0 + it * RPL + lq - row0, hi - row0));   // at most lq
+        dma16_sbase<NT>(bytes + (int64_t)row0 * tok * 2, (uint32_t)row * (uint32_t)(tok * 2) + (uint32_t)(((lane % KCH) ^ swz(it * RPL + lq)) * 16),
+                        dst + it * RPL * ROWB);
+    }
+}
+
 // attn_rows_kernel: 32 packed (query, head) rows per block (GQA packing and transposed products as in
 // attn_mfma_kernel), which the wavefronts SHARE: each takes every NW-th 32-key sub-step of the block's key
 // run with its own softmax state, and the states are joined through LDS at the end.  The 256-row kernel would leave
@@ -103,7 +120,7 @@ __global__ __launch_bounds__(64 * rows_waves(D), D == 256 ? 1 : 2) void attn_row
         const int qi = min(i_row, p.tq - 1);
         const int hq = hkv * p.G + r_row - i_row * p.G;
         const int imax = min(p.tq - 1, div_by(rt * 32 + 31, p.by_G)), imin = min(p.tq - 1, div_by(rt * 32, p.by_G));
-        WindowUnits wu = {0, 0, (p.n_ctx + imax + 32) / 32};   // sub-steps that some query of the tile sees
+        WindowUnits wu = {0, 0, (p.n_ctx + imax + 32) / 32, 0, 0};   // sub-steps that some query of the tile sees
         if constexpr (kWindow) wu = window_units(p, imin, imax, 32);
         const int units = wu.count;
         auto first_key = [&](int u) __attribute__((always_inline)) -> int { return 32 * (kWindow && u >= wu.sinks ? u + wu.gap : u); };
@@ -115,8 +132,16 @@ __global__ __launch_bounds__(64 * rows_waves(D), D == 256 ? 1 : 2) void attn_row
         uint32_t k_in[KD], v_in[VD];
         lane_offsets<D>(k_in, lane, p.s_k.token, k_swz);
         lane_offsets<D>(v_in, lane, p.s_v.token, v_swz);
-        auto load_k = [&](int u) __attribute__((always_inline)) { load_half<D, NT>(kbytes, p.s_k.token, first_key(u), p.N, k_in, lane, k_swz, kbuf); };
-        auto load_v = [&](int u) __attribute__((always_inline)) { load_half<D, NT>(vbytes, p.s_v.token, first_key(u), p.N, v_in, lane, v_swz, vbuf); };
+        auto load = [&](const unsigned char *bytes, int64_t tok, int u, auto &in, auto swz, lds_byte *dst) __attribute__((always_inline)) {
+            if constexpr (kWindow) {
+                const bool sink = u < wu.sinks;
+                load_half_between<D, NT>(bytes, tok, first_key(u), sink ? 0 : wu.oldest, (sink ? wu.sink_end : p.N) - 1, in, lane, swz, dst);
+            } else {
+                load_half<D, NT>(bytes, tok, 32 * u, p.N, in, lane, swz, dst);
+            }
+        };
+        auto load_k = [&](int u) __attribute__((always_inline)) { load(kbytes, p.s_k.token, u, k_in, k_swz, kbuf); };
+        auto load_v = [&](int u) __attribute__((always_inline)) { load(vbytes, p.s_v.token, u, v_in, v_swz, vbuf); };
         int u = u0 + wave;
         bf16x8 qf[NKS];
         const bf16_t *qrow = static_cast<const bf16_t *>(p.q) + l * p.s_q.layer + (int64_t)hq * p.s_q.head + (int64_t)qi * p.s_q.token;
@@ -355,7 +380,7 @@ __global__ __launch_bounds__(64 * rows_waves(D), D == 256 ? 1 : 2) void attn_row
 
         int qi[RH], hq[RH], imin[RH], u0[RH], u1[RH];
         bool valid[RH];
-        WindowUnits wu = {0, 0, 0};
+        WindowUnits wu = {0, 0, 0, 0, 0};
         int left = 0;   // last key that some query's window has left
 #pragma unroll
         for (int h = 0; h < RH; ++h) {
@@ -386,8 +411,16 @@ __global__ __launch_bounds__(64 * rows_waves(D), D == 256 ? 1 : 2) void attn_row
         uint32_t k_in[KD], v_in[VD];
         lane_offsets<D>(k_in, lane, p.s_k.token, k_swz);
         lane_offsets<D>(v_in, lane, p.s_v.token, v_swz);
-        auto load_k = [&](int u) __attribute__((always_inline)) { load_half<D, NT>(kbytes, p.s_k.token, first_key(u), p.N, k_in, lane, k_swz, kbuf); };
-        auto load_v = [&](int u) __attribute__((always_inline)) { load_half<D, NT>(vbytes, p.s_v.token, first_key(u), p.N, v_in, lane, v_swz, vbuf); };
+        auto load = [&](const unsigned char *bytes, int64_t tok, int u, auto &in, auto swz, lds_byte *dst) __attribute__((always_inline)) {
+            if constexpr (kWindow) {
+                const bool sink = u < wu.sinks;
+                load_half_between<D, NT>(bytes, tok, first_key(u), sink ? 0 : wu.oldest, (sink ? wu.sink_end : p.N) - 1, in, lane, swz, dst);
+            } else {
+                load_half<D, NT>(bytes, tok, 32 * u, p.N, in, lane, swz, dst);
+            }
+        };
+        auto load_k = [&](int u) __attribute__((always_inline)) { load(kbytes, p.s_k.token, u, k_in, k_swz, kbuf); };
+        auto load_v = [&](int u) __attribute__((always_inline)) { load(vbytes, p.s_v.token, u, v_in, v_swz, vbuf); };
         int u = u0[0] + wave, turn = 0;
         bf16x8 qf[RH][NF / 2];
 #pragma unroll

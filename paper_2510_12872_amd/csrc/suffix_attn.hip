@@ -76,7 +76,7 @@ __device__ __forceinline__ void exact_tile()
     }
     const int lh = div_by(logical, p.by_row_tiles), rt = p.n_row_tiles - 1 - (logical - lh * p.n_row_tiles);
     const int imin = min(p.tq - 1, div_by(rt * BM, p.by_G)), imax = min(p.tq - 1, div_by(rt * BM + BM - 1, p.by_G));
-    WindowUnits wu = {0, 0, (p.n_ctx + imax) / 32 + 1};
+    WindowUnits wu = {0, 0, (p.n_ctx + imax) / 32 + 1, 0, 0};
     if (KEYS == Keys::kWindow) wu = window_units(p, imin, imax, 32);
     const int tiles = (wu.count + 1) / 2;
     const int begin = SPLIT ? 2 * even_bound(split, p, tiles) : 0, end = 2 * (SPLIT ? even_bound(split + 1, p, tiles) : tiles);   // in halves of tiles
@@ -183,7 +183,7 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     const int wg_imin = min(p.tq - 1, div_by(rt * BM, p.by_G));
     const int all_tiles = (p.n_ctx + wg_imax + 1 + 63) / 64;
     const int first_hidden = (p.n_ctx + wg_imin) / 64 + 1;
-    WindowUnits wu = {0, 0, 2 * all_tiles};   // in halves of tiles
+    WindowUnits wu = {0, 0, 2 * all_tiles, 0, 0};   // in halves of tiles
     if constexpr (kWindow) wu = window_units(p, wg_imin, wg_imax, 32);
     const int walk_tiles = kWindow ? (wu.count + 1) / 2 : all_tiles;   // (a half too many lies behind the last query)
     // (a run cut evenly may begin with keys that some query does not see: the reference of such a row is set later)
@@ -256,7 +256,14 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     const int lq = lane / KCH;  // this lane's row inside a load
     const uint32_t k_row_bytes = (uint32_t)(p.s_k.token * 2), v_row_bytes = (uint32_t)(p.s_v.token * 2);
     auto load_rows = [&](const unsigned char *bytes, int64_t tok_stride, uint32_t row_bytes, int row0, uint32_t voff,
-                         const lds_byte *dst) __attribute__((always_inline)) {
+                         const lds_byte *dst, [[maybe_unused]] bool sink) __attribute__((always_inline)) {
+        if constexpr (kWindow) {   // likewise rows that no query sees: the nearest one that some query sees instead
+            const int lo = sink ? -origin : wu.oldest - origin, hi = sink ? wu.sink_end - 1 - origin : N_() - 1;
+            const int row0c = max(lo, min(row0, hi));
+            const int row = max(0, min(lq + row0 - row0c, hi - row0c));
+            dma16_sbase(bytes + (int64_t)row0c * tok_stride * 2, voff + (uint32_t)(row - lq) * row_bytes, dst);
+            return;
+        }
         const int row0c = min(row0, N_() - 1);            // wavefront-uniform
         const int excess = max(lq - (N_() - 1 - row0c), 0);  // rows this lane would overshoot by
         dma16_sbase(bytes + (int64_t)row0c * tok_stride * 2, voff - (uint32_t)excess * row_bytes, dst);
@@ -268,14 +275,14 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
 #pragma unroll
         for (int it = 0; it < LPT; ++it)
             load_rows(kbytes, p.s_k.token, k_row_bytes, 32 * h + half_shift(h) + rbase + it * RPL, ld_koff[it],
-                      kring + (h & 3) * HALFB + (rbase + it * RPL) * ROWB);
+                      kring + (h & 3) * HALFB + (rbase + it * RPL) * ROWB, h < sink_halves);
     };
     auto load_v64 = [&](int tile) __attribute__((always_inline)) {
         if (tile >= n_tiles) return;
 #pragma unroll
         for (int it = 0; it < LPT; ++it)
             load_rows(vbytes, p.s_v.token, v_row_bytes, 64 * tile + half_shift(2 * tile + wave / (NW / 2)) + wave * RW + it * RPL, ld_voff[it],
-                      vbuf + (tile & 1) * TILEB + (wave * RW + it * RPL) * ROWB);
+                      vbuf + (tile & 1) * TILEB + (wave * RW + it * RPL) * ROWB, 2 * tile + wave / (NW / 2) < sink_halves);
     };
     // ---- 4-bit caches: a thread holds the codes of CT channels of one row of a 64-key tile (NW threads a row) and their scales, requested a tile ahead
     // of their turn, decodes them at the start of a tile and stores them where the direct loads would have put them.
