@@ -305,8 +305,8 @@ def reuse_agent(w, model, agent, out=None, gran=kv.W_TOKEN, scratches=None, stre
 
 
 class CompactCache:
-    """An agent's cache in 4 bits per value: room for `capacity` tokens, of which the first `length` are there.  A 3072-token cache of 32 layers,
-    8 heads and 128 channels takes 214 MB where bf16 takes 805."""
+    """An agent's cache in 4 bits per value: room for `capacity` tokens, of which the first `length` are there.  4096 tokens of 32 layers, 8 heads
+    and 128 channels take 143 MB where bf16 takes 537."""
 
     def __init__(self, model, capacity, device):
         self.model, self.capacity, self.length = model, capacity, 0
