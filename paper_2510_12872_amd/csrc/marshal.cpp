@@ -233,16 +233,23 @@ int32_t tokens_of(const at::Tensor &t)
     return (int32_t)t.size(2);
 }
 
-// The stream's handle: the given one's, or the current one's on the current device.
-void *stream_of(PyObject *o)
+// The stream's handle: the given one's, or the current one's on the current device.  `device`: that device, if asked for (a stream that names none: -1).
+void *stream_of(PyObject *o, long *device = nullptr)
 {
     PyObject *h;
     if (o != Py_None) {
+        if (device) {
+            PyObject *dev = PyObject_GetAttr(o, names.device_index);
+            if (!dev) throw Decline{};
+            *device = PyLong_CheckExact(dev) ? PyLong_AsLong(dev) : -1;
+            Py_DECREF(dev);
+        }
         h = PyObject_GetAttr(o, names.cuda_stream);
     } else {
         if (lib.current_stream == Py_None) throw Decline{};
         PyObject *dev = PyObject_CallNoArgs(lib.current_device);
         if (!dev) throw Decline{};
+        if (device) *device = PyLong_CheckExact(dev) ? PyLong_AsLong(dev) : -1;
         h = PyObject_CallOneArg(lib.current_stream, dev);
         Py_DECREF(dev);
     }
@@ -257,12 +264,10 @@ void *stream_of(PyObject *o)
 // The same, of the call's device: a stream of another one would run the kernels where the tensors are not.
 void *stream_of(const Call &c, PyObject *o)
 {
-    PyObject *dev = o == Py_None ? PyObject_CallNoArgs(lib.current_device) : PyObject_GetAttr(o, names.device_index);
-    if (!dev) throw Decline{};
-    const long v = PyLong_CheckExact(dev) ? PyLong_AsLong(dev) : -1;
-    Py_DECREF(dev);
-    if (v != c.device) throw Decline{};
-    return stream_of(o);
+    long device = -1;
+    void *stream = stream_of(o, &device);
+    if (device != c.device) throw Decline{};
+    return stream;
 }
 
 PyObject *item(PyObject *dict, PyObject *name)   // borrowed; None where there is none
