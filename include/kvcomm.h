@@ -457,7 +457,8 @@ int kvcomm_place_qkv(const kvcomm_model *model, kvcomm_tensor q, kvcomm_tensor k
  * ties to the even code, so |error| <= scale (half the top step), and what lies beyond 7 * 2^125 saturates.  A block with a NaN or an infinity
  * gets byte 255.  Reproducible bit for bit.
  * kvcomm_dequantize_kv4: the values back, exact in either type (below 2^-126: subnormal).
- * Errors as for kvcomm_capture_offsets; KVCOMM_EINVAL where an output shares bytes with another tensor of the call.  */
+ * Errors as for kvcomm_capture_offsets; KVCOMM_EINVAL where an output shares bytes with another tensor of the call
+ * (compared as in kvcomm_place_qkv: codes and scales, keys and values may lie token by token beside each other).  */
 typedef struct {
     kvcomm_tensor codes, scales;
 } kvcomm_tensor4;

@@ -104,7 +104,11 @@ int kv4_call(bool back, const kvcomm_model *model, const kvcomm_tensor (&x)[2], 
     if (st) return st;
     if (n <= 0) return KVCOMM_EINVAL;
     const int L = model->n_layers, H = model->n_kv_heads, D = model->head_dim;
-    Extent in[6], out[6];
+    struct Part {   // a tensor of the call, bytes of its rows and of what its strides count
+        kvcomm_tensor t;
+        int64_t row;
+        int es;
+    } in[6], out[6];
     int n_in = 0, n_out = 0;
     Kv4Params p{};
     for (int w = 0; w < 2; ++w) {
@@ -115,15 +119,18 @@ int kv4_call(bool back, const kvcomm_model *model, const kvcomm_tensor (&x)[2], 
         p.s_x[w] = strides_of(x[w]);
         p.s_codes[w] = strides_of(x4[w].codes);
         p.s_scales[w] = strides_of(x4[w].scales);
-        (back ? out[n_out++] : in[n_in++]) = extent_of(x[w], L, H, n, D, elem_size(model->dtype));
-        (back ? in[n_in++] : out[n_out++]) = extent_of(x4[w].codes, L, H, n, D / 2, 1);
-        (back ? in[n_in++] : out[n_out++]) = extent_of(x4[w].scales, L, H, n, D / 32, 1);
+        const int es = elem_size(model->dtype);
+        (back ? out[n_out++] : in[n_in++]) = Part{x[w], (int64_t)D * es, es};
+        (back ? in[n_in++] : out[n_out++]) = Part{x4[w].codes, D / 2, 1};
+        (back ? in[n_in++] : out[n_out++]) = Part{x4[w].scales, D / 32, 1};
     }
+    auto extent = [&](const Part &a) { return extent_of(a.t, L, H, n, (int)(a.row / a.es), a.es); };
+    auto meet = [&](const Part &a, const Part &b) { return extents_overlap(extent(a), extent(b)) && !beside_each_other(a.t, H, a.row, a.es, b.t, H, b.row, b.es, L); };
     for (int i = 0; i < n_out; ++i) {
         for (int j = 0; j < n_in; ++j)
-            if (extents_overlap(out[i], in[j])) return KVCOMM_EINVAL;
+            if (meet(out[i], in[j])) return KVCOMM_EINVAL;
         for (int j = 0; j < i; ++j)
-            if (extents_overlap(out[i], out[j])) return KVCOMM_EINVAL;
+            if (meet(out[i], out[j])) return KVCOMM_EINVAL;
     }
     p.n = n;
     p.H = H;

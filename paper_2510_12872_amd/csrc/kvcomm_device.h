@@ -276,6 +276,20 @@ static inline bool extents_overlap(const Extent &a, const Extent &b)
     return false;
 }
 
+// Do two tensors lie token by token beside each other, as the parts of a projection or the keys and values of a [token, 2, head, channel] cache do?  They have the same distance
+// st from token to token, layers (and heads, where these are not within a token's st bytes) lie whole numbers of st apart, and each stays in its own piece of every st bytes.
+// row: bytes of a row, es: bytes of what the strides count.
+static inline bool beside_each_other(const kvcomm_tensor &a, int Ha, int64_t row_a, int es_a, const kvcomm_tensor &b, int Hb, int64_t row_b, int es_b, int L)
+{
+    const int64_t st = a.stride_token * es_a;
+    if (st <= 0 || b.stride_token * es_b != st) return false;
+    if (L > 1 && (a.stride_layer * es_a % st || b.stride_layer * es_b % st)) return false;
+    auto piece = [&](const kvcomm_tensor &t, int H, int64_t row, int es) { return (t.stride_head * es % st ? (H - 1) * t.stride_head * es : 0) + row; };
+    int64_t gap = (int64_t)(reinterpret_cast<uintptr_t>(b.ptr) - reinterpret_cast<uintptr_t>(a.ptr)) % st;   // of b's piece behind a's begin
+    if (gap < 0) gap += st;
+    return gap >= piece(a, Ha, row_a, es_a) && gap + piece(b, Hb, row_b, es_b) <= st;
+}
+
 // Launches a kernel that takes its parameter block by value and maps THIS launch's own return code: an
 // error that an earlier, unrelated HIP call left on the thread is neither reported nor cleared.
 template <typename P>

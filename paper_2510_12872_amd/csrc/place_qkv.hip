@@ -182,18 +182,6 @@ int launch_place(PlaceParams &p, int L, hipStream_t s)
     return launch(p.heads_per_group == at_once ? one : two, dim3((unsigned)blocks), dim3(kBlock), 0, s, p);
 }
 
-// Tensors that lie token by token beside each other, as the parts of a projection do: the same distance st from token to token, layers whole numbers of tokens apart,
-// and all heads of each within its own piece of every st bytes.
-bool beside_each_other(const kvcomm_tensor &a, int Ha, const kvcomm_tensor &b, int Hb, int L, int D, int es)
-{
-    const int64_t st = a.stride_token;
-    if (st <= 0 || b.stride_token != st || (L > 1 && (a.stride_layer % st || b.stride_layer % st))) return false;
-    const int64_t piece_a = (Ha - 1) * a.stride_head + D, piece_b = (Hb - 1) * b.stride_head + D;
-    int64_t gap = (int64_t)(reinterpret_cast<uintptr_t>(b.ptr) - reinterpret_cast<uintptr_t>(a.ptr)) % (st * es);   // of b's piece behind a's begin
-    if (gap < 0) gap += st * es;
-    return gap >= piece_a * es && gap + piece_b * es <= st * es;
-}
-
 }  // namespace
 
 extern "C" int kvcomm_place_qkv(const kvcomm_model *model, kvcomm_tensor q, kvcomm_tensor k, kvcomm_tensor v, int32_t n_tokens, int32_t first_pos,
@@ -235,7 +223,7 @@ extern "C" int kvcomm_place_qkv(const kvcomm_model *model, kvcomm_tensor q, kvco
         p.s_weight[i] = w_stride[i];
         from[n_from++] = extent_of(w, L, 1, 1, D, es);
     }
-    auto apart = [&](int i, int j, const kvcomm_tensor &y) { return beside_each_other(out[is[i]], heads[is[i]], y, heads[is[j]], L, D, es); };
+    auto apart = [&](int i, int j, const kvcomm_tensor &y) { return beside_each_other(out[is[i]], heads[is[i]], D * es, es, y, heads[is[j]], D * es, es, L); };
     for (int i = 0; i < n_to; ++i) {
         for (int j = 0; j < n_from; ++j) {
             const bool pair = j < n_pairs;

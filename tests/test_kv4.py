@@ -135,6 +135,25 @@ def test_rows_of_a_longer_cache_on_another_stream():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("D,dtype", [(128, torch.bfloat16), (64, torch.float32)])
+def test_records(D, dtype):
+    """Keys and values of a token together, codes and scales of a token together: the bits of separate tensors."""
+    L, H, n = 2, 3, 21
+    m = kv.Model(L, H, H, D, dtype, 1e4)
+    kv_rows = _values((L, n, 2, H, D), dtype, 8).cuda()
+    k, v = (kv_rows[:, :, i].transpose(1, 2) for i in range(2))
+    record = -(-(D // 2 + D // 32) // 16) * 16
+    raw = torch.zeros((2, L, H, n, record), dtype=torch.uint8, device="cuda")
+    pair = lambda i: (raw[i][..., :D // 2], raw[i][..., D // 2:D // 2 + D // 32])
+    got = kv.kvcomm_quantize_kv4(m, k, v, out_k=pair(0), out_v=pair(1))
+    want = kv.kvcomm_quantize_kv4(m, k.contiguous(), v.contiguous())
+    assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))
+    back = torch.zeros_like(kv_rows)
+    kv.kvcomm_dequantize_kv4(m, pair(0), pair(1), out_k=back[:, :, 0].transpose(1, 2), out_v=back[:, :, 1].transpose(1, 2))
+    assert all(torch.equal(back[:, :, i].transpose(1, 2), t) for i, t in enumerate(kv.kvcomm_dequantize_kv4(m, *want)))
+
+
+@pytest.mark.gpu
 def test_refusals_of_the_binding():
     m = kv.Model(2, 2, 4, 64, torch.bfloat16, 1e4)
     x = lambda n=3, h=2, d=torch.bfloat16, D=64: torch.zeros((2, h, n, D), dtype=d, device="cuda")
@@ -167,6 +186,9 @@ def test_refusals_of_the_library():
         for back in (False, True):
             if not (back and "v4" in change):   # (two inputs may be one)
                 assert call(**change, back=back) == -1, (change, back)
+    # keys' codes and scales in records of 80 bytes a token: 64 and 4 bytes beside each other, and one byte too far
+    record = lambda at: binding._CTensor4(T(0x30000000, 80 * 1024, 80 * 256, 80), T(0x30000000 + at, 80 * 1024, 80 * 256, 80))
+    assert call(k4=record(60)) == -1 and call(k4=record(80 - 0)) == -1
     assert call(D=96) == -2
     assert call(n=1 << 30, k=T(0x10000000, sl=1 << 50, sh=1 << 45), v=T(0x10000000 + (1 << 42), sl=1 << 50, sh=1 << 45),
                 k4=binding._CTensor4(T(1 << 56, 1 << 50, 1 << 45, 64), T((1 << 56) + (1 << 40), 1 << 50, 1 << 45, 4)),
