@@ -242,6 +242,27 @@ def _done(status):
     return True
 
 
+INT32_MAX = 2 ** 31 - 1
+
+
+def _int32(x, what):
+    """A number for the library.  ctypes would pass on its last 32 bits."""
+    x = int(x)
+    if not -INT32_MAX - 1 <= x <= INT32_MAX:
+        raise KVCommError(EINVAL, f"{what}: {x} does not fit 32 bits")
+    return x
+
+
+def _int32s(xs, n, what):
+    """The same of a list, as an array of n elements (one at least)."""
+    return (ctypes.c_int32 * max(n, 1))(*[_int32(x, what) for x in xs])
+
+
+def _at_most_int32(x, what):
+    """A number of tokens of which more than a cache can hold means all of them."""
+    return _int32(min(int(x), INT32_MAX), what)
+
+
 def _not_a_tensor(what, dtype):
     return KVCommError(-1, f"{what}: expected a 4-d {dtype} device tensor with contiguous channels")
 
@@ -303,7 +324,7 @@ def _anchor_args(anchors, anchor_len, dtype, what):
     n = len(anchors)
     if anchor_len is None:
         anchor_len = [a.shape[2] for a in anchors]
-    lens = (ctypes.c_int32 * n)(*[int(x) for x in anchor_len])
+    lens = _int32s(anchor_len, n, "anchor_len")
     return ptrs, layout, lens
 
 
@@ -384,7 +405,7 @@ def kvcomm_align_kv(model, base_k, base_v, anchor_dk, anchor_dv, weights, delta_
     if anchor_delta_pos is not None:
         if len(anchor_delta_pos) != A:
             raise KVCommError(-1, "anchor_delta_pos must have one entry per anchor")
-        adp = (ctypes.c_int32 * max(A, 1))(*[int(x) for x in anchor_delta_pos])
+        adp = _int32s(anchor_delta_pos, A, "anchor_delta_pos")
     if A:
         if weights is None or weights.dtype != torch.float32 or not weights.is_contiguous():
             raise KVCommError(-1, "weights: expected a contiguous fp32 device tensor [n, A]")
@@ -392,14 +413,14 @@ def kvcomm_align_kv(model, base_k, base_v, anchor_dk, anchor_dv, weights, delta_
             raise KVCommError(-1, "weights: wrong number of elements for this granularity")
     _check(lib.kvcomm_align_kv(ctypes.byref(model.c()), gran, _desc(base_k, model.dtype, "base_k"),
                                _desc(base_v, model.dtype, "base_v"), seg_len, pk, pv, layout, lens, A,
-                               None if weights is None else weights.data_ptr(), int(delta_pos), adp,
+                               None if weights is None else weights.data_ptr(), _int32(delta_pos, "delta_pos"), adp,
                                _desc(out_k, model.dtype, "out_k"), _desc(out_v, model.dtype, "out_v"),
                                _stream_ptr(stream)))
     return out_k, out_v
 
 
 def kvcomm_suffix_attn_workspace(model, n_ctx, tq):
-    return int(load_library().kvcomm_suffix_attn_workspace(ctypes.byref(model.c()), int(n_ctx), int(tq)))
+    return int(load_library().kvcomm_suffix_attn_workspace(ctypes.byref(model.c()), _int32(n_ctx, "n_ctx"), _int32(tq, "tq")))
 
 
 def _in_private_pool(t):
@@ -468,14 +489,14 @@ def _suffix_attn(model, q, cache_k, cache_v, n_ctx, max_blocks, softmax_scale, o
     cmodel = model.c()
     ws, ws_bytes, _keep = None, 0, None
     if workspace is not None or need is None:
-        ws, ws_bytes, _keep = _attn_workspace(cmodel, int(n_ctx), tq, workspace, q.device, stream)
+        ws, ws_bytes, _keep = _attn_workspace(cmodel, _int32(n_ctx, "n_ctx"), _int32(tq, "tq"), workspace, q.device, stream)
     args = (ctypes.byref(cmodel), _desc(q, model.dtype, "q"), _desc(cache_k, model.dtype, "cache_k"),
-            _desc(cache_v, model.dtype, "cache_v"), int(n_ctx), tq, float(softmax_scale), _desc(out, model.dtype, "out"),
+            _desc(cache_v, model.dtype, "cache_v"), _int32(n_ctx, "n_ctx"), _int32(tq, "tq"), float(softmax_scale), _desc(out, model.dtype, "out"),
             None if lse_out is None else lse_out.data_ptr())
     if max_blocks is None:
         _check(lib.kvcomm_suffix_attn(*args, ws, ws_bytes, _stream_ptr(stream)))
     else:
-        _check(lib.kvcomm_suffix_attn_confined_ws(*args, int(max_blocks), ws, ws_bytes, _stream_ptr(stream)))
+        _check(lib.kvcomm_suffix_attn_confined_ws(*args, _int32(max_blocks, "max_blocks"), ws, ws_bytes, _stream_ptr(stream)))
     return (out, lse_out) if want_lse else out
 
 
@@ -560,8 +581,8 @@ def kvcomm_anchor_predict(weights, anchor_len, seg_len, gamma, entropy_out=None,
         workspace = _workspace(max(kvcomm_anchor_predict_workspace(n), 8), dev, stream)
     if _done(_native.anchor_predict(weights, anchor_len, seg_len, gamma, entropy_out, result_out, workspace, stream)):
         return (result_out, entropy_out) if want_entropy else result_out
-    lens = (ctypes.c_int32 * max(A, 1))(*[int(x) for x in anchor_len])
-    _check(lib.kvcomm_anchor_predict(weights.data_ptr(), n, lens, A, int(seg_len), float(gamma),
+    lens = _int32s(anchor_len, A, "anchor_len")
+    _check(lib.kvcomm_anchor_predict(weights.data_ptr(), n, lens, A, _int32(seg_len, "seg_len"), float(gamma),
                                      None if entropy_out is None else entropy_out.data_ptr(), result_out.data_ptr(),
                                      workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                      _stream_ptr(stream)))
@@ -583,7 +604,7 @@ def kvcomm_capture_offsets(model, base_k, base_v, real_k, real_v, delta_pos, out
         return out_dk, out_dv
     d = lambda t, what: _desc(t, model.dtype, what)
     _check(lib.kvcomm_capture_offsets(ctypes.byref(model.c()), d(base_k, "base_k"), d(base_v, "base_v"),
-                                      d(real_k, "real_k"), d(real_v, "real_v"), seg_len, int(delta_pos),
+                                      d(real_k, "real_k"), d(real_v, "real_v"), seg_len, _int32(delta_pos, "delta_pos"),
                                       d(out_dk, "out_dk"), d(out_dv, "out_dv"), _stream_ptr(stream)))
     return out_dk, out_dv
 
@@ -594,8 +615,7 @@ def _same_layout(a, b):
 
 def kvcomm_anchor_weights_batch_workspace(model, seg_lens, n_anchors, gran=W_TOKEN, rule=RULE_L2_SOFTMAX):
     n = len(seg_lens)
-    sl = (ctypes.c_int32 * n)(*[int(x) for x in seg_lens])
-    na = (ctypes.c_int32 * n)(*[int(x) for x in n_anchors])
+    sl, na = _int32s(seg_lens, n, "seg_lens"), _int32s(n_anchors, n, "n_anchors")
     return int(load_library().kvcomm_anchor_weights_batch_workspace(ctypes.byref(model.c()), gran, rule, sl, na, n))
 
 
@@ -679,7 +699,7 @@ def _align_kv_batch(model, jobs, units, gran, stream):
         if jd.get("anchor_delta_pos") is not None:
             if len(jd["anchor_delta_pos"]) != A:
                 raise KVCommError(-1, "anchor_delta_pos must have one entry per anchor")
-            adp = (ctypes.c_int32 * max(A, 1))(*[int(x) for x in jd["anchor_delta_pos"]])
+            adp = _int32s(jd["anchor_delta_pos"], A, "anchor_delta_pos")
         w = jd.get("weights")
         S = jd["base_k"].shape[2]
         if A:
@@ -690,13 +710,13 @@ def _align_kv_batch(model, jobs, units, gran, stream):
         keep.append((pk, pv, lens, adp))
         d = lambda t, what: _desc(t, model.dtype, what)
         cjobs[j] = _CAlignJob(d(jd["base_k"], "base_k"), d(jd["base_v"], "base_v"), d(jd["out_k"], "out_k"),
-                              d(jd["out_v"], "out_v"), S, int(jd["delta_pos"]), pk, pv, lens, adp, A,
+                              d(jd["out_v"], "out_v"), S, _int32(jd["delta_pos"], "delta_pos"), pk, pv, lens, adp, A,
                               None if w is None else w.data_ptr(), 0 if (w is None or not A) else w.numel() // A)
     args = (ctypes.byref(model.c()), gran, layout if layout is not None else _CTensor(None, 0, 0, 0), cjobs, n)
     if units is None:
         _check(lib.kvcomm_align_kv_batch(*args, _stream_ptr(stream)))
     else:
-        _check(lib.kvcomm_align_kv_batch_beside(*args, int(units), _stream_ptr(stream)))
+        _check(lib.kvcomm_align_kv_batch_beside(*args, _int32(units, "units"), _stream_ptr(stream)))
 
 
 def _desc_q8(t, what):
@@ -745,8 +765,7 @@ def kvcomm_align_kv_q8(model, base_k, base_v, anchor_dk8, anchor_dv8, scale_k, s
         raise KVCommError(-1, "anchor lists and scales differ in length")
     if A:
         pk, pv, layout = _anchor_ptrs_q8(anchor_dk8, anchor_dv8)
-        lens = (ctypes.c_int32 * A)(*[int(x) for x in (anchor_len if anchor_len is not None
-                                                        else [a.shape[2] for a in anchor_dk8])])
+        lens = _int32s(anchor_len if anchor_len is not None else [a.shape[2] for a in anchor_dk8], A, "anchor_len")
         sk = (ctypes.c_float * A)(*[float(x) for x in scale_k])
         sv = (ctypes.c_float * A)(*[float(x) for x in scale_v])
         if weights is None or weights.dtype != torch.float32 or not weights.is_contiguous():
@@ -757,10 +776,10 @@ def kvcomm_align_kv_q8(model, base_k, base_v, anchor_dk8, anchor_dv8, scale_k, s
         layout, pk, pv, lens, sk, sv = _CTensor(None, 0, 0, 0), None, None, None, None, None
     adp = None
     if anchor_delta_pos is not None:
-        adp = (ctypes.c_int32 * max(A, 1))(*[int(x) for x in anchor_delta_pos])
+        adp = _int32s(anchor_delta_pos, A, "anchor_delta_pos")
     _check(lib.kvcomm_align_kv_q8(ctypes.byref(model.c()), gran, _desc(base_k, model.dtype, "base_k"),
                                   _desc(base_v, model.dtype, "base_v"), seg_len, pk, pv, layout, lens, sk, sv, A,
-                                  None if weights is None else weights.data_ptr(), int(delta_pos), adp,
+                                  None if weights is None else weights.data_ptr(), _int32(delta_pos, "delta_pos"), adp,
                                   _desc(out_k, model.dtype, "out_k"), _desc(out_v, model.dtype, "out_v"),
                                   _stream_ptr(stream)))
     return out_k, out_v
@@ -789,20 +808,20 @@ def kvcomm_align_kv_q8_batch(model, jobs, gran=W_TOKEN, stream=None):
                 raise KVCommError(-1, "all anchors of a batched call must share one layout")
             layout = lay
             al = jd.get("anchor_len")
-            lens = (ctypes.c_int32 * A)(*[int(x) for x in (al if al is not None else [a.shape[2] for a in dk8])])
+            lens = _int32s(al if al is not None else [a.shape[2] for a in dk8], A, "anchor_len")
             sk = (ctypes.c_float * A)(*[float(x) for x in jd["scale_k"]])
             sv = (ctypes.c_float * A)(*[float(x) for x in jd["scale_v"]])
         if jd.get("anchor_delta_pos") is not None:
             if len(jd["anchor_delta_pos"]) != A:
                 raise KVCommError(-1, "anchor_delta_pos must have one entry per anchor")
-            adp = (ctypes.c_int32 * max(A, 1))(*[int(x) for x in jd["anchor_delta_pos"]])
+            adp = _int32s(jd["anchor_delta_pos"], A, "anchor_delta_pos")
         w = jd.get("weights")
         if A and (w is None or w.dtype != torch.float32 or not w.is_contiguous() or w.numel() % A):
             raise KVCommError(-1, "weights: expected a contiguous fp32 device tensor [n, A]")
         keep.append((pk, pv, lens, sk, sv, adp))
         d = lambda t, what: _desc(t, model.dtype, what)
         cjobs[j] = _CAlignQ8Job(d(jd["base_k"], "base_k"), d(jd["base_v"], "base_v"), d(jd["out_k"], "out_k"),
-                                d(jd["out_v"], "out_v"), jd["base_k"].shape[2], int(jd["delta_pos"]), pk, pv, lens, adp,
+                                d(jd["out_v"], "out_v"), jd["base_k"].shape[2], _int32(jd["delta_pos"], "delta_pos"), pk, pv, lens, adp,
                                 sk, sv, A, None if w is None else w.data_ptr(),
                                 0 if (w is None or not A) else w.numel() // A)
     _check(lib.kvcomm_align_kv_q8_batch(ctypes.byref(model.c()), gran,
@@ -853,7 +872,7 @@ def kvcomm_place_qkv(model, q, k, v, first_pos, q_out=None, k_out=None, v_out=No
     if _done(_native.place_qkv(model, q, k, v, first_pos, q_weight, k_weight, norm_eps, q_out, k_out, v_out, stream)):
         return q_out, k_out, v_out
     ins, outs = (q, k, v), (q_out, k_out, v_out)
-    n = next((x.shape[2] for x in ins if x is not None), 0)
+    n = _int32(next((x.shape[2] for x in ins if x is not None), 0), "tokens")
     none = _CTensor(None, 0, 0, 0)
     cin, cout = [none] * 3, [none] * 3
     for i, (x, y, what) in enumerate(zip(ins, outs, "qkv")):
@@ -868,7 +887,7 @@ def kvcomm_place_qkv(model, q, k, v, first_pos, q_out=None, k_out=None, v_out=No
                               tuple(w.shape) not in ((model.head_dim,), (model.n_layers, model.head_dim))):
             raise KVCommError(EINVAL, f"{what}: expected a {model.dtype} device tensor [D] or [L, D] with contiguous channels")
         weights.append((None, 0) if w is None else (w.data_ptr(), w.stride(0) if w.dim() == 2 else 0))
-    _check(lib.kvcomm_place_qkv(ctypes.byref(model.c()), *cin, n, int(first_pos), weights[0][0], weights[1][0], weights[0][1], weights[1][1],
+    _check(lib.kvcomm_place_qkv(ctypes.byref(model.c()), *cin, n, _int32(first_pos, "first_pos"), weights[0][0], weights[1][0], weights[0][1], weights[1][1],
                                 float(norm_eps), *cout, _on_stream_of((*ins, *outs, q_weight, k_weight), stream)))
     return outs
 
@@ -883,6 +902,7 @@ def kvcomm_quantize_kv4(model, k, v, out_k=None, out_v=None, stream=None):
         out_v = _new_compact(model, n, k.device) if out_v is None else out_v
     if _done(_native.quantize_kv4(model, k, v, out_k, out_v, stream)):
         return out_k, out_v
+    _int32(n, "tokens")
     shape = (model.n_layers, model.n_kv_heads, n, model.head_dim)
     _check(lib.kvcomm_quantize_kv4(ctypes.byref(model.c()), _sized(k, model.dtype, shape, "k"), _sized(v, model.dtype, shape, "v"), n,
                                    _compact(model, out_k, n, "out_k"), _compact(model, out_v, n, "out_v"),
@@ -900,6 +920,7 @@ def kvcomm_dequantize_kv4(model, k, v, out_k=None, out_v=None, stream=None):
         out_v = torch.empty(shape, dtype=model.dtype, device=k[0].device) if out_v is None else out_v
     if _done(_native.dequantize_kv4(model, k, v, out_k, out_v, stream)):
         return out_k, out_v
+    _int32(n, "tokens")
     _check(lib.kvcomm_dequantize_kv4(ctypes.byref(model.c()), _compact(model, k, n, "k"), _compact(model, v, n, "v"), n,
                                      _sized(out_k, model.dtype, shape, "out_k"), _sized(out_v, model.dtype, shape, "out_v"),
                                      _on_stream_of((*k, *v, out_k, out_v), stream)))
@@ -907,11 +928,12 @@ def kvcomm_dequantize_kv4(model, k, v, out_k=None, out_v=None, stream=None):
 
 
 def kvcomm_suffix_attn_kv4_workspace(model, n_ctx, tq):
-    return int(load_library().kvcomm_suffix_attn_kv4_workspace(ctypes.byref(model.c()), int(n_ctx), int(tq)))
+    return int(load_library().kvcomm_suffix_attn_kv4_workspace(ctypes.byref(model.c()), _int32(n_ctx, "n_ctx"), _int32(tq, "tq")))
 
 
 def kvcomm_suffix_attn_window_workspace(model, n_ctx, tq, window, n_sinks=0):
-    return int(load_library().kvcomm_suffix_attn_window_workspace(ctypes.byref(model.c()), int(n_ctx), int(tq), int(window), int(n_sinks)))
+    return int(load_library().kvcomm_suffix_attn_window_workspace(ctypes.byref(model.c()), _int32(n_ctx, "n_ctx"), _int32(tq, "tq"),
+                                                                  _at_most_int32(window, "window"), _at_most_int32(n_sinks, "n_sinks")))
 
 
 def _attn_outputs(q, out, lse_out, want_lse, stream):
@@ -925,6 +947,7 @@ def _attn_outputs(q, out, lse_out, want_lse, stream):
 
 def _attn_checked(model, q, out, lse_out, workspace):
     """(descriptor of q, of out, pointer of lse_out, pointer and bytes of workspace) of a call that the native module declined."""
+    _int32(q.shape[2], "tq")
     shape = (model.n_layers, model.n_q_heads, q.shape[2], model.head_dim)
     cq, cout = _sized(q, model.dtype, shape, "q"), _sized(out, model.dtype, shape, "out")
     if lse_out is not None and (lse_out.dtype != torch.float32 or not lse_out.is_cuda or not lse_out.is_contiguous() or
@@ -948,9 +971,10 @@ def kvcomm_suffix_attn_kv4(model, q, cache_k, cache_v, n_ctx, softmax_scale=0.0,
         workspace = _attn_scratch(need, q.device, stream) if need else None
     if not _done(_native.suffix_attn_kv4(model, q, cache_k, cache_v, n_ctx, softmax_scale, out, lse_out, workspace, stream)):
         cq, cout, lse, ws = _attn_checked(model, q, out, lse_out, workspace)
-        N = int(n_ctx) + tq
+        n_ctx = _int32(n_ctx, "n_ctx")
+        N = n_ctx + tq
         _check(lib.kvcomm_suffix_attn_kv4(ctypes.byref(model.c()), cq, _compact(model, cache_k, N, "cache_k"), _compact(model, cache_v, N, "cache_v"),
-                                          int(n_ctx), tq, float(softmax_scale), cout, lse, *ws,
+                                          n_ctx, tq, float(softmax_scale), cout, lse, *ws,
                                           _on_stream_of((q, *cache_k, *cache_v, out, lse_out, workspace), stream)))
     return (out, lse_out) if want_lse else out
 
@@ -969,9 +993,10 @@ def kvcomm_suffix_attn_window(model, q, cache_k, cache_v, n_ctx, window, n_sinks
         workspace = _attn_scratch(need, q.device, stream) if need else None
     if not _done(_native.suffix_attn_window(model, q, cache_k, cache_v, n_ctx, window, n_sinks, softmax_scale, out, lse_out, workspace, stream)):
         cq, cout, lse, ws = _attn_checked(model, q, out, lse_out, workspace)
-        shape = (model.n_layers, model.n_kv_heads, int(n_ctx) + tq, model.head_dim)
+        n_ctx, window, n_sinks = _int32(n_ctx, "n_ctx"), _at_most_int32(window, "window"), _at_most_int32(n_sinks, "n_sinks")
+        shape = (model.n_layers, model.n_kv_heads, n_ctx + tq, model.head_dim)
         _check(lib.kvcomm_suffix_attn_window(ctypes.byref(model.c()), cq, _sized(cache_k, model.dtype, shape, "cache_k"),
-                                             _sized(cache_v, model.dtype, shape, "cache_v"), int(n_ctx), tq, int(window), int(n_sinks),
+                                             _sized(cache_v, model.dtype, shape, "cache_v"), n_ctx, tq, window, n_sinks,
                                              float(softmax_scale), cout, lse, *ws,
                                              _on_stream_of((q, cache_k, cache_v, out, lse_out, workspace), stream)))
     return (out, lse_out) if want_lse else out
