@@ -346,7 +346,11 @@ def suffix_step(model, q, k, v, cache, n_ctx, window=None, n_sinks=0, q_weight=N
         with kv.on_stream(stream):   # what only this step's kernels read belongs to their stream
             placed_q, placed_k, _ = kv.kvcomm_place_qkv(model, q, k, None, n_ctx, stream=stream, **norm)
             cache.append(placed_k, v, stream)
-            return cache.attend(placed_q, out, stream)
+            try:
+                return cache.attend(placed_q, out, stream)
+            except BaseException:   # the step has not been made: one made again finds the cache as it was
+                cache.length = n_ctx
+                raise
     cache_k, cache_v = (t[:, :, :end] for t in cache)
     with kv.on_stream(stream):
         placed_q = kv.kvcomm_place_qkv(model, q, k, v, n_ctx, k_out=cache_k[:, :, n_ctx:], v_out=cache_v[:, :, n_ctx:], stream=stream, **norm)[0]
