@@ -436,7 +436,8 @@ int kvcomm_align_kv_q8_batch(const kvcomm_model *model, int32_t gran, kvcomm_ten
  * another tensor of the call returns KVCOMM_EINVAL (tensors that lie token by token beside each other, as in a projection, are told
  * apart; of others whole (layer, head) blocks are compared, first to last token).
  * Errors: KVCOMM_EINVAL / KVCOMM_EUNSUPPORTED as above; KVCOMM_EINVAL for n_tokens <= 0, positions beyond INT32_MAX,
- * norm_eps negative, infinite or NaN, a weight without a norm or without its tensor.       */
+ * norm_eps negative, infinite or NaN, a weight without a norm or without its tensor.  (norm_eps = 0 means no norm; one without an
+ * eps is asked for with an eps that is lost beside the squares.)                            */
 int kvcomm_place_qkv(const kvcomm_model *model, kvcomm_tensor q, kvcomm_tensor k, kvcomm_tensor v,
                      int32_t n_tokens, int32_t first_pos,
                      const void *q_weight, const void *k_weight, int64_t q_weight_stride, int64_t k_weight_stride,

@@ -873,6 +873,8 @@ def kvcomm_place_qkv(model, q, k, v, first_pos, q_out=None, k_out=None, v_out=No
         return q_out, k_out, v_out
     ins, outs = (q, k, v), (q_out, k_out, v_out)
     n = _int32(next((x.shape[2] for x in ins if x is not None), 0), "tokens")
+    if norm_eps != 0 and ctypes.c_float(float(norm_eps)).value == 0:
+        raise KVCommError(EINVAL, f"norm_eps: {norm_eps} is 0 in fp32, which means no norm")
     none = _CTensor(None, 0, 0, 0)
     cin, cout = [none] * 3, [none] * 3
     for i, (x, y, what) in enumerate(zip(ins, outs, "qkv")):

@@ -615,7 +615,9 @@ PyObject *place_qkv(PyObject *, PyObject *const *args, Py_ssize_t n)
             ws[i] = d == 2 ? t.stride(0) : 0;
         }
         const int32_t first = as_int(a[4]);
-        const float eps = (float)as_double(a[7]);
+        const double norm_eps = as_double(a[7]);
+        const float eps = (float)norm_eps;
+        if (eps == 0.f && norm_eps != 0.0) throw Decline{};   // (would mean no norm)
         void *stream = stream_of(c, a[11]);
         return unlocked([&] {
             return lib.place_qkv(&c.m, in[0], in[1], in[2], (int32_t)tokens, first, w[0], w[1], ws[0], ws[1], eps, out[0], out[1], out[2], stream);
