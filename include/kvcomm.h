@@ -436,7 +436,8 @@ int kvcomm_align_kv_q8_batch(const kvcomm_model *model, int32_t gran, kvcomm_ten
  * another tensor of the call returns KVCOMM_EINVAL (tensors that lie token by token beside each other, as in a projection, are told
  * apart; of others whole (layer, head) blocks are compared, first to last token).
  * Errors: KVCOMM_EINVAL / KVCOMM_EUNSUPPORTED as above; KVCOMM_EINVAL for n_tokens <= 0, positions beyond INT32_MAX,
- * norm_eps negative, infinite or NaN, a weight without a norm or without its tensor.  (norm_eps = 0 means no norm; one without an
+ * norm_eps negative, infinite or NaN, a weight without a norm or without its tensor; KVCOMM_EUNSUPPORTED where a launch would
+ * hold 2^32 threads (from 2^35 values in a tensor on, or 2^24 layers).  (norm_eps = 0 means no norm; one without an
  * eps is asked for with an eps that is lost beside the squares.)                            */
 int kvcomm_place_qkv(const kvcomm_model *model, kvcomm_tensor q, kvcomm_tensor k, kvcomm_tensor v,
                      int32_t n_tokens, int32_t first_pos,
@@ -459,7 +460,8 @@ int kvcomm_place_qkv(const kvcomm_model *model, kvcomm_tensor q, kvcomm_tensor k
  * gets byte 255.  Reproducible bit for bit.
  * kvcomm_dequantize_kv4: the values back, exact in either type (below 2^-126: subnormal).
  * Errors as for kvcomm_capture_offsets; KVCOMM_EINVAL where an output shares bytes with another tensor of the call
- * (compared as in kvcomm_place_qkv: codes and scales, keys and values may lie token by token beside each other).  */
+ * (compared as in kvcomm_place_qkv: codes and scales, keys and values may lie token by token beside each other);
+ * KVCOMM_EUNSUPPORTED for sizes as there.                                                           */
 typedef struct {
     kvcomm_tensor codes, scales;
 } kvcomm_tensor4;
@@ -475,7 +477,8 @@ int kvcomm_dequantize_kv4(const kvcomm_model *model, kvcomm_tensor4 k, kvcomm_te
  * type.  Decoded values are exact in either type; from there on the arithmetic is that of
  * kvcomm_suffix_attn.  lse_out, softmax_scale, workspace (kvcomm_suffix_attn_kv4_workspace() bytes, 16-byte aligned,
  * or none) and errors as there; KVCOMM_EUNSUPPORTED for bf16 models and token strides of 2^26 bytes or more (a tile's rows are addressed by
- * 32-bit offsets).  A key that a query does not see has no influence on it, whatever it holds.        */
+ * 32-bit offsets), for more than 2^30 tokens, and for more rows than a launch holds: fewer than 2^32 threads, of which a long prompt's (layer, query
+ * head, query) rows take two each (f32: 16), those of a few queries 32.  A key that a query does not see has no influence on it, whatever it holds.        */
 size_t kvcomm_suffix_attn_kv4_workspace(const kvcomm_model *model, int32_t n_ctx, int32_t tq);
 
 int kvcomm_suffix_attn_kv4(const kvcomm_model *model, kvcomm_tensor q,
@@ -492,7 +495,7 @@ int kvcomm_suffix_attn_kv4(const kvcomm_model *model, kvcomm_tensor q,
  * rows that no query sees are not looked at, or without influence, whatever they hold: a stream may have dropped them.  Time goes by the
  * keys that are seen, not by the length of the cache.  f32 and bf16, lse_out, softmax_scale, workspace
  * (kvcomm_suffix_attn_window_workspace() bytes, 16-byte aligned, or none) and errors as for kvcomm_suffix_attn; KVCOMM_EINVAL for
- * window <= 0 or n_sinks < 0.                                                              */
+ * window <= 0 or n_sinks < 0; KVCOMM_EUNSUPPORTED for more tokens or rows than kvcomm_suffix_attn_kv4 takes.    */
 size_t kvcomm_suffix_attn_window_workspace(const kvcomm_model *model, int32_t n_ctx, int32_t tq,
                                            int32_t window, int32_t n_sinks);
 

@@ -81,11 +81,13 @@ static inline int attn_cache4(const kvcomm_model &model, const kvcomm_tensor4 &k
     return KVCOMM_OK;
 }
 
-// Tokens of a cache whose tiles the kernels count with 32-bit integers; a launch holds fewer than 2^32 threads, of 512 in a block (at most 16 runs of 16 rows).
-constexpr int64_t kMaxTokens = (int64_t)1 << 30;
-static inline bool fits_a_launch(const AttnParams &p)
+// Tokens of a cache whose tiles, and packed rows, that the kernels count with 32-bit integers; and fewer (layer, kv head, row) triples than a launch
+// holds threads: no kernel has fewer than two for a row.  The plan is made within these bounds; launch_attn() and launch_attn_f32() look at its blocks.
+constexpr int64_t kMaxTokens = (int64_t)1 << 30, kMaxRows = ((int64_t)1 << 31) - 512;
+static inline bool plannable(const kvcomm_model &m, int n_ctx, int tq)
 {
-    return (int64_t)p.n_ctx + p.tq <= kMaxTokens && (double)p.L * p.Hkv * ((double)p.G * p.tq / 16 + 1) < (1 << 23);
+    const int64_t rows = (int64_t)(m.n_q_heads / m.n_kv_heads) * tq;
+    return (int64_t)n_ctx + tq <= kMaxTokens && rows <= kMaxRows && (double)m.n_layers * m.n_kv_heads * (double)rows < 2147483648.0;
 }
 
 }  // namespace kvc

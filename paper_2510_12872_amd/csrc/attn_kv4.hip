@@ -344,7 +344,7 @@ int launch_attn_kv4_rows(const AttnParams &p, int D, unsigned n_blocks, hipStrea
 
 extern "C" size_t kvcomm_suffix_attn_kv4_workspace(const kvcomm_model *model, int32_t n_ctx, int32_t tq)
 {
-    if (check_model(model) || tq <= 0 || n_ctx < 0 || model->dtype != KVCOMM_BF16 || (int64_t)n_ctx + tq > kMaxTokens) return 0;
+    if (check_model(model) || tq <= 0 || n_ctx < 0 || model->dtype != KVCOMM_BF16 || !plannable(*model, n_ctx, tq)) return 0;
     return attn_workspace(*model, plan_kv4(*model, n_ctx, tq, true));
 }
 
@@ -355,7 +355,7 @@ extern "C" int kvcomm_suffix_attn_kv4(const kvcomm_model *model, kvcomm_tensor q
     AttnParams p{};
     int st = attn_params(model, q, n_ctx, tq, softmax_scale, out, lse_out, p);
     if (st || (st = attn_cache4(*model, cache_k, cache_v, p))) return st;
-    if (!fits_a_launch(p)) return KVCOMM_EUNSUPPORTED;
+    if (!plannable(*model, n_ctx, tq)) return KVCOMM_EUNSUPPORTED;
     if (model->dtype == KVCOMM_F32) return launch_f32(p, model->head_dim, attn_f32_groups(*model, tq, 0), 0, static_cast<hipStream_t>(stream));
     // Rows of a 64-key tile are addressed by a 32-bit offset from the first.
     for (const Strides &t : {p.s_k, p.s_v, p.s_ks, p.s_vs})

@@ -18,7 +18,7 @@ void clamp_window(int32_t n_ctx, int32_t tq, int32_t &window, int32_t &n_sinks)
 extern "C" size_t kvcomm_suffix_attn_window_workspace(const kvcomm_model *model, int32_t n_ctx, int32_t tq, int32_t window, int32_t n_sinks)
 {
     if (check_model(model) || tq <= 0 || n_ctx < 0 || window <= 0 || n_sinks < 0 || model->dtype != KVCOMM_BF16) return 0;
-    if ((int64_t)n_ctx + tq > kMaxTokens) return 0;
+    if (!plannable(*model, n_ctx, tq)) return 0;
     clamp_window(n_ctx, tq, window, n_sinks);
     return attn_workspace(*model, attn_plan_window(*model, n_ctx, tq, window, n_sinks, true));
 }
@@ -31,7 +31,7 @@ extern "C" int kvcomm_suffix_attn_window(const kvcomm_model *model, kvcomm_tenso
     int st = attn_params(model, q, n_ctx, tq, softmax_scale, out, lse_out, p);
     if (st || (st = attn_cache(*model, cache_k, cache_v, p))) return st;
     if (window <= 0 || n_sinks < 0) return KVCOMM_EINVAL;
-    if (!fits_a_launch(p)) return KVCOMM_EUNSUPPORTED;
+    if (!plannable(*model, n_ctx, tq)) return KVCOMM_EUNSUPPORTED;
     clamp_window(n_ctx, tq, window, n_sinks);
     p.window = window;
     p.n_sinks = n_sinks;

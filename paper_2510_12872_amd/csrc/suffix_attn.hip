@@ -825,6 +825,10 @@ int launch_attn(const kvcomm_model &m, AttnParams &p, AttnPlan plan, const AttnP
     const int D = m.head_dim;
     const size_t need = attn_workspace(m, plan);
     if (plan.n_splits > 1 && (!workspace || workspace_bytes < need || !aligned16(workspace))) plan = uncut;
+    // A launch holds fewer than 2^32 threads.
+    const int threads = !plan.rows_kernel ? 2 * plan.tile_rows : p.k_scales ? 512 : 64 * rows_waves(D);
+    const double items = (double)p.L * p.Hkv * plan.n_row_tiles * plan.n_splits;
+    if (items > INT32_MAX || ((max_blocks <= 0 || max_blocks >= items) && items * threads >= 4294967296.0)) return KVCOMM_EUNSUPPORTED;
     p.n_row_tiles = plan.n_row_tiles;
     p.n_splits = plan.n_splits;
     p.groups_per_tile = plan.tile_rows / plan.group_rows;
