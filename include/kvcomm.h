@@ -478,7 +478,9 @@ int kvcomm_dequantize_kv4(const kvcomm_model *model, kvcomm_tensor4 k, kvcomm_te
  * kvcomm_suffix_attn.  lse_out, softmax_scale, workspace (kvcomm_suffix_attn_kv4_workspace() bytes, 16-byte aligned,
  * or none) and errors as there; KVCOMM_EUNSUPPORTED for bf16 models and token strides of 2^26 bytes or more (a tile's rows are addressed by
  * 32-bit offsets), for more than 2^30 tokens, and for more rows than a launch holds: fewer than 2^32 threads, of which a long prompt's (layer, query
- * head, query) rows take two each (f32: 16), those of a few queries 32.  A key that a query does not see has no influence on it, whatever it holds.        */
+ * head, query) rows take two each (f32: 16), those of a few queries 32.  A key that a query does not see has no influence on it, whatever it holds;
+ * rows that share a block with one that meets a NaN or an infinity are computed again key by key for that, which takes 7 times (one token, 4000 keys) to
+ * 300 times (512 queries, 32000 keys) as long.  */
 size_t kvcomm_suffix_attn_kv4_workspace(const kvcomm_model *model, int32_t n_ctx, int32_t tq);
 
 int kvcomm_suffix_attn_kv4(const kvcomm_model *model, kvcomm_tensor q,
@@ -492,7 +494,8 @@ int kvcomm_suffix_attn_kv4(const kvcomm_model *model, kvcomm_tensor q,
  * up to its own and to the cache's first n_sinks tokens,
  *   token j is seen  iff  j <= p  and  (j > p - window  or  j < n_sinks).
  * window >= 1 (a query always sees itself; window >= n_ctx + tq is kvcomm_suffix_attn), n_sinks >= 0.  The cache is laid out as there;
- * rows that no query sees are not looked at, or without influence, whatever they hold: a stream may have dropped them.  Time goes by the
+ * rows that no query sees are not looked at, or without influence, whatever they hold: a stream may have dropped them (a NaN or
+ * an infinity that some query sees costs time as in kvcomm_suffix_attn_kv4).  Time goes by the
  * keys that are seen, not by the length of the cache.  f32 and bf16, lse_out, softmax_scale, workspace
  * (kvcomm_suffix_attn_window_workspace() bytes, 16-byte aligned, or none) and errors as for kvcomm_suffix_attn; KVCOMM_EINVAL for
  * window <= 0 or n_sinks < 0; KVCOMM_EUNSUPPORTED for more tokens or rows than kvcomm_suffix_attn_kv4 takes.    */

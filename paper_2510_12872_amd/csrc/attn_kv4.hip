@@ -171,6 +171,8 @@ __global__ __launch_bounds__(512, D == 256 ? 2 : 4) void attn_kv4_rows_kernel(co
             m = m_new;
             mc = m == -INFINITY ? 0.f : m * p.scale_log2;   // a row that sees no key of this run yet: exponentials 0
         }
+        // Probabilities as bf16, which the second product takes: each is off by up to 2^-8 of itself, half a step, and a sum of many by far less, which the
+        // result's own rounding to bf16 exceeds.  Sums stay fp32 and are of the unrounded ones.
         u32x4 pk;
         float rs0 = 0.f, rs1 = 0.f;
 #pragma unroll

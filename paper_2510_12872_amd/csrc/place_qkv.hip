@@ -3,8 +3,8 @@
 // values to their rows of the agent's cache.
 //   x' = x / sqrt(mean_c x_c^2 + eps) * w_c;   out_c = x'_c cos - x'_{c + D/2} sin,   out_{c + D/2} = x'_{c + D/2} cos + x'_c sin,
 // the angle of pair c being position * theta^(-2c/D).  fp32 throughout, one rounding at the store.
-// HBM bound (each value is read and written once: 402 MB of 32 layers x 512 tokens in 63 us, 6.4 TB/s with the last-level cache's help); with a token or two the launch is one
-// chain of load, trigonometry, reduction and store (3.8 us).
+// HBM bound (each value is read and written once: 402 MB of 32 layers x 512 tokens in 75 us, 5.4 TB/s, a copy's rate; 63 us on the same tensors again and again, part of
+// which the last-level cache then holds); with a token or two the launch is one chain of load, trigonometry, reduction and store (2.6 us; 3.6 us from launch to launch).
 // A thread owns the 16 bytes of channels c ... and the 16 bytes of c + D/2 ..., both members of its pairs, and keeps its (token, channels)
 // from head to head: the cosines and sines, in double up to their rounding, are formed once per thread and stay in registers.
 #include <float.h>
@@ -49,7 +49,7 @@ struct PlaceParams {
     double inv_freq[128];
 };
 
-// NORM: eps > 0.  U: heads whose loads a thread has in flight together (two as fast as four: 62.7 and 63.3 us for 32 layers x 512 tokens).
+// NORM: eps > 0.  U: heads whose loads a thread has in flight together (two as fast as four: 62.7 and 63.3 us for 32 layers x 512 tokens, the same ones every time).
 template <typename T, int D, bool NORM, int U>
 __global__ __launch_bounds__(kBlock) void place_kernel(const PlaceParams p)
 {
@@ -165,7 +165,7 @@ int launch_place(PlaceParams &p, int L, hipStream_t s)
     while ((1 << p.log_tokens) < std::min(p.n, rows)) ++p.log_tokens;
     p.n_tiles = (int)(((int64_t)p.n + (1 << p.log_tokens) - 1) >> p.log_tokens);
     const int at_once = rows >> p.log_tokens;
-    // A thread moves four heads, fewer where the launch would have less than half a block per unit.  32 query and 8 kv heads, D = 128, norm, us with 1 / 2 / 4 / 8 / 16
+    // A thread moves four heads, fewer where the launch would have less than half a block per unit.  32 query and 8 kv heads, D = 128, norm, us on the same tensors every time with 1 / 2 / 4 / 8 / 16
     // heads: 32 layers x 512 tokens 84.7 / 65.1 / 62.7 / 64.2 / 68.9, one layer 32 tokens 4.0 / 4.3 / 5.1 / 6.8 / 9.4, 512 tokens 6.1 / 5.9 / 5.9 / 7.6 / 10.1.
     int64_t groups = 0, blocks = 0;
     for (int heads = 4; heads >= 1 && blocks < 128; heads /= 2) {
