@@ -238,7 +238,8 @@ int kvcomm_align_kv_batch_beside(const kvcomm_model *model, int32_t gran, kvcomm
  * use fp32 arithmetic throughout.
  * Errors: KVCOMM_EINVAL for null/misaligned pointers, tq <= 0, n_ctx < 0;
  * KVCOMM_EUNSUPPORTED for bf16 caches whose token stride is D * 2^21 elements or more
- * (the kernel addresses a group of 512 / D rows with a 32-bit byte offset).                 */
+ * (the kernel addresses a group of 512 / D rows with a 32-bit byte offset), and where tokens, the (query head, query) rows of a kv
+ * head, or the threads of a launch do not fit 31 or 32 bits.                                */
 #define KVCOMM_ATTN_MIN_SPLIT_KEYS 512
 
 size_t kvcomm_suffix_attn_workspace(const kvcomm_model *model, int32_t n_ctx, int32_t tq);

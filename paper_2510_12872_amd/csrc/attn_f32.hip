@@ -450,7 +450,9 @@ int launch_attn_f32(const AttnParams &p, int D, unsigned n_blocks, hipStream_t s
 {
     const bool whole = !p.window && !p.k_scales;   // a whole cache of this type
     if (p.N <= f32_row_keys(D) && whole) {
-        const dim3 grid((unsigned)(((int64_t)p.L * p.Hkv * p.G * p.tq + 3) / 4)), block(256);
+        const int64_t blocks = ((int64_t)p.L * p.Hkv * p.G * p.tq + 3) / 4;
+        if (blocks >= 1 << 24) return KVCOMM_EUNSUPPORTED;   // a launch holds fewer than 2^32 threads
+        const dim3 grid((unsigned)blocks), block(256);
         switch (D) {
             case 64: return launch(attn_f32_row_kernel<64>, grid, block, 0, stream, p);
             case 128: return launch(attn_f32_row_kernel<128>, grid, block, 0, stream, p);

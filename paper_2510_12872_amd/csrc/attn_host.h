@@ -24,7 +24,7 @@ static inline int attn_params(const kvcomm_model *model, const kvcomm_tensor &q,
     p.G = model->n_q_heads / model->n_kv_heads;
     p.n_ctx = n_ctx;
     p.tq = tq;
-    p.N = n_ctx + tq;
+    p.N = (int32_t)((int64_t)n_ctx + tq);   // (refused if it does not fit)
     p.scale = softmax_scale > 0.f ? softmax_scale : (float)(1.0 / sqrt((double)model->head_dim));
     p.scale_log2 = (float)((double)p.scale * 1.4426950408889634);
     p.n_splits = 1;
@@ -84,10 +84,12 @@ static inline int attn_cache4(const kvcomm_model &model, const kvcomm_tensor4 &k
 // Tokens of a cache whose tiles, and packed rows, that the kernels count with 32-bit integers; and fewer (layer, kv head, row) triples than a launch
 // holds threads: no kernel has fewer than two for a row.  The plan is made within these bounds; launch_attn() and launch_attn_f32() look at its blocks.
 constexpr int64_t kMaxTokens = (int64_t)1 << 30, kMaxRows = ((int64_t)1 << 31) - 512;
-static inline bool plannable(const kvcomm_model &m, int n_ctx, int tq)
+static inline bool plannable(const kvcomm_model &m, int n_ctx, int tq, int64_t max_tokens = kMaxTokens, double max_all_rows = 2147483648.0)
 {
     const int64_t rows = (int64_t)(m.n_q_heads / m.n_kv_heads) * tq;
-    return (int64_t)n_ctx + tq <= kMaxTokens && rows <= kMaxRows && (double)m.n_layers * m.n_kv_heads * (double)rows < 2147483648.0;
+    return (int64_t)n_ctx + tq <= max_tokens && rows <= kMaxRows && (double)m.n_layers * m.n_kv_heads * (double)rows < max_all_rows;
 }
+// Whole caches: as far as 32-bit tokens and 64-bit plans reach (a confined launch of few blocks may walk any number of items).
+static inline bool plannable_whole(const kvcomm_model &m, int n_ctx, int tq) { return plannable(m, n_ctx, tq, kMaxRows, 1099511627776.0); }
 
 }  // namespace kvc

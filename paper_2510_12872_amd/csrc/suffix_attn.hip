@@ -767,7 +767,7 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
 
 extern "C" size_t kvcomm_suffix_attn_workspace(const kvcomm_model *model, int32_t n_ctx, int32_t tq)
 {
-    if (check_model(model) || tq <= 0 || n_ctx < 0 || model->dtype != KVCOMM_BF16) return 0;
+    if (check_model(model) || tq <= 0 || n_ctx < 0 || model->dtype != KVCOMM_BF16 || !plannable_whole(*model, n_ctx, tq)) return 0;
     return attn_workspace(*model, attn_plan(*model, n_ctx, tq, true));
 }
 
@@ -808,6 +808,7 @@ int suffix_attn(const kvcomm_model *model, kvcomm_tensor q, kvcomm_tensor cache_
     AttnParams p{};
     int st = attn_params(model, q, n_ctx, tq, softmax_scale, out, lse_out, p);
     if (st || (st = attn_cache(*model, cache_k, cache_v, p))) return st;
+    if (!plannable_whole(*model, n_ctx, tq)) return KVCOMM_EUNSUPPORTED;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int D = model->head_dim;
 
