@@ -169,7 +169,8 @@ int kvcomm_anchor_weights_static(const kvcomm_model *model, int32_t gran, float 
  *                      pointer and strides).  Any other sharing of bytes between an output and
  *                      another tensor of the call (the other output, a base tensor, a selected
  *                      anchor's deviations, the weights) returns KVCOMM_EINVAL; the check works
- *                      on the byte runs of whole (layer, head) blocks, first to last token.
+ *                      on the byte runs of whole (layer, head) blocks, first to last token, up to 2^22 of them (whole
+ *                      ranges beyond).
  * n_anchors may be 0 (pure re-positioning; weights may then be NULL).
  * Errors: KVCOMM_EINVAL / KVCOMM_EUNSUPPORTED as above.                                  */
 int kvcomm_align_kv(const kvcomm_model *model, int32_t gran,

@@ -10,6 +10,7 @@
 
 #include <algorithm>
 #include <utility>
+#include <new>
 #include <vector>
 
 #include "kvcomm.h"
@@ -226,10 +227,13 @@ static inline int64_t floor_div(int64_t x, int64_t y)   // y > 0
 }
 
 // Do two tensors touch a common byte?  Exact at the granularity of blocks (gaps between the tokens of one
-// block count as touched).  Cheap when the whole ranges are disjoint, which is the usual case.
+// block count as touched).  Cheap when the whole ranges are disjoint, which is the usual case.  Beyond 2^22 blocks, or where there is no memory
+// to list them, ranges that meet count as touched.
+constexpr int64_t kMaxBlocksTold = (int64_t)1 << 22;
 static inline bool extents_overlap(const Extent &a, const Extent &b)
 {
     if (a.hi() <= b.lo() || b.hi() <= a.lo()) return false;
+    if ((int64_t)a.L * a.H > kMaxBlocksTold || (int64_t)b.L * b.H > kMaxBlocksTold) return true;
     if (a.sl == b.sl && a.sh == b.sh && a.L == b.L && a.H == b.H) {
         // Views of one allocation: block (l, h) of a meets block (l + dl, h + dh) of b iff the distance of their
         // first bytes, d0 + dl * sl + dh * sh, lies in (-run_b, run_a); only the index differences matter.  The axis with
@@ -253,7 +257,13 @@ static inline bool extents_overlap(const Extent &a, const Extent &b)
         return false;
     }
     std::vector<std::pair<uintptr_t, uintptr_t>> blocks;
-    blocks.reserve((size_t)a.L * a.H);
+    std::vector<uintptr_t> max_end;
+    try {
+        blocks.reserve((size_t)a.L * a.H);
+        max_end.resize((size_t)a.L * a.H);
+    } catch (const std::bad_alloc &) {
+        return true;
+    }
     for (int l = 0; l < a.L; ++l)
         for (int h = 0; h < a.H; ++h) {
             const uintptr_t lo = a.base + (uintptr_t)(l * a.sl + h * a.sh);
@@ -261,7 +271,6 @@ static inline bool extents_overlap(const Extent &a, const Extent &b)
         }
     std::sort(blocks.begin(), blocks.end());
     uintptr_t reach = 0;   // running maximum of the ends, so that nested blocks are handled too
-    std::vector<uintptr_t> max_end(blocks.size());
     for (size_t i = 0; i < blocks.size(); ++i) {
         reach = std::max(reach, blocks[i].second);
         max_end[i] = reach;
