@@ -510,6 +510,86 @@ int kvcomm_suffix_attn_window(const kvcomm_model *model, kvcomm_tensor q,
                               kvcomm_tensor out, float *lse_out,
                               void *workspace, size_t workspace_bytes, void *stream);
 
+/* --------------------------------------------------------------------------------------
+ * A batch of sequences whose keys and values lie in the pages of one pool: several answers to one assembled cache, agents of different
+ * lengths decoded together.  A pool [L, Hkv, n_pages, page_size, D] is described by its five axes' strides, in any order; token t of
+ * sequence b lies in slot t % page_size of page table[b * table_stride + t / page_size].  What changes from step to step lies in DEVICE memory (so that a captured
+ * graph sees it change), what bounds it in the structure:
+ *   table        DEVICE int32, table_width entries of each sequence.  An entry outside [0, n_pages) is no page: its tokens are not there.
+ *   lens         DEVICE int32 [n_seqs]: tokens of each sequence, its new ones included (less than 0 counts as 0).
+ *   starts       DEVICE int32 [n_seqs + 1], not decreasing, or NULL: rows starts[b] ... starts[b + 1] - 1 of the queries are sequence b's
+ *                new tokens, its last ones.  Rows before starts[0] and from starts[n_seqs] on belong to no sequence and stay as they were.
+ *                NULL: one row each (n_rows == n_seqs), a decoded token.
+ *   max_rows     about the most rows that a sequence has, 0: not known.  For the choice of a kernel only: results are right whatever it says.
+ * Row i of the n_b rows of sequence b is its token lens[b] - n_b + i.  Whatever table, lens and starts hold, nothing outside the described tensors
+ * is read or written; where starts decreases, which rows are written is not defined.
+ * Limits: page_size a power of two, 16 ... 65536 (KVCOMM_EUNSUPPORTED else); 1 <= n_seqs <= KVCOMM_MAX_SEQS; n_rows >= 1; table_width * page_size <= 2^30;
+ * table_width = 0 or n_pages = 0: no sequence has tokens in pages (the pools' pointers are then ignored).                     */
+#define KVCOMM_MAX_SEQS 8192
+
+typedef struct {
+    void *ptr;             /* device pointer to element (layer 0, head 0, page 0, slot 0, channel 0) */
+    int64_t stride_layer;  /* in elements; pointer and strides aligned like a kvcomm_tensor's */
+    int64_t stride_head;
+    int64_t stride_page;
+    int64_t stride_token;
+} kvcomm_pages;
+
+typedef struct {
+    const int32_t *table;
+    const int32_t *lens;
+    const int32_t *starts;
+    int64_t table_stride;  /* entries from one sequence's to the next's */
+    int32_t table_width;
+    int32_t n_seqs;
+    int32_t n_rows;        /* rows of the queries, of all sequences and none */
+    int32_t page_size;
+    int32_t n_pages;
+    int32_t max_rows;
+} kvcomm_batch;
+
+/* kvcomm_place_qkv for the new tokens of a batch (workflow step 4): token t of a sequence stands at position first_pos + t, its query goes to its row of
+ * q_out, its key and value to its slot of the pages.
+ *   q, q_out             [L, Hq, n_rows, D]; k, v [L, Hkv, n_rows, D].  Pairs (q, q_out), (k, pages_k), (v, pages_v) as in kvcomm_place_qkv: one whose pointers
+ *                        are NULL is left out; weights, norm and arithmetic as there, results bit for bit.
+ *   first_pos            position of a sequence's token 0: the length of the cache that the sequences continue, or 0.
+ * A token that has no page (or lies before its sequence's first, lens[b] < n_b) is not stored; its query is placed.  Slots that no new token has stay as
+ * they were.  A slot that two new tokens share holds one of them.
+ * q_out may be exactly q; any other sharing of bytes between an output and another tensor of the call returns KVCOMM_EINVAL (pools of one shape may lie
+ * interleaved in any order, other tensors are compared by whole ranges).  Other errors as for kvcomm_place_qkv; KVCOMM_EINVAL for a batch whose pointers are missing
+ * or not 4-byte aligned, whose sizes are not positive or whose positions leave 32 bits.                                                                     */
+int kvcomm_place_qkv_paged(const kvcomm_model *model, kvcomm_tensor q, kvcomm_tensor k, kvcomm_tensor v, const kvcomm_batch *batch,
+                           int32_t first_pos, const void *q_weight, const void *k_weight, int64_t q_weight_stride,
+                           int64_t k_weight_stride, float norm_eps, kvcomm_tensor q_out, kvcomm_pages pages_k, kvcomm_pages pages_v,
+                           void *stream);
+
+/* Causal attention of a batch over its pages: row i of sequence b sees the tokens 0 ... lens[b] - n_b + i that are there.
+ *   q, out       [L, Hq, n_rows, D];  lse_out  DEVICE [L, Hq, n_rows] fp32 or NULL.  A row that sees nothing: output 0, log-sum-exp -infinity.
+ *   workspace    DEVICE scratch of kvcomm_paged_attn_workspace() bytes, 16-byte aligned, or NULL: with it the keys of a sequence are shared out over
+ *                several thread blocks where there are few rows.  Without it (NULL, too small or misaligned) the same result up to rounding, only slower.
+ *                Its contents do not matter before the call and are undefined afterwards.
+ * Types, arithmetic and softmax_scale as for kvcomm_suffix_attn; a key that a row does not see has no influence on it, whatever it holds (blocks that meet a NaN, an infinity
+ * or an entry that is no page are computed again key by key, as in kvcomm_suffix_attn_kv4).  Reproducible: no atomics; a row's sums depend on lens and starts
+ * of the whole batch, by the cut of the keys.
+ * Errors: KVCOMM_EINVAL / KVCOMM_EUNSUPPORTED as above; KVCOMM_EUNSUPPORTED for token strides as in kvcomm_suffix_attn and where the rows or the
+ * launch's threads do not fit 31 or 32 bits.                                                            */
+size_t kvcomm_paged_attn_workspace(const kvcomm_model *model, const kvcomm_batch *batch);
+
+int kvcomm_paged_attn(const kvcomm_model *model, kvcomm_tensor q, kvcomm_pages pages_k, kvcomm_pages pages_v,
+                      const kvcomm_batch *batch, float softmax_scale, kvcomm_tensor out, float *lse_out,
+                      void *workspace, size_t workspace_bytes, void *stream);
+
+/* kvcomm_paged_attn of a batch whose sequences all continue one cache: every row sees the n_prefix >= 1 tokens of prefix_k / prefix_v [L, Hkv, n_prefix, D]
+ * (an agent's assembled cache) and the tokens of its own pages up to its own.  The scores with the prefix are formed for the rows of all
+ * sequences together, so its keys and values are read once for the batch and not once per sequence.  Everything else as there; without a
+ * workspace they are read per sequence.                                                                  */
+size_t kvcomm_paged_attn_prefix_workspace(const kvcomm_model *model, int32_t n_prefix, const kvcomm_batch *batch);
+
+int kvcomm_paged_attn_prefix(const kvcomm_model *model, kvcomm_tensor q, kvcomm_tensor prefix_k, kvcomm_tensor prefix_v,
+                             int32_t n_prefix, kvcomm_pages pages_k, kvcomm_pages pages_v, const kvcomm_batch *batch,
+                             float softmax_scale, kvcomm_tensor out, float *lse_out, void *workspace, size_t workspace_bytes,
+                             void *stream);
+
 /* Human-readable name of a kvcomm_status; never NULL. */
 const char *kvcomm_status_string(int status);
 

@@ -15,6 +15,7 @@ import os
 import sys
 import warnings
 from dataclasses import dataclass
+from typing import Optional
 
 import torch
 
@@ -58,6 +59,17 @@ class _CTensor4(ctypes.Structure):
     _fields_ = [("codes", _CTensor), ("scales", _CTensor)]
 
 
+class _CPages(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("stride_layer", ctypes.c_int64), ("stride_head", ctypes.c_int64),
+                ("stride_page", ctypes.c_int64), ("stride_token", ctypes.c_int64)]
+
+
+class _CBatch(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("starts", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+                ("table_width", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("max_rows", ctypes.c_int32)]
+
+
 class _CAlignJob(ctypes.Structure):
     _fields_ = [("base_k", _CTensor), ("base_v", _CTensor), ("out_k", _CTensor), ("out_v", _CTensor),
                 ("seg_len", ctypes.c_int32), ("delta_pos", ctypes.c_int32),
@@ -97,6 +109,17 @@ class Model:
             raise KVCommError(-2, f"unsupported dtype {self.dtype}")
         return _CModel(self.n_layers, self.n_kv_heads, self.n_q_heads, self.head_dim, _DTYPES[self.dtype],
                        float(self.rope_theta))
+
+
+@dataclass(frozen=True)
+class Batch:
+    """Sequences whose keys and values lie in the pages of a pool (kvcomm_batch of the C header), as int32 device tensors: table [B, W] the pages of
+    each, lens [B] its tokens, the new ones included, starts [B + 1] its rows of the queries (None: one row each); max_rows: about
+    the most rows of a sequence, 0: not known.  What the tensors hold is read when a call's kernels run, so a captured graph follows its changes."""
+    table: torch.Tensor
+    lens: torch.Tensor
+    starts: Optional[torch.Tensor] = None
+    max_rows: int = 0
 
 
 _lib = None
@@ -219,6 +242,17 @@ def load_library():
     lib.kvcomm_suffix_attn_window_workspace.restype = sz
     lib.kvcomm_suffix_attn_window.argtypes = [mp, _CTensor, _CTensor, _CTensor, i32, i32, i32, i32, f32, _CTensor, vp, vp, sz, vp]
     lib.kvcomm_suffix_attn_window.restype = ctypes.c_int
+    bp = ctypes.POINTER(_CBatch)
+    lib.kvcomm_place_qkv_paged.argtypes = [mp, _CTensor, _CTensor, _CTensor, bp, i32, vp, vp, i64, i64, f32, _CTensor, _CPages, _CPages, vp]
+    lib.kvcomm_place_qkv_paged.restype = ctypes.c_int
+    lib.kvcomm_paged_attn_workspace.argtypes = [mp, bp]
+    lib.kvcomm_paged_attn_workspace.restype = sz
+    lib.kvcomm_paged_attn.argtypes = [mp, _CTensor, _CPages, _CPages, bp, f32, _CTensor, vp, vp, sz, vp]
+    lib.kvcomm_paged_attn.restype = ctypes.c_int
+    lib.kvcomm_paged_attn_prefix_workspace.argtypes = [mp, i32, bp]
+    lib.kvcomm_paged_attn_prefix_workspace.restype = sz
+    lib.kvcomm_paged_attn_prefix.argtypes = [mp, _CTensor, _CTensor, _CTensor, i32, _CPages, _CPages, bp, f32, _CTensor, vp, vp, sz, vp]
+    lib.kvcomm_paged_attn_prefix.restype = ctypes.c_int
     lib.kvcomm_status_string.argtypes = [ctypes.c_int]
     lib.kvcomm_status_string.restype = ctypes.c_char_p
     lib.kvcomm_version.argtypes = []
@@ -860,6 +894,19 @@ def _new_compact(model, n, device):
             torch.empty(head + (model.head_dim // 32,), dtype=torch.uint8, device=device))
 
 
+def _norm_weights(model, q_weight, k_weight, norm_eps):
+    """(pointer, elements from layer to layer) of the weights of queries and keys."""
+    if norm_eps != 0 and ctypes.c_float(float(norm_eps)).value == 0:
+        raise KVCommError(EINVAL, f"norm_eps: {norm_eps} is 0 in fp32, which means no norm")
+    weights = []
+    for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None and (w.dtype != model.dtype or not w.is_cuda or w.stride(-1) != 1 or
+                              tuple(w.shape) not in ((model.head_dim,), (model.n_layers, model.head_dim))):
+            raise KVCommError(EINVAL, f"{what}: expected a {model.dtype} device tensor [D] or [L, D] with contiguous channels")
+        weights.append((None, 0) if w is None else (w.data_ptr(), w.stride(0) if w.dim() == 2 else 0))
+    return weights
+
+
 def kvcomm_place_qkv(model, q, k, v, first_pos, q_out=None, k_out=None, v_out=None, q_weight=None, k_weight=None, norm_eps=0.0, stream=None):
     """Projections of a suffix q [L,Hq,n,D], k, v [L,Hkv,n,D] -> (q_out, k_out, v_out): per-head RMS norm of q and k where norm_eps > 0 (times
     q_weight, k_weight [D] or [L, D]), rotation of token i to position first_pos + i, v copied.  k_out and v_out are normally views of the agent's
@@ -873,8 +920,6 @@ def kvcomm_place_qkv(model, q, k, v, first_pos, q_out=None, k_out=None, v_out=No
         return q_out, k_out, v_out
     ins, outs = (q, k, v), (q_out, k_out, v_out)
     n = _int32(next((x.shape[2] for x in ins if x is not None), 0), "tokens")
-    if norm_eps != 0 and ctypes.c_float(float(norm_eps)).value == 0:
-        raise KVCommError(EINVAL, f"norm_eps: {norm_eps} is 0 in fp32, which means no norm")
     none = _CTensor(None, 0, 0, 0)
     cin, cout = [none] * 3, [none] * 3
     for i, (x, y, what) in enumerate(zip(ins, outs, "qkv")):
@@ -883,12 +928,7 @@ def kvcomm_place_qkv(model, q, k, v, first_pos, q_out=None, k_out=None, v_out=No
         if x is not None:
             shape = (model.n_layers, model.n_kv_heads if i else model.n_q_heads, n, model.head_dim)
             cin[i], cout[i] = _sized(x, model.dtype, shape, what), _sized(y, model.dtype, shape, what + "_out")
-    weights = []
-    for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if w is not None and (w.dtype != model.dtype or not w.is_cuda or w.stride(-1) != 1 or
-                              tuple(w.shape) not in ((model.head_dim,), (model.n_layers, model.head_dim))):
-            raise KVCommError(EINVAL, f"{what}: expected a {model.dtype} device tensor [D] or [L, D] with contiguous channels")
-        weights.append((None, 0) if w is None else (w.data_ptr(), w.stride(0) if w.dim() == 2 else 0))
+    weights = _norm_weights(model, q_weight, k_weight, norm_eps)
     _check(lib.kvcomm_place_qkv(ctypes.byref(model.c()), *cin, n, _int32(first_pos, "first_pos"), weights[0][0], weights[1][0], weights[0][1], weights[1][1],
                                 float(norm_eps), *cout, _on_stream_of((*ins, *outs, q_weight, k_weight), stream)))
     return outs
@@ -1002,3 +1042,128 @@ def kvcomm_suffix_attn_window(model, q, cache_k, cache_v, n_ctx, window, n_sinks
                                              float(softmax_scale), cout, lse, *ws,
                                              _on_stream_of((q, cache_k, cache_v, out, lse_out, workspace), stream)))
     return (out, lse_out) if want_lse else out
+
+
+def _int32_tensor(t, dim, what):
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or t.dim() != dim or not t.is_cuda or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise KVCommError(EINVAL, f"{what}: expected a {dim}-d int32 device tensor, contiguous along its last axis")
+    return t
+
+
+def _batch(batch, n_rows, page_size, n_pages):
+    """kvcomm_batch of a batch over a pool of these pages."""
+    table, lens = _int32_tensor(batch.table, 2, "table"), _int32_tensor(batch.lens, 1, "lens")
+    B, starts = lens.shape[0], batch.starts
+    if table.shape[0] != B:
+        raise KVCommError(EINVAL, f"table: {table.shape[0]} rows for {B} sequences")
+    if starts is not None and _int32_tensor(starts, 1, "starts").shape[0] != B + 1:
+        raise KVCommError(EINVAL, f"starts: expected {B + 1} entries, not {starts.shape[0]}")
+    return _CBatch(table.data_ptr() or None, lens.data_ptr() or None, None if starts is None else starts.data_ptr(), table.stride(0) if B > 1 else 0,
+                   _int32(table.shape[1], "table"), _int32(B, "sequences"), _int32(n_rows, "rows"), _int32(page_size, "page_size"), _int32(n_pages, "pages"),
+                   _int32(batch.max_rows, "max_rows"))
+
+
+def _pool(model, t, pages, what):
+    """Descriptor of a pool of `pages` = (pages, slots), None: any."""
+    if t.dtype != model.dtype or t.dim() != 5 or not t.is_cuda or t.stride(4) != 1:
+        raise KVCommError(EINVAL, f"{what}: expected a 5-d {model.dtype} device tensor [L, Hkv, pages, slots, D] with contiguous channels")
+    shape = (model.n_layers, model.n_kv_heads, *(tuple(t.shape[2:4]) if pages is None else pages), model.head_dim)
+    if tuple(t.shape) != shape:
+        raise KVCommError(EINVAL, f"{what}: expected shape {shape}, not {tuple(t.shape)}")
+    return _CPages(t.data_ptr() or None, *t.stride()[:4])
+
+
+def kvcomm_place_qkv_paged(model, q, k, v, batch, pages_k, pages_v, first_pos=0, q_out=None, q_weight=None, k_weight=None, norm_eps=0.0, stream=None):
+    """kvcomm_place_qkv for the new tokens of a batch: q [L,Hq,n,D] -> q_out (made if not passed, and returned), k, v [L,Hkv,n,D] -> their slots of
+    the pools pages_k, pages_v [L,Hkv,pages,slots,D].  Token t of a sequence stands at position first_pos + t.  None in the place of q, or of k and its
+    pool, or of v and its pool leaves it out (the batch's pages are then those of the other pool)."""
+    lib = load_library()
+    if q_out is None and q is not None:
+        with on_stream(stream):
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            if batch.starts is not None:   # rows of no sequence stay as they were: zeros
+                q_out.zero_()
+    n = _int32(next((x.shape[2] for x in (q, k, v) if x is not None), 0), "rows")
+    pool = pages_k if pages_k is not None else pages_v
+    none, no_pages = _CTensor(None, 0, 0, 0), _CPages(None, 0, 0, 0, 0)
+    pages = None if pool is None else tuple(pool.shape[2:4])
+    if pages is not None and len(pages) != 2:
+        raise KVCommError(EINVAL, "pages_k / pages_v: expected 5-d device tensors [L, Hkv, pages, slots, D]")
+    cin, cpool, cout = [none] * 3, [no_pages] * 2, none
+    for i, (x, y, what) in enumerate(((q, q_out, "q"), (k, pages_k, "k"), (v, pages_v, "v"))):
+        if (x is None) != (y is None):
+            raise KVCommError(EINVAL, f"{what} without its place" if y is None else f"a place without {what}")
+        if x is None:
+            continue
+        shape = (model.n_layers, model.n_kv_heads if i else model.n_q_heads, n, model.head_dim)
+        cin[i] = _sized(x, model.dtype, shape, what)
+        if i:
+            cpool[i - 1] = _pool(model, y, pages, "pages_" + what)
+        else:
+            cout = _sized(y, model.dtype, shape, "q_out")
+    cbatch = _batch(batch, n, 16 if pages is None else pages[1], 0 if pages is None else pages[0])
+    weights = _norm_weights(model, q_weight, k_weight, norm_eps)
+    _check(lib.kvcomm_place_qkv_paged(ctypes.byref(model.c()), *cin, ctypes.byref(cbatch), _int32(first_pos, "first_pos"), weights[0][0], weights[1][0],
+                                      weights[0][1], weights[1][1], float(norm_eps), cout, *cpool,
+                                      _on_stream_of((q, k, v, q_out, pages_k, pages_v, q_weight, k_weight, batch.table, batch.lens, batch.starts), stream)))
+    return q_out
+
+
+def _pages_of(model, pages_k, pages_v):
+    ck = _pool(model, pages_k, None, "pages_k")
+    return ck, _pool(model, pages_v, tuple(pages_k.shape[2:4]), "pages_v")
+
+
+def kvcomm_paged_attn_workspace(model, n_rows, page_size, n_pages, batch):
+    return int(load_library().kvcomm_paged_attn_workspace(ctypes.byref(model.c()), ctypes.byref(_batch(batch, n_rows, page_size, n_pages))))
+
+
+def kvcomm_paged_attn_prefix_workspace(model, n_prefix, n_rows, page_size, n_pages, batch):
+    return int(load_library().kvcomm_paged_attn_prefix_workspace(ctypes.byref(model.c()), _int32(n_prefix, "n_prefix"),
+                                                                 ctypes.byref(_batch(batch, n_rows, page_size, n_pages))))
+
+
+def _paged_attn(model, q, prefix_k, prefix_v, pages_k, pages_v, batch, softmax_scale, out, lse_out, want_lse, stream, workspace):
+    """Both attention calls; prefix_k None: without a prefix."""
+    lib = load_library()
+    if out is None or (want_lse and lse_out is None):
+        made = out is None, lse_out is None
+        out, lse_out = _attn_outputs(q, out, lse_out, want_lse, stream)
+        if batch.starts is not None:   # rows of no sequence stay as they were: zeros
+            with on_stream(stream):
+                for t, new in zip((out, lse_out), made):
+                    if new and t is not None:
+                        t.zero_()
+    ck, cv = _pages_of(model, pages_k, pages_v)
+    n = _int32(q.shape[2], "rows")
+    cbatch, cmodel = _batch(batch, n, pages_k.shape[3], pages_k.shape[2]), model.c()
+    prefix = ()
+    if prefix_k is not None:
+        shape = (model.n_layers, model.n_kv_heads, prefix_k.shape[2], model.head_dim)
+        prefix = (_sized(prefix_k, model.dtype, shape, "prefix_k"), _sized(prefix_v, model.dtype, shape, "prefix_v"), _int32(shape[2], "n_prefix"))
+    if workspace is None:
+        need = (lib.kvcomm_paged_attn_prefix_workspace(ctypes.byref(cmodel), prefix[2], ctypes.byref(cbatch)) if prefix else
+                lib.kvcomm_paged_attn_workspace(ctypes.byref(cmodel), ctypes.byref(cbatch)))
+        workspace = _attn_scratch(need, q.device, stream) if need else None
+    cq, cout, lse, ws = _attn_checked(model, q, out, lse_out, workspace)
+    call = lib.kvcomm_paged_attn_prefix if prefix else lib.kvcomm_paged_attn
+    _check(call(ctypes.byref(cmodel), cq, *prefix, ck, cv, ctypes.byref(cbatch), float(softmax_scale), cout, lse, *ws,
+                _on_stream_of((q, prefix_k, prefix_v, pages_k, pages_v, out, lse_out, workspace, batch.table, batch.lens, batch.starts), stream)))
+    return (out, lse_out) if want_lse else out
+
+
+def kvcomm_paged_attn(model, q, pages_k, pages_v, batch, softmax_scale=0.0, out=None, lse_out=None, want_lse=False, stream=None, workspace=None):
+    """Causal attention of a batch's new tokens q [L,Hq,n,D] over their sequences' pages, pools [L,Hkv,pages,slots,D].
+
+    workspace: kvcomm_paged_attn_workspace() bytes on the device (made here if not given)."""
+    return _paged_attn(model, q, None, None, pages_k, pages_v, batch, softmax_scale, out, lse_out, want_lse, stream, workspace)
+
+
+def kvcomm_paged_attn_prefix(model, q, prefix_k, prefix_v, pages_k, pages_v, batch, softmax_scale=0.0, out=None, lse_out=None, want_lse=False,
+                             stream=None, workspace=None):
+    """kvcomm_paged_attn of sequences that all continue the tokens prefix_k, prefix_v [L,Hkv,n_prefix,D], which every row sees.
+
+    workspace: kvcomm_paged_attn_prefix_workspace() bytes on the device (made here if not given)."""
+    if prefix_k is None or prefix_v is None:
+        raise KVCommError(EINVAL, "prefix_k, prefix_v: a batch without a prefix goes through kvcomm_paged_attn")
+    return _paged_attn(model, q, prefix_k, prefix_v, pages_k, pages_v, batch, softmax_scale, out, lse_out, want_lse, stream, workspace)

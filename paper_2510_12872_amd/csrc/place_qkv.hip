@@ -7,11 +7,12 @@
 // which the last-level cache then holds); with a token or two the launch is one chain of load, trigonometry, reduction and store (2.6 us; 3.6 us from launch to launch).
 // A thread owns the 16 bytes of channels c ... and the 16 bytes of c + D/2 ..., both members of its pairs, and keeps its (token, channels)
 // from head to head: the cosines and sines, in double up to their rounding, are formed once per thread and stay in registers.
+// kvcomm_place_qkv_paged: the same kernel for the rows of a batch; a row's sequence, position and slot are found while its values travel.
 #include <float.h>
 
 #include <type_traits>
 
-#include "kvcomm_device.h"
+#include "paged.h"
 
 namespace {
 
@@ -49,10 +50,17 @@ struct PlaceParams {
     double inv_freq[128];
 };
 
+// Of a batch: outs of keys and values are pools, their strides those of a slot.
+struct PagedPlaceParams : PlaceParams {
+    Batch batch;
+    int64_t page[2];   // from page to page
+};
+
 // NORM: eps > 0.  U: heads whose loads a thread has in flight together (two as fast as four: 62.7 and 63.3 us for 32 layers x 512 tokens, the same ones every time).
-template <typename T, int D, bool NORM, int U>
-__global__ __launch_bounds__(kBlock) void place_kernel(const PlaceParams p)
+template <typename T, int D, bool NORM, int U, class P>
+__global__ __launch_bounds__(kBlock) void place_kernel(const P p)
 {
+    constexpr bool PAGED = std::is_same_v<P, PagedPlaceParams>;
     constexpr int EPV = Elem<T>::EPV, LPR = D / 2 / EPV;   // channels of a 16-byte piece, lanes of a row
     const int c = threadIdx.x % LPR, slot = threadIdx.x / LPR;
     double freq[EPV];   // the arguments lie in memory that no cache holds yet: all that is needed of them is requested first (one token 3.8 -> 3.6 us)
@@ -67,7 +75,7 @@ __global__ __launch_bounds__(kBlock) void place_kernel(const PlaceParams p)
     const int end = min(head0 + p.heads_per_group, p.heads[which]);
     const int t = (tile << p.log_tokens) + (slot & ((1 << p.log_tokens) - 1));
     const int step = (kBlock / LPR) >> p.log_tokens;       // heads that the block moves at once
-    const bool live = t < p.n;
+    bool live = t < p.n;
     const int tt = min(t, p.n - 1);
     int head = head0 + (slot >> p.log_tokens);
     const int64_t in_head = p.s_in[which].head, out_head = p.s_out[which].head;
@@ -89,6 +97,21 @@ __global__ __launch_bounds__(kBlock) void place_kernel(const PlaceParams p)
         }
     };
     load(head);
+    int pos = p.first_pos + tt;
+    if constexpr (PAGED) {
+        const int b = sequence_of(p.batch, tt, threadIdx.x & 63), bb = max(b, 0);
+        int first, n;
+        sequence_rows(p.batch, bb, first, n);
+        const int i = tt - first, token = sequence_len(p.batch, bb) - n + i;
+        live &= b >= 0 && i >= 0 && i < n;
+        pos = (int)max((int64_t)INT32_MIN, min((int64_t)INT32_MAX, (int64_t)p.first_pos + token));   // (beyond: in no page)
+        if (which) {
+            const int page = live && token >= 0 ? page_of(p.batch, bb, token) : -1;
+            live &= page >= 0;
+            const int slot = token & ((1 << p.batch.log_page) - 1);
+            dst += (live ? (int64_t)page * p.page[which - 1] + (int64_t)slot * p.s_out[which].token : 0) - (int64_t)tt * p.s_out[which].token;
+        }
+    }
     if (which == 2) {
         while (true) {
 #pragma unroll
@@ -109,7 +132,7 @@ __global__ __launch_bounds__(kBlock) void place_kernel(const PlaceParams p)
     float co[EPV], si[EPV];
 #pragma unroll
     for (int i = 0; i < EPV; ++i) {
-        const float2 cs = rope_cos_sin(p.first_pos + tt, freq[i]);
+        const float2 cs = rope_cos_sin(pos, freq[i]);
         co[i] = cs.x;
         si[i] = cs.y;
     }
@@ -157,8 +180,8 @@ __global__ __launch_bounds__(kBlock) void place_kernel(const PlaceParams p)
     }
 }
 
-template <typename T, int D>
-int launch_place(PlaceParams &p, int L, hipStream_t s)
+template <typename T, int D, class P>
+int launch_place(P &p, int L, hipStream_t s)
 {
     constexpr int rows = kBlock / (D / 2 / Elem<T>::EPV);   // of a block at once
     p.log_tokens = 0;
@@ -177,9 +200,20 @@ int launch_place(PlaceParams &p, int L, hipStream_t s)
     if (blocks >= 1 << 24) return KVCOMM_EUNSUPPORTED;   // a launch holds fewer than 2^32 threads along an axis
     p.by_tiles = make_divisor((uint32_t)p.n_tiles);
     p.by_groups = make_divisor((uint32_t)groups);
-    const auto one = p.eps > 0.f ? place_kernel<T, D, true, 1> : place_kernel<T, D, false, 1>;
-    const auto two = p.eps > 0.f ? place_kernel<T, D, true, 2> : place_kernel<T, D, false, 2>;
+    const auto one = p.eps > 0.f ? place_kernel<T, D, true, 1, P> : place_kernel<T, D, false, 1, P>;
+    const auto two = p.eps > 0.f ? place_kernel<T, D, true, 2, P> : place_kernel<T, D, false, 2, P>;
     return launch(p.heads_per_group == at_once ? one : two, dim3((unsigned)blocks), dim3(kBlock), 0, s, p);
+}
+
+template <class P>
+int launch_place(const kvcomm_model &m, P &p, hipStream_t s)
+{
+    const bool f32 = m.dtype == KVCOMM_F32;
+    switch (m.head_dim) {
+        case 64: return f32 ? launch_place<float, 64>(p, m.n_layers, s) : launch_place<bf16_t, 64>(p, m.n_layers, s);
+        case 128: return f32 ? launch_place<float, 128>(p, m.n_layers, s) : launch_place<bf16_t, 128>(p, m.n_layers, s);
+        default: return f32 ? launch_place<float, 256>(p, m.n_layers, s) : launch_place<bf16_t, 256>(p, m.n_layers, s);
+    }
 }
 
 }  // namespace
@@ -236,11 +270,137 @@ extern "C" int kvcomm_place_qkv(const kvcomm_model *model, kvcomm_tensor q, kvco
     p.first_pos = first_pos;
     p.eps = norm_eps;
     fill_inv_freq(p.inv_freq, model->rope_theta, D);
-    hipStream_t s = static_cast<hipStream_t>(stream);
-    const bool f32 = dt == KVCOMM_F32;
-    switch (D) {
-        case 64: return f32 ? launch_place<float, 64>(p, L, s) : launch_place<bf16_t, 64>(p, L, s);
-        case 128: return f32 ? launch_place<float, 128>(p, L, s) : launch_place<bf16_t, 128>(p, L, s);
-        default: return f32 ? launch_place<float, 256>(p, L, s) : launch_place<bf16_t, 256>(p, L, s);
+    return launch_place(*model, p, static_cast<hipStream_t>(stream));
+}
+
+namespace {
+
+// A pool as the caller described it: four axes of rows of `row` bytes, strides in bytes.
+struct PoolExtent {
+    uintptr_t base;
+    int64_t stride[4], row;
+    int32_t n[4];
+    uintptr_t hi() const
+    {
+        uintptr_t end = base + (uintptr_t)row;
+        for (int i = 0; i < 4; ++i) end += (uintptr_t)((n[i] - 1) * stride[i]);
+        return end;
     }
+};
+
+PoolExtent extent_of(const kvcomm_pages &t, const kvcomm_model &m, const kvcomm_batch &b)
+{
+    const int es = elem_size(m.dtype);
+    PoolExtent e = {reinterpret_cast<uintptr_t>(t.ptr), {t.stride_layer * es, t.stride_head * es, t.stride_page * es, t.stride_token * es},
+                    (int64_t)m.head_dim * es, {m.n_layers, m.n_kv_heads, b.n_pages, b.page_size}};
+    for (int i = 1; i < 4; ++i)   // longest stride first
+        for (int j = i; j > 0 && e.stride[j - 1] < e.stride[j]; --j) {
+            std::swap(e.stride[j - 1], e.stride[j]);
+            std::swap(e.n[j - 1], e.n[j]);
+        }
+    return e;
+}
+
+// Do rows of two pools of the same strides and sizes meet, the second one's base `d` bytes behind the first's?  Some sum of d and multiples |k_i| < n_i of
+// the strides from axis `i` on then lies within a row.  What the shorter strides reach leaves few k_i of each; many (strides that do not nest) count as met.
+bool rows_meet(const PoolExtent &e, int i, int64_t d)
+{
+    if (i == 4) return d > -e.row && d < e.row;
+    int64_t reach = e.row;
+    for (int j = i + 1; j < 4; ++j) reach += (e.n[j] - 1) * e.stride[j];
+    if (e.stride[i] == 0) return rows_meet(e, i + 1, d);
+    const int64_t lo = std::max<int64_t>(floor_div(-reach - d, e.stride[i]) + 1, -(int64_t)(e.n[i] - 1));
+    const int64_t hi = std::min<int64_t>(-floor_div(d - reach, e.stride[i]) - 1, e.n[i] - 1);
+    if (hi - lo > 4) return true;
+    for (int64_t k = lo; k <= hi; ++k)
+        if (rows_meet(e, i + 1, d + k * e.stride[i])) return true;
+    return false;
+}
+
+bool pools_meet(const PoolExtent &a, const PoolExtent &b)
+{
+    if (a.hi() <= b.base || b.hi() <= a.base) return false;
+    for (int i = 0; i < 4; ++i)
+        if (a.stride[i] != b.stride[i] || a.n[i] != b.n[i]) return true;
+    return rows_meet(a, 0, (int64_t)(b.base - a.base));
+}
+
+}  // namespace
+
+extern "C" int kvcomm_place_qkv_paged(const kvcomm_model *model, kvcomm_tensor q, kvcomm_tensor k, kvcomm_tensor v, const kvcomm_batch *batch,
+                                      int32_t first_pos, const void *q_weight, const void *k_weight, int64_t q_weight_stride,
+                                      int64_t k_weight_stride, float norm_eps, kvcomm_tensor q_out, kvcomm_pages pages_k, kvcomm_pages pages_v, void *stream)
+{
+    int st = check_model(model);
+    if (st) return st;
+    PagedPlaceParams p{};
+    if ((st = check_batch(batch, p.batch))) return st;
+    const int dt = model->dtype, es = elem_size(dt), D = model->head_dim, L = model->n_layers, n = batch->n_rows;
+    if ((int64_t)first_pos + p.batch.cap > INT32_MAX) return KVCOMM_EINVAL;
+    if (!(norm_eps >= 0.f) || norm_eps > FLT_MAX) return KVCOMM_EINVAL;
+    const bool pages = p.batch.cap > 0;   // else there is nothing to store into: keys and values are not looked at
+    const kvcomm_tensor in[3] = {q, k, v};
+    const kvcomm_pages *pool[2] = {&pages_k, &pages_v};
+    const int heads[3] = {model->n_q_heads, model->n_kv_heads, model->n_kv_heads};
+    const void *weight[2] = {q_weight, k_weight};
+    const int64_t w_stride[2] = {q_weight_stride, k_weight_stride};
+    Extent from[5];
+    int n_from = 0, of[5] = {3, 3, 3, 3, 3};   // which of the inputs, 3: a weight
+    for (int i = 0; i < 3; ++i) {
+        const void *out = i ? (pages ? pool[i - 1]->ptr : in[i].ptr) : q_out.ptr;
+        if (!in[i].ptr && !out) continue;
+        if ((st = check_tensor(in[i], dt, true)) || (st = i ? (pages ? check_pages(*pool[i - 1], dt) : KVCOMM_OK) : check_tensor(q_out, dt, true))) return st;
+        of[n_from] = i;
+        from[n_from++] = extent_of(in[i], L, heads[i], n, D, es);
+        if (i && !pages) continue;
+        p.in[i] = in[i].ptr;
+        p.out[i] = const_cast<void *>(out);
+        p.s_in[i] = strides_of(in[i]);
+        p.s_out[i] = i ? Strides{pool[i - 1]->stride_layer, pool[i - 1]->stride_head, pool[i - 1]->stride_token} : strides_of(q_out);
+        if (i) p.page[i - 1] = pool[i - 1]->stride_page;
+        p.heads[i] = heads[i];
+    }
+    if (n_from == 0) return KVCOMM_EINVAL;
+    for (int i = 0; i < 2; ++i) {
+        if (!weight[i]) continue;
+        if (norm_eps == 0.f || !in[i].ptr) return KVCOMM_EINVAL;
+        const kvcomm_tensor w = {const_cast<void *>(weight[i]), w_stride[i], 0, 0};
+        if ((st = check_tensor(w, dt, true))) return st;
+        p.weight[i] = weight[i];
+        p.s_weight[i] = w_stride[i];
+        from[n_from++] = extent_of(w, L, 1, 1, D, es);
+    }
+    // What the device reads of the batch is an input, too.
+    const int64_t entries = p.batch.cap ? ((int64_t)batch->n_seqs - 1) * batch->table_stride + batch->table_width : 0;
+    const Extent ints[3] = {extent_flat(batch->lens, 4 * (size_t)batch->n_seqs), extent_flat(batch->starts, batch->starts ? 4 * ((size_t)batch->n_seqs + 1) : 0),
+                            extent_flat(batch->table, 4 * (size_t)entries)};
+    auto within = [](const Extent &x, uintptr_t lo, uintptr_t hi) { return x.lo() < hi && lo < x.hi() && x.run > 0; };
+    PoolExtent to[2] = {};
+    for (int i = 0; i < 2; ++i) {
+        if (!p.out[i + 1]) continue;
+        to[i] = extent_of(*pool[i], *model, *batch);
+        for (int j = 0; j < n_from; ++j)
+            if (within(from[j], to[i].base, to[i].hi())) return KVCOMM_EINVAL;
+        for (const Extent &x : ints)
+            if (within(x, to[i].base, to[i].hi())) return KVCOMM_EINVAL;
+    }
+    if (p.out[1] && p.out[2] && pools_meet(to[0], to[1])) return KVCOMM_EINVAL;
+    if (p.out[0]) {
+        const Extent out = extent_of(q_out, L, heads[0], n, D, es);
+        for (int j = 0; j < n_from; ++j) {
+            const int i = of[j];
+            if (i == 0 && same_extent(out, from[j])) continue;
+            if (extents_overlap(out, from[j]) && !(i < 3 && beside_each_other(q_out, heads[0], D * es, es, in[i], heads[i], D * es, es, L))) return KVCOMM_EINVAL;
+        }
+        for (const Extent &x : ints)
+            if (within(x, out.lo(), out.hi())) return KVCOMM_EINVAL;
+        for (int i = 0; i < 2; ++i)
+            if (p.out[i + 1] && within(out, to[i].base, to[i].hi())) return KVCOMM_EINVAL;
+    }
+    if (!p.out[0] && !p.out[1] && !p.out[2]) return KVCOMM_OK;   // keys and values alone, and no page to store them in
+    p.n = n;
+    p.first_pos = first_pos;
+    p.eps = norm_eps;
+    fill_inv_freq(p.inv_freq, model->rope_theta, D);
+    return launch_place(*model, p, static_cast<hipStream_t>(stream));
 }
