@@ -523,7 +523,7 @@ int kvcomm_suffix_attn_window(const kvcomm_model *model, kvcomm_tensor q,
  *   max_rows     about the most rows that a sequence has, 0: not known.  For the choice of a kernel only: results are right whatever it says.
  * Row i of the n_b rows of sequence b is its token lens[b] - n_b + i.  Whatever table, lens and starts hold, nothing outside the described tensors
  * is read or written; where starts decreases, which rows are written is not defined.
- * Limits: page_size a power of two, 16 ... 65536 (KVCOMM_EUNSUPPORTED else); 1 <= n_seqs <= KVCOMM_MAX_SEQS; n_rows >= 1; table_width * page_size <= 2^30;
+ * Limits: page_size a power of two, 16 ... 65536 (KVCOMM_EUNSUPPORTED else); 1 <= n_seqs <= KVCOMM_MAX_SEQS; n_rows >= 1; n_prefix + table_width * page_size <= 2^30;
  * table_width = 0 or n_pages = 0: no sequence has tokens in pages (the pools' pointers are then ignored).                     */
 #define KVCOMM_MAX_SEQS 8192
 

@@ -1,9 +1,12 @@
 // Attention of a batch of sequences over the pages of a pool, behind a cache that all of them continue: what its kernels share.
 //   out_i = softmax_j(scale <q_i, k_j>) v_j   over the prefix's tokens and the tokens of row i's sequence up to its own.
-// The keys of a sequence are counted in halves of tiles, 32 keys each: first the prefix's (the last of which may be short), then those of its pages.  An
-// item of work is a tile of packed (row, query head) rows r = i * G + g of one kv head (of one sequence, or of all sequences over
-// the prefix) and a run of halves; where a row's halves go to several items, each leaves an unnormalised output, a reference and a sum,
-// which attn_paged_combine_kernel joins.
+// Keys are counted in halves of tiles, 32 each.  An item of work is a tile of packed (row, query head) rows r = i * G + g of one kv head, of one
+// sequence over its pages (and over the prefix before them, where that is not done for all sequences together), or of all sequences over the prefix.
+//
+// The walk of the wavefront kernels (attn_paged_rows.hip, attn_paged_f32.hip): the halves of all items of all (layer, kv head) pairs lie behind each
+// other on one axis, which is cut into as many equal runs as wavefronts fit the chip.  Every wavefront walks its run, whatever the lengths are, without a word to
+// another one.  An item that lies in one run is finished there.  Of one that does not, each wavefront leaves its part: unnormalised output, reference and sum of each
+// row, in the second of its two slots, or, if it holds the item's last half, in the first.  attn_paged_combine_kernel joins them.
 #pragma once
 
 #include "attn_common.h"
@@ -18,10 +21,31 @@ struct PagedAttnParams {
     Strides s_q, s_o, s_pk, s_pv;
     PoolStrides s_k, s_v;
     Batch batch;
-    int32_t L, Hkv, G, n_prefix;
+    int32_t L, Hkv, G, D, n_prefix;
     float scale, scale_log2;
     divisor_t by_G, by_Hkv;
+    // The plan.
+    int32_t walked_prefix;   // halves of the prefix before a sequence's own: all of them or, where the prefix has items of its own, 0
+    int32_t prefix_tiles;    // row tiles of the prefix's items on the wavefronts' axis
+    int32_t prefix_runs;     // or: runs that a tiles kernel cuts the prefix into
+    int32_t tile_rows;
+    int32_t n_waves;         // runs of the axis
+    int32_t most_rows;       // packed rows of the sequences that the launch takes
+    int32_t max_items;       // of a (layer, kv head) on the axis, at most
+    // Scratch, or null: then an item is the work of the wavefront in whose run it begins.  A row's part: D outputs; reference and sum.
+    float *slot_o, *slot_ml;   // [n_waves][2][tile rows]
+    float *row_o, *row_ml;     // [0]: whole items of sequences, [1 ...]: of the prefix and its runs; [layer, query head, row]
+    int32_t *items;            // [layer, kv head][max_items][2]: first and last wavefront of an item; kDirect, kWhole
+    int32_t *item_of;          // [n_rows][2]: item of its sequence's first tile, its number in the sequence
 };
+enum : int32_t { kDirect = -1, kWhole = -2 };   // its rows lie in `out`; in row_o
+
+// The rows of all sequences.
+__device__ __forceinline__ void all_rows(const PagedAttnParams &p, int &first, int &n)
+{
+    first = p.batch.starts ? max(0, min(p.batch.starts[0], p.batch.n_rows)) : 0;
+    n = p.batch.starts ? max(0, min(p.batch.starts[p.batch.n_seqs], p.batch.n_rows) - first) : p.batch.n_rows;
+}
 
 // A sequence's tokens from row i of n on: the last one that it sees, -1 or less: none.
 __device__ __forceinline__ int last_seen(int len, int n, int i, int cap) { return min(len - n + i, min(len, cap) - 1); }
@@ -121,6 +145,284 @@ __device__ __forceinline__ void paged_store_row(const PagedAttnParams &p, int l,
         }
     }
     if (p.lse && lane == 0) p.lse[((int64_t)l * p.Hkv * p.G + hq) * p.batch.n_rows + row] = none ? -INFINITY : m * p.scale + logf(sum);
+}
+
+// ------------------------------------------------------------------------------------------ the walk
+typedef const __attribute__((address_space(4))) int32_t const_int;   // read through the scalar cache (whole-wavefront values)
+__device__ __forceinline__ const_int *scalar(const int32_t *x) { return (const_int *)(uintptr_t)x; }
+
+// An item; all of it the same in all lanes.
+struct PagedItem {
+    int lh, b;          // b < 0: the rows of all sequences over the prefix
+    int tile, tiles;    // row tile, row tiles of the sequence
+    int first, n;       // rows
+    int len;            // tokens by `lens`
+    int walk;           // halves of the prefix at the item's beginning
+    int count;          // halves of the tile, 1 at least (an item without keys has its place on the axis)
+    int index;          // among the items of lh
+};
+
+template <int TR>   // packed rows of a tile
+struct PagedWalk {
+    const PagedAttnParams &p;
+    const int lane;
+    int64_t width = 0;   // halves of a (layer, kv head) on the axis
+    int64_t run = 0;     // of a wavefront
+    PagedItem item = {};
+
+    __device__ __forceinline__ PagedWalk(const PagedAttnParams &p, int lane) : p(p), lane(lane) {}
+
+    __device__ __forceinline__ int tiles_of(int n) const
+    {
+        const int rows = n * p.G;
+        return rows <= p.most_rows ? (rows + TR - 1) / TR : 0;
+    }
+    __device__ __forceinline__ int count_of(int len) const { return max(1, p.walked_prefix + (min(len, p.batch.cap) + 31) / 32); }
+    __device__ __forceinline__ int prefix_count() const { return (p.n_prefix + 31) / 32; }
+
+    // Halves of the sequences c ... c + 63 up to each lane's, and that lane's row tiles.
+    __device__ __forceinline__ int64_t scan(int c, int &tiles) const
+    {
+        const int b = c + lane;
+        int64_t x = 0;
+        tiles = 0;
+        if (b < p.batch.n_seqs) {
+            int first, n;
+            sequence_rows(p.batch, b, first, n);
+            tiles = tiles_of(n);
+            x = (int64_t)tiles * count_of(sequence_len(p.batch, b));
+        }
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int64_t y = __shfl_up(x, off);
+            if (lane >= off) x += y;
+        }
+        return x;
+    }
+    __device__ __forceinline__ static int64_t uniform(int64_t x)
+    {
+        return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x) | (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32);
+    }
+    __device__ __forceinline__ static int64_t of_lane(int64_t x, int lane)
+    {
+        return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32);
+    }
+    // x / d for 0 <= x < 2^53, d > 0
+    __device__ __forceinline__ static int64_t quotient(int64_t x, int64_t d)
+    {
+        int64_t q = (int64_t)((double)x / (double)d);
+        q -= q * d > x;
+        return q + ((q + 1) * d <= x);
+    }
+
+    // The first item that wavefront `wave` works on, and its halves of it; false: none.  min_run: halves of a run at least.
+    __device__ __forceinline__ bool begin(int wave, int min_run, int64_t &pos, int64_t &end, int &h0)
+    {
+        const int64_t ahead = (int64_t)p.prefix_tiles * prefix_count();
+        int tiles;
+        int64_t upto = scan(0, tiles);   // (kept: most batches have no more)
+        width = ahead + of_lane(upto, 63);
+        for (int c = 64; c < p.batch.n_seqs; c += 64) {
+            int t;
+            width += of_lane(scan(c, t), 63);
+        }
+        const int64_t total = width * p.L * p.Hkv;
+        run = max((int64_t)min_run, quotient(total + p.n_waves - 1, p.n_waves));
+        pos = run * wave;
+        end = min(pos + run, total);
+        if (pos >= end) return false;
+        item.lh = (int)quotient(pos, width);
+        int64_t at = pos - (int64_t)item.lh * width;
+        if (at < ahead) {
+            const int count = prefix_count();
+            set_prefix((int)quotient(at, count));
+            h0 = (int)(at - (int64_t)item.tile * count);
+        } else {
+            at -= ahead;
+            int index = p.prefix_tiles;
+            for (int c = 0;; c += 64) {
+                if (c) upto = scan(c, tiles);
+                const int64_t sum = of_lane(upto, 63);
+                const bool here = at < sum;
+                // row tiles up to each lane's
+                int before = tiles;
+#pragma unroll
+                for (int off = 1; off < 64; off <<= 1) {
+                    const int y = __shfl_up(before, off);
+                    if (lane >= off) before += y;
+                }
+                if (here) {
+                    const int j = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > at));
+                    at -= j ? of_lane(upto, j - 1) : 0;
+                    item.index = index + (j ? __builtin_amdgcn_readlane(before, j - 1) : 0);
+                    set_sequence(c + j);
+                    item.tile = (int)quotient(at, item.count);
+                    item.index += item.tile;
+                    h0 = (int)(at - (int64_t)item.tile * item.count);
+                    break;
+                }
+                at -= sum;
+                index += __builtin_amdgcn_readlane(before, 63);
+            }
+        }
+        if (!p.slot_o && h0 > 0) {   // the item is another one's: on to the next
+            pos += item.count - h0;
+            h0 = 0;
+            if (pos >= end) return false;
+            return next();
+        }
+        return true;
+    }
+    // The item behind it; false: there is none.
+    __device__ __forceinline__ bool next()
+    {
+        ++item.index;
+        if (item.tile + 1 < item.tiles) {
+            ++item.tile;
+            return true;
+        }
+        int b = item.b;   // (the prefix: -1)
+        while (true) {
+            if (++b == p.batch.n_seqs) {
+                if (++item.lh >= p.L * p.Hkv) return false;
+                item.index = 0;
+                b = -1;
+                if (p.prefix_tiles) {
+                    set_prefix(0);
+                    return true;
+                }
+                continue;
+            }
+            int first, n;
+            rows_of(b, first, n);
+            if (tiles_of(n) > 0) break;
+        }
+        set_sequence(b);
+        return true;
+    }
+
+private:
+    __device__ __forceinline__ void rows_of(int b, int &first, int &n) const
+    {
+        if (!p.batch.starts) {
+            first = b;
+            n = 1;
+            return;
+        }
+        first = max(0, min(scalar(p.batch.starts)[b], p.batch.n_rows));
+        n = max(0, min(scalar(p.batch.starts)[b + 1], p.batch.n_rows) - first);
+    }
+    __device__ __forceinline__ void set_prefix(int tile)
+    {
+        item.b = -1;
+        item.tile = tile;
+        item.tiles = p.prefix_tiles;
+        item.index = tile;
+        item.count = item.walk = prefix_count();
+        item.len = 0;
+        all_rows(p, item.first, item.n);
+    }
+    __device__ __forceinline__ void set_sequence(int b)
+    {
+        item.b = b;
+        rows_of(b, item.first, item.n);
+        item.tile = 0;
+        item.tiles = tiles_of(item.n);
+        item.len = max(0, scalar(p.batch.lens)[b]);
+        item.walk = p.walked_prefix;
+        item.count = count_of(item.len);
+    }
+};
+
+// Wavefronts of attn_paged_rows_kernel that a compute unit holds: by LDS, and by registers.
+constexpr int paged_rows_waves(int D, int rows) { return D == 256 ? 5 : rows == 32 ? 8 : D == 128 ? 10 : 16; }
+
+int launch_paged_rows(const PagedAttnParams &p, int tile_rows, hipStream_t s);
+
+constexpr int kPagedMinRun = 4;   // halves of a wavefront's run at least
+
+// Where the results of a segment, halves seg0 ... h of an item, go.  pos: the axis behind the segment, run: a wavefront's run of it.
+struct PagedPlace {
+    int kind;        // kDirect; kWhole: row_o; 0: a slot of the wavefront
+    float *o, *ml;   // of the slot's rows, or of rows by (layer, query head, row)
+};
+template <int TR>
+__device__ __forceinline__ PagedPlace paged_place(const PagedAttnParams &p, const PagedItem &it, int seg0, int h, int64_t pos, int64_t run, int lane)
+{
+    const bool ends = h + 1 == it.count, whole = ends && seg0 == 0;
+    const bool apart = p.n_prefix > 0 && p.walked_prefix == 0;   // the prefix has items of its own: every row is joined
+    PagedPlace to = {whole ? apart ? kWhole : kDirect : 0, nullptr, nullptr};
+    if (!p.slot_o) return to;
+    const int64_t wave = blockIdx.x;
+    if (to.kind == kWhole) {
+        const int64_t all = (int64_t)p.L * p.Hkv * p.G * p.batch.n_rows * (it.b < 0 ? 1 : 0);
+        to.o = p.row_o + all * p.D;
+        to.ml = p.row_ml + all * 2;
+    } else if (to.kind == 0) {
+        const int64_t slot = (2 * wave + (ends ? 0 : 1)) * TR;
+        to.o = p.slot_o + slot * p.D;
+        to.ml = p.slot_ml + slot * 2;
+    }
+    if (ends) {
+        if (lane < 2 && it.index < p.max_items) {
+            const int64_t begin = pos - it.count;   // of the item, on the axis
+            const int first = to.kind ? to.kind : (int)PagedWalk<TR>::quotient(begin, run);
+            p.items[((int64_t)it.lh * p.max_items + it.index) * 2 + lane] = lane ? (int)wave : first;
+        }
+        if (it.lh == 0 && it.b >= 0) {   // the rows whose first head lies in this tile
+            const int i0 = div_by(it.tile * TR + p.G - 1, p.by_G);
+            if (lane < TR && i0 + lane < it.n && (i0 + lane) * p.G < (it.tile + 1) * TR) {
+                p.item_of[2 * (it.first + i0 + lane)] = it.index - it.tile;
+                p.item_of[2 * (it.first + i0 + lane) + 1] = i0 + lane;
+            }
+        }
+    }
+    return to;
+}
+
+// Row r of an item's tile, in that place.
+struct PagedRow {
+    bool valid;
+    int l, hq, i, row;
+    int64_t flat;   // (layer, query head, row)
+    int64_t o;      // in the place
+};
+__device__ __forceinline__ PagedRow paged_row(const PagedAttnParams &p, const PagedItem &it, const PagedPlace &to, int tile_rows, int r)
+{
+    PagedRow x;
+    const int packed = it.tile * tile_rows + r;
+    x.l = div_by(it.lh, p.by_Hkv);
+    const int hkv = it.lh - x.l * p.Hkv;
+    x.i = div_by(packed, p.by_G);
+    x.hq = hkv * p.G + packed - x.i * p.G;
+    x.valid = x.i < it.n;
+    x.row = it.first + x.i;
+    x.flat = ((int64_t)x.l * p.Hkv * p.G + x.hq) * p.batch.n_rows + x.row;
+    x.o = to.kind == 0 ? r : x.flat;
+    return x;
+}
+
+// The segment by the formula.
+template <typename T, int D, int TR>
+__device__ __forceinline__ void paged_exact_segment(const PagedAttnParams &p, const PagedItem &it, const PagedPlace &to, int seg0, int h, int lane)
+{
+#pragma unroll 1
+    for (int r = 0; r < TR; ++r) {
+        const PagedRow row = paged_row(p, it, to, TR, r);
+        if (!row.valid) return;
+        float m, sum, o[8];
+        paged_exact_row<T, D>(p, row.l, it.lh - row.l * p.Hkv, row.hq, row.row, it.b, it.b < 0 ? -1 : last_seen(it.len, it.n, row.i, p.batch.cap), it.walk, seg0, h + 1, lane, m, sum, o);
+        if (to.kind == kDirect) {
+            paged_store_row<T, D>(p, row.l, row.hq, row.row, lane, m, sum, o);
+        } else {
+            if (lane < D / 8) {
+                f32x4 *po = reinterpret_cast<f32x4 *>(to.o + row.o * D + 8 * lane);
+                po[0] = f32x4{o[0], o[1], o[2], o[3]};
+                po[1] = f32x4{o[4], o[5], o[6], o[7]};
+            }
+            if (lane < 2) to.ml[row.o * 2 + lane] = lane ? sum : m;
+        }
+    }
 }
 
 }  // namespace kvc

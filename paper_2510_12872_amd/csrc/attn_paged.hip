@@ -26,6 +26,139 @@ __global__ __launch_bounds__(256) void attn_paged_row_kernel(const PagedAttnPara
     paged_store_row<T, D>(p, l, hq, row, lane, m, sum, o);
 }
 
+// The results of rows whose keys went to several wavefronts or runs: out = sum_s f_s O_s / sum_s f_s l_s, f_s = exp2((m_s - max m) scale log2 e), parts in
+// a fixed order.  One wavefront per row; D / 4 lanes hold its channels, and the 64 / (D / 4) such groups take the parts in turn.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attn_paged_combine_kernel(const PagedAttnParams p)
+{
+    constexpr int CL = D / 4, NG = 64 / CL, U = 4;
+    const int lane = threadIdx.x & 63, Hq = p.Hkv * p.G, n_rows = p.batch.n_rows;
+    const int64_t flat = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t all = (int64_t)p.L * Hq * n_rows;
+    if (flat >= all) return;
+    const int row = (int)(flat % n_rows), head = (int)(flat / n_rows), l = head / Hq, hq = head - l * Hq, hkv = div_by(hq, p.by_G), g = hq - hkv * p.G;
+    int first, n;
+    all_rows(p, first, n);
+    if (row < first || row >= first + n) return;
+    const bool apart = p.n_prefix > 0 && p.walked_prefix == 0;
+    // What the walks left of an item: `count` slots from wavefront `wave` on, the last of them an item's end; or one part by rows.  (Clamped: item_of is not
+    // written for every row where starts decreases.)
+    struct Parts {
+        int wave, count, row;
+        bool whole;
+    };
+    auto parts_of = [&](int index, int packed) -> Parts {
+        const int32_t *e = p.items + ((int64_t)(l * p.Hkv + hkv) * p.max_items + max(0, min(index, p.max_items - 1))) * 2;
+        const int w0 = e[0], w1 = e[1];
+        if (w0 < 0) return Parts{w0, 1, 0, true};
+        const int last = max(0, min(w1, p.n_waves - 1)), from = min(w0, last);
+        return Parts{from, last - from + 1, packed & (p.tile_rows - 1), false};
+    };
+    const int packed = p.item_of[2 * row + 1] * p.G + g;
+    const Parts own = parts_of(p.item_of[2 * row] + (int)((uint32_t)packed / (uint32_t)p.tile_rows), packed);
+    if (own.wave == kDirect) return;
+    Parts before = {0, p.prefix_runs, 0, true};
+    if (apart && p.prefix_tiles) {
+        const int at = (row - first) * p.G + g;
+        before = parts_of((int)((uint32_t)at / (uint32_t)p.tile_rows), at);
+    }
+    const int count = own.count + (apart ? before.count : 0);
+    auto place = [&](int k, const float *&o, const float *&ml) {
+        const bool b = k >= own.count;
+        const Parts &x = b ? before : own;
+        if (b) k -= own.count;
+        if (x.whole) {
+            const int64_t at = flat + (b ? 1 + k : 0) * all;
+            o = p.row_o + at * D;
+            ml = p.row_ml + at * 2;
+        } else {
+            const int64_t at = (2 * (int64_t)(x.wave + k) + (k + 1 < x.count ? 1 : 0)) * p.tile_rows + x.row;
+            o = p.slot_o + at * D;
+            ml = p.slot_ml + at * 2;
+        }
+    };
+    float M = -INFINITY;
+    for (int k = lane; k < count; k += 64) {
+        const float *o, *ml;
+        place(k, o, ml);
+        M = fmaxf(M, ml[0]);
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
+    const int group = lane / CL, c = 4 * (lane % CL);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    for (int k0 = group; k0 < count; k0 += NG * U) {
+        f32x4 os[U];
+        float ms[U], ls[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float *o, *ml;
+            place(min(k0 + u * NG, count - 1), o, ml);
+            ms[u] = ml[0];
+            ls[u] = ml[1];
+            os[u] = *reinterpret_cast<const f32x4 *>(o + c);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (k0 + u * NG < count && (ms[u] != -INFINITY || ls[u] != 0.f)) {   // (reference -inf, sum 0: nothing seen; NaN: NaN scores)
+                const float f = __builtin_amdgcn_exp2f((ms[u] - M) * p.scale_log2);
+                sum = fmaf(f, ls[u], sum);
+                acc += f * os[u];
+            }
+        }
+    }
+#pragma unroll
+    for (int off = CL; off < 64; off <<= 1) {
+        sum += __shfl_xor(sum, off);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], off);
+    }
+    const bool none = M == -INFINITY && sum == 0.f;
+    if (group == 0) {
+        const float inv = none ? 0.f : 1.f / sum;
+        T *out = static_cast<T *>(p.out) + l * p.s_o.layer + (int64_t)hq * p.s_o.head + (int64_t)row * p.s_o.token + c;
+        if constexpr (sizeof(T) == 2)
+            *reinterpret_cast<u32x2 *>(out) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+        else
+            *reinterpret_cast<f32x4 *>(out) = acc * inv;
+    }
+    if (p.lse && lane == 0) p.lse[flat] = none ? -INFINITY : M * p.scale + logf(sum);
+}
+
+// How a call is carried out: the sizes that depend on the model, the batch's host side and the prefix's length alone.
+struct Plan {
+    int tile_rows, n_waves, prefix_tiles;
+    int64_t max_items, row_parts;   // parts by rows: [row_parts][layer, query head, row]
+    size_t bytes;
+};
+
+Plan plan_of(const kvcomm_model &m, const kvcomm_batch &b, int n_prefix)
+{
+    Plan pl{};
+    const int G = m.n_q_heads / m.n_kv_heads, D = m.head_dim;
+    const int64_t LH = (int64_t)m.n_layers * m.n_kv_heads, rows = (int64_t)b.n_rows * G;
+    const int64_t most = b.starts ? (b.max_rows ? std::min<int64_t>(b.max_rows, b.n_rows) : b.n_rows) * G : G;
+    pl.tile_rows = D < 256 && (most > 16 || (n_prefix && rows > 16)) ? 32 : 16;
+    pl.n_waves = kChipCUs * paged_rows_waves(D, pl.tile_rows);
+    pl.prefix_tiles = n_prefix ? (int)((rows + pl.tile_rows - 1) / pl.tile_rows) : 0;
+    pl.max_items = pl.prefix_tiles + (b.starts ? rows / pl.tile_rows + b.n_seqs : (int64_t)b.n_seqs * ((G + pl.tile_rows - 1) / pl.tile_rows));
+    pl.row_parts = n_prefix ? 2 : 0;
+    pl.bytes = sizeof(float) * (size_t)(D + 2) * ((size_t)pl.n_waves * 2 * pl.tile_rows + (size_t)(pl.row_parts * LH * rows)) +
+               sizeof(int32_t) * ((size_t)(2 * LH * pl.max_items) + 2 * (size_t)b.n_rows);
+    return pl;
+}
+
+// What attention calls refuse before anything else is looked at: sizes that their 32-bit counts do not hold.
+bool countable(const kvcomm_model &m, const kvcomm_batch &b)
+{
+    const double G = m.n_q_heads / m.n_kv_heads;
+    return (double)b.n_rows * G <= (double)kMaxRows && (double)b.n_rows * m.n_q_heads * m.n_layers < 67108864.0 && (double)m.n_layers * m.n_kv_heads <= INT32_MAX;
+}
+
+// The direct loads' 32-bit offsets: see direct_loads_reach().
+bool reaches(int64_t token_stride, int D) { return direct_loads_reach(Strides{0, 0, token_stride}, D); }
+
 int paged_attn(const kvcomm_model *model, const kvcomm_tensor &q, const kvcomm_tensor &prefix_k, const kvcomm_tensor &prefix_v, int32_t n_prefix,
                const kvcomm_pages &pages_k, const kvcomm_pages &pages_v, const kvcomm_batch *batch, float softmax_scale, const kvcomm_tensor &out,
                float *lse_out, void *workspace, size_t workspace_bytes, void *stream)
@@ -38,7 +171,10 @@ int paged_attn(const kvcomm_model *model, const kvcomm_tensor &q, const kvcomm_t
     if (n_prefix && ((st = check_tensor(prefix_k, dt, true)) || (st = check_tensor(prefix_v, dt, true)))) return st;
     if (p.batch.cap && ((st = check_pages(pages_k, dt)) || (st = check_pages(pages_v, dt)))) return st;
     if (!aligned4(lse_out)) return KVCOMM_EINVAL;
-    if (n_prefix > kMaxPagedTokens) return KVCOMM_EUNSUPPORTED;
+    if ((int64_t)n_prefix + p.batch.cap > kMaxPagedTokens || !countable(*model, *batch)) return KVCOMM_EUNSUPPORTED;
+    if (dt == KVCOMM_BF16 && ((p.batch.cap && (!reaches(pages_k.stride_token, D) || !reaches(pages_v.stride_token, D))) ||
+                              (n_prefix && (!reaches(prefix_k.stride_token, D) || !reaches(prefix_v.stride_token, D)))))
+        return KVCOMM_EUNSUPPORTED;
     p.q = q.ptr;
     p.out = out.ptr;
     p.lse = lse_out;
@@ -60,21 +196,59 @@ int paged_attn(const kvcomm_model *model, const kvcomm_tensor &q, const kvcomm_t
     p.scale_log2 = (float)((double)p.scale * 1.4426950408889634);
     p.by_G = make_divisor((uint32_t)p.G);
     p.by_Hkv = make_divisor((uint32_t)p.Hkv);
-    const double rows = (double)p.L * p.Hkv * p.G * p.batch.n_rows;
-    if (rows >= 67108864.0) return KVCOMM_EUNSUPPORTED;
-    const dim3 grid((unsigned)((rows + 3) / 4)), block(256);
+    p.D = D;
+    const int64_t rows = (int64_t)p.L * p.Hkv * p.G * p.batch.n_rows;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const bool f32 = dt == KVCOMM_F32;
-    switch (D) {
-        case 64: return launch(f32 ? attn_paged_row_kernel<float, 64> : attn_paged_row_kernel<bf16_t, 64>, grid, block, 0, s, p);
-        case 128: return launch(f32 ? attn_paged_row_kernel<float, 128> : attn_paged_row_kernel<bf16_t, 128>, grid, block, 0, s, p);
-        default: return launch(f32 ? attn_paged_row_kernel<float, 256> : attn_paged_row_kernel<bf16_t, 256>, grid, block, 0, s, p);
+    if (dt == KVCOMM_F32) {
+        if (rows >= 67108864) return KVCOMM_EUNSUPPORTED;
+        const dim3 grid((unsigned)((rows + 3) / 4)), block(256);
+        switch (D) {
+            case 64: return launch(attn_paged_row_kernel<float, 64>, grid, block, 0, s, p);
+            case 128: return launch(attn_paged_row_kernel<float, 128>, grid, block, 0, s, p);
+            default: return launch(attn_paged_row_kernel<float, 256>, grid, block, 0, s, p);
+        }
     }
+    const Plan pl = plan_of(*model, *batch, n_prefix);
+    const bool scratch = workspace && aligned16(workspace) && workspace_bytes >= pl.bytes;
+    p.tile_rows = pl.tile_rows;
+    p.n_waves = pl.n_waves;
+    p.most_rows = INT32_MAX;
+    p.max_items = (int32_t)pl.max_items;
+    if (scratch) {
+        float *x = static_cast<float *>(workspace);
+        auto take = [&](int64_t n) { float *y = x; x += n; return y; };
+        p.slot_o = take((int64_t)pl.n_waves * 2 * pl.tile_rows * D);
+        p.row_o = take(pl.row_parts * rows * D);
+        p.slot_ml = take((int64_t)pl.n_waves * 2 * pl.tile_rows * 2);
+        p.row_ml = take(pl.row_parts * rows * 2);
+        p.items = reinterpret_cast<int32_t *>(take(2 * (int64_t)p.L * p.Hkv * pl.max_items));
+        p.item_of = reinterpret_cast<int32_t *>(x);
+        p.prefix_tiles = pl.prefix_tiles;
+    } else {
+        p.walked_prefix = (n_prefix + 31) / 32;
+    }
+    if ((st = launch_paged_rows(p, pl.tile_rows, s)) || !scratch) return st;
+    const dim3 grid((unsigned)((rows + 3) / 4)), block(256);
+    switch (D) {
+        case 64: return launch(attn_paged_combine_kernel<bf16_t, 64>, grid, block, 0, s, p);
+        case 128: return launch(attn_paged_combine_kernel<bf16_t, 128>, grid, block, 0, s, p);
+        default: return launch(attn_paged_combine_kernel<bf16_t, 256>, grid, block, 0, s, p);
+    }
+}
+
+size_t workspace_of(const kvcomm_model *model, const kvcomm_batch *batch, int32_t n_prefix)
+{
+    Batch b;
+    if (check_model(model) || check_batch(batch, b) || n_prefix < 0 || (int64_t)n_prefix + b.cap > kMaxPagedTokens || model->dtype != KVCOMM_BF16 || !countable(*model, *batch)) return 0;
+    return plan_of(*model, *batch, n_prefix).bytes;
 }
 
 }  // namespace
 
-extern "C" size_t kvcomm_paged_attn_workspace(const kvcomm_model *model, const kvcomm_batch *batch) { return 0; }
+extern "C" size_t kvcomm_paged_attn_workspace(const kvcomm_model *model, const kvcomm_batch *batch)
+{
+    return workspace_of(model, batch, 0);
+}
 
 extern "C" int kvcomm_paged_attn(const kvcomm_model *model, kvcomm_tensor q, kvcomm_pages pages_k, kvcomm_pages pages_v, const kvcomm_batch *batch,
                                  float softmax_scale, kvcomm_tensor out, float *lse_out, void *workspace, size_t workspace_bytes, void *stream)
@@ -83,7 +257,10 @@ extern "C" int kvcomm_paged_attn(const kvcomm_model *model, kvcomm_tensor q, kvc
     return paged_attn(model, q, none, none, 0, pages_k, pages_v, batch, softmax_scale, out, lse_out, workspace, workspace_bytes, stream);
 }
 
-extern "C" size_t kvcomm_paged_attn_prefix_workspace(const kvcomm_model *model, int32_t n_prefix, const kvcomm_batch *batch) { return 0; }
+extern "C" size_t kvcomm_paged_attn_prefix_workspace(const kvcomm_model *model, int32_t n_prefix, const kvcomm_batch *batch)
+{
+    return n_prefix <= 0 ? 0 : workspace_of(model, batch, n_prefix);
+}
 
 extern "C" int kvcomm_paged_attn_prefix(const kvcomm_model *model, kvcomm_tensor q, kvcomm_tensor prefix_k, kvcomm_tensor prefix_v, int32_t n_prefix,
                                         kvcomm_pages pages_k, kvcomm_pages pages_v, const kvcomm_batch *batch, float softmax_scale, kvcomm_tensor out,

@@ -1,0 +1,312 @@
+// bf16 attention of few rows over pages and a prefix (decoded tokens): single wavefronts on the walk of attn_paged.h.
+#include "attn_paged.h"
+
+namespace {
+
+using namespace kvc;
+
+template <int N>
+__device__ __forceinline__ void wait_loads()   // at most N of this wavefront's vector-memory operations stay outstanding
+{
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
+
+// attn_paged_rows_kernel: 16 * RH packed rows on 16x16x32 MFMAs, products, operand layout and LDS swizzles as in attn_rows_kernel16, but a wavefront is alone: it
+// walks 32 keys after the other of its run, K and V of a half go global -> LDS into its own 64 * D bytes, and those of the next half, of whatever item, are
+// requested as soon as the operands of this one are in registers.  Nothing is joined inside the launch, so that no wavefront waits for another one;
+// their number per compute unit is what fits LDS.
+// What bounds it is HBM.  A half lies in one page or in two, whose entries are read, through the scalar cache, a half ahead.
+template <int D, int RH>
+__global__ __launch_bounds__(64, RH == 2 || D == 256 ? 2 : D == 128 ? 3 : 4) void attn_paged_rows_kernel(const PagedAttnParams p)
+{
+    constexpr int TR = 16 * RH;
+    constexpr int NF = D / 16, KCH = D / 8, ROWB = D * 2, HALFB = 32 * ROWB;
+    constexpr int RPL = 64 / KCH, LPT = 32 / RPL;              // key rows filled by one wavefront-wide direct load, loads of a half
+    constexpr int KD = 16 / RPL, VD = RPL < 8 ? 8 / RPL : 1;   // loads after which the swizzle pattern of the rows repeats
+    auto k_swz = [](int key) __attribute__((always_inline)) -> int { return D == 64 ? (key >> 1) & 7 : key & 15; };
+    auto v_swz = [](int key) __attribute__((always_inline)) -> int {
+        return D == 64 ? (2 * (key & 2)) | ((key >> 1) & 2) : 4 * (key & 3) | ((key >> 1) & 2);
+    };
+    __shared__ __align__(16) unsigned char smem[2 * HALFB];
+    const int lane = threadIdx.x, n = lane & 15, g = lane >> 4, lq = lane / KCH;
+    lds_byte *kbuf = (lds_byte *)smem, *vbuf = kbuf + HALFB;
+
+    PagedWalk<TR> walk(p, lane);
+    int64_t pos, end;
+    int h;
+    if (!walk.begin(blockIdx.x, kPagedMinRun, pos, end, h)) return;
+    // What nobody reads again and the last-level cache does not hold is not kept there.
+    const bool nt = walk.width * p.L * p.Hkv * (HALFB * 2) > (int64_t)256 << 20;
+
+    // ---- where the halves of an item lie
+    const unsigned char *kp, *vp, *kf, *vf;   // (layer, head) of the pools and of the prefix
+    const_int *table = nullptr;
+    int tokens = 0;                           // of the sequence that exist
+    auto enter = [&]() __attribute__((always_inline)) {   // walk.item
+        const PagedItem &it = walk.item;
+        const int l = div_by(it.lh, p.by_Hkv), hkv = it.lh - l * p.Hkv;
+        kp = reinterpret_cast<const unsigned char *>(static_cast<const bf16_t *>(p.k) + l * p.s_k.layer + hkv * p.s_k.head);
+        vp = reinterpret_cast<const unsigned char *>(static_cast<const bf16_t *>(p.v) + l * p.s_v.layer + hkv * p.s_v.head);
+        kf = reinterpret_cast<const unsigned char *>(static_cast<const bf16_t *>(p.prefix_k) + l * p.s_pk.layer + hkv * p.s_pk.head);
+        vf = reinterpret_cast<const unsigned char *>(static_cast<const bf16_t *>(p.prefix_v) + l * p.s_pv.layer + hkv * p.s_pv.head);
+        tokens = it.b < 0 ? 0 : min(it.len, p.batch.cap);
+        table = scalar(p.batch.table) + (int64_t)max(it.b, 0) * p.batch.table_stride;
+    };
+    struct Half {       // of an item, to be loaded
+        int at;         // key of the prefix or token of the pages
+        bool prefix;
+        int page[2];    // of the tokens at ... and at + 16 ...
+    };
+    // (Tokens behind the last one that exists are read as that one, see load(); an item without tokens reads nothing.)
+    auto half_at = [&](int h_) __attribute__((always_inline)) -> Half {
+        Half x = {32 * h_, h_ < walk.item.walk, {0, 0}};
+        if (!x.prefix) {
+            x.at -= 32 * walk.item.walk;
+            if (tokens > 0) {
+                x.page[0] = table[x.at >> p.batch.log_page];
+                x.page[1] = table[min(x.at + 16, tokens - 1) >> p.batch.log_page];
+            }
+        }
+        return x;
+    };
+    uint32_t k_chunk[KD], v_chunk[VD];   // bytes inside a row that this lane fetches
+#pragma unroll
+    for (int i = 0; i < KD; ++i) k_chunk[i] = ((lane % KCH) ^ k_swz(i * RPL + lq)) * 16;
+#pragma unroll
+    for (int i = 0; i < VD; ++i) v_chunk[i] = ((lane % KCH) ^ v_swz(i * RPL + lq)) * 16;
+    bool no_page = false;   // of the segment
+    auto load_rows = [&](auto nt_c, const unsigned char *row, int64_t tok, int count, uint32_t chunk, lds_byte *dst) __attribute__((always_inline)) {
+        // `count` rows exist from `row` on (1 at least); a lane whose row does not reads the last one
+        dma16_sbase<decltype(nt_c)::value>(row, (uint32_t)min(lq, count - 1) * (uint32_t)(tok * 2) + chunk, dst);
+    };
+    auto load_as = [&](auto nt_c, const Half &x, const unsigned char *pool, int64_t page_stride, int64_t tok, const unsigned char *pre, int64_t pre_tok, auto &chunk,
+                       lds_byte *dst) __attribute__((always_inline)) {
+        constexpr int NC = sizeof(chunk) / sizeof(chunk[0]);
+        if (x.prefix) {
+#pragma unroll
+            for (int i = 0; i < LPT; ++i) {
+                const int row = min(x.at + i * RPL, p.n_prefix - 1);
+                load_rows(nt_c, pre + (int64_t)row * pre_tok * 2, pre_tok, p.n_prefix - row, chunk[i % NC], dst + i * RPL * ROWB);
+            }
+        } else if (tokens > 0) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const bool there = (uint32_t)x.page[half] < (uint32_t)p.batch.n_pages;
+                const int first = min(x.at + 16 * half, tokens - 1);   // (of the page that page[half] is)
+                const unsigned char *base = pool + (int64_t)(there ? x.page[half] : 0) * page_stride * 2;
+#pragma unroll
+                for (int i = half * LPT / 2; i < (half + 1) * LPT / 2; ++i) {
+                    const int row = max(first, min(x.at + i * RPL, tokens - 1));
+                    load_rows(nt_c, base + (int64_t)(row & ((1 << p.batch.log_page) - 1)) * tok * 2, tok, tokens - row, chunk[i % NC], dst + i * RPL * ROWB);
+                }
+            }
+        }
+    };
+    auto load = [&](const Half &x, const unsigned char *pool, int64_t page_stride, int64_t tok, const unsigned char *pre, int64_t pre_tok, auto &chunk,
+                    lds_byte *dst) __attribute__((always_inline)) {
+        if (nt)
+            load_as(std::true_type{}, x, pool, page_stride, tok, pre, pre_tok, chunk, dst);
+        else
+            load_as(std::false_type{}, x, pool, page_stride, tok, pre, pre_tok, chunk, dst);
+    };
+    auto load_k = [&](const Half &x) __attribute__((always_inline)) { load(x, kp, p.s_k.page, p.s_k.token, kf, p.s_pk.token, k_chunk, kbuf); };
+    auto load_v = [&](const Half &x) __attribute__((always_inline)) { load(x, vp, p.s_v.page, p.s_v.token, vf, p.s_pv.token, v_chunk, vbuf); };
+
+    // ---- the rows of an item
+    PagedItem cur;
+    bf16x8 qf[RH][NF / 2];
+    int last[RH], last_min = 0;    // last token that this lane's row sees, and that the tile's first row does
+    f32x4 o[RH][NF];
+    float m[RH], mc[RH], lsum[RH];   // lsum: this lane's quarter of the row sum
+    int seg0 = 0;                    // first half of the segment
+    auto rows = [&](int first_half) __attribute__((always_inline)) {
+        cur = walk.item;
+        seg0 = first_half;
+        no_page = false;
+        const int l = div_by(cur.lh, p.by_Hkv), hkv = cur.lh - l * p.Hkv;
+        last_min = last_seen(cur.len, cur.n, min(div_by(cur.tile * TR, p.by_G), cur.n - 1), p.batch.cap);
+#pragma unroll
+        for (int x = 0; x < RH; ++x) {
+            const int r = cur.tile * TR + 16 * x + n, i = div_by(r, p.by_G), ii = max(0, min(i, cur.n - 1));
+            const int row = min(cur.first + ii, p.batch.n_rows - 1);
+            last[x] = last_seen(cur.len, cur.n, ii, p.batch.cap);
+            const bf16_t *q = static_cast<const bf16_t *>(p.q) + l * p.s_q.layer + (int64_t)(hkv * p.G + r - i * p.G) * p.s_q.head + (int64_t)row * p.s_q.token;
+#pragma unroll
+            for (int ks = 0; ks < NF / 2; ++ks) qf[x][ks] = as_bf16x8(load16(q + ks * 32 + g * 8));
+#pragma unroll
+            for (int db = 0; db < NF; ++db) o[x][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+            m[x] = -INFINITY, mc[x] = 0.f, lsum[x] = 0.f;
+        }
+        __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0), seen by the compiler: it puts no wait for the queries into the loop
+    };
+
+    enter();
+    Half x = half_at(h);
+    load_k(x);
+    load_v(x);
+    rows(h);
+
+    // Operand addresses: K chunk 4 * ks + g of key n (and 16 + n); V^T is transposed on the way out of LDS.
+    int k_off[NF / 2], v_off[NF];
+#pragma unroll
+    for (int ks = 0; ks < NF / 2; ++ks) k_off[ks] = n * ROWB + (((4 * ks + g) ^ k_swz(n)) * 16);
+    {
+        const int row = 4 * g + (n >> 2);
+#pragma unroll
+        for (int db = 0; db < NF; ++db) {
+            const int col = 16 * db + 4 * (n & 3);
+            v_off[db] = row * ROWB + ((col >> 3) ^ v_swz(row)) * 16 + (col & 7) * 2;
+        }
+    }
+
+    while (true) {
+        const bool ends = h + 1 == cur.count;   // the item
+        ++pos;
+        bool more = pos < end || (!p.slot_o && !ends);
+        int nh = h + 1;
+        if (!x.prefix) no_page |= tokens > 0 && ((uint32_t)x.page[0] >= (uint32_t)p.batch.n_pages || (uint32_t)x.page[1] >= (uint32_t)p.batch.n_pages);
+        // Keys of this half that a row sees: those before its limit (counted from this lane's first).
+        const int edge = x.prefix ? p.n_prefix - 1 - x.at : last_min - x.at;
+        int limit[RH];
+#pragma unroll
+        for (int i = 0; i < RH; ++i) limit[i] = (x.prefix ? p.n_prefix - 1 : last[i]) - x.at - 4 * g;
+        if (more && ends) {
+            more = walk.next();
+            nh = 0;
+            if (more) enter();
+        }
+        Half nx = x;
+        if (more) nx = half_at(nh);
+
+        wait_loads<LPT>();               // K has landed (V may be outstanding)
+        bf16x8 ka[NF];                   // all operand reads in flight at once: ks = i / 2, keys 16 * (i & 1) ...
+#pragma unroll
+        for (int i = 0; i < NF; ++i) ka[i] = as_bf16x8(*(const __attribute__((address_space(3))) u32x4 *)(kbuf + (i & 1) * 16 * ROWB + k_off[i >> 1]));
+        wait_lds();                      // K has been read: its buffer is free
+        if (more) load_k(nx);
+        f32x4 s[RH][2];                  // score j of this lane: key 16 * (j / 4) + 4 * g + j % 4
+#pragma unroll
+        for (int i = 0; i < NF; ++i)
+#pragma unroll
+            for (int r = 0; r < RH; ++r)
+                s[r][i & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[i], qf[r][i >> 1], i < 2 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[r][i & 1], 0, 0, 0);
+        if (edge < 31) {                 // some key is hidden from some row
+#pragma unroll
+            for (int r = 0; r < RH; ++r)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (16 * (j >> 2) + (j & 3) > limit[r]) s[r][j >> 2][j & 3] = -INFINITY;
+        }
+        float mx[RH];
+        bool grows = false;
+#pragma unroll
+        for (int r = 0; r < RH; ++r) {
+            mx[r] = s[r][0][0];
+#pragma unroll
+            for (int j = 1; j < 8; ++j) mx[r] = fmaxf(mx[r], s[r][j >> 2][j & 3]);
+            mx[r] = query_max(mx[r]);
+            grows |= mx[r] > m[r];
+        }
+        if (__builtin_amdgcn_ballot_w64(grows) != 0) {
+#pragma unroll
+            for (int r = 0; r < RH; ++r) {   // (a row whose reference stays is multiplied by 1)
+                const float m_new = fmaxf(m[r], mx[r]);
+                const float corr = m[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[r] - m_new) * p.scale_log2);
+                lsum[r] *= corr;
+#pragma unroll
+                for (int db = 0; db < NF; ++db) o[r][db] *= corr;
+                m[r] = m_new;
+                mc[r] = m[r] == -INFINITY ? 0.f : m[r] * p.scale_log2;   // a row that has seen no key yet: exponentials 0
+            }
+        }
+        // Probabilities are rounded to bf16 for the second product, as in the other attention kernels; their sums take them unrounded.
+        bf16x8 pf[RH];
+#pragma unroll
+        for (int r = 0; r < RH; ++r) {
+            u32x4 pk;
+            float rs0 = 0.f, rs1 = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][j >> 1][2 * (j & 1)], p.scale_log2, -mc[r]));
+                const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][j >> 1][2 * (j & 1) + 1], p.scale_log2, -mc[r]));
+                rs0 += e0;
+                rs1 += e1;
+                pk[j] = pack_bf16x2(e0, e1);
+            }
+            pf[r] = as_bf16x8(pk);
+            lsum[r] += rs0 + rs1;
+        }
+        if (more)
+            wait_loads<LPT>();   // V has landed (K of the next half may be outstanding)
+        else
+            wait_loads<0>();
+        bf16x8 va[NF];
+#pragma unroll
+        for (int db = 0; db < NF; ++db) va[db] = lds_read_tr_pair(vbuf + v_off[db], vbuf + v_off[db] + 16 * ROWB);
+        wait_lds();                      // V has been read
+        if (more) load_v(nx);
+#pragma unroll
+        for (int db = 0; db < NF; ++db)
+#pragma unroll
+            for (int r = 0; r < RH; ++r) o[r][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[db], pf[r], o[r][db], 0, 0, 0);
+
+        if (ends || !more) {
+            // ---- the segment [seg0, h] of the item is done
+            const PagedPlace to = paged_place<TR>(p, cur, seg0, h, pos, walk.run, lane);
+            bool odd = no_page;
+#pragma unroll
+            for (int r = 0; r < RH; ++r) {
+                lsum[r] = query_sum(lsum[r]);
+                float zero = lsum[r] * 0.f;
+#pragma unroll
+                for (int i = 0; i < 4 * NF; ++i) zero = fmaf(o[r][i / 4][i % 4], 0.f, zero);
+                odd |= state_is_odd(zero, m[r], lsum[r]);
+            }
+            if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+                paged_exact_segment<bf16_t, D, TR>(p, cur, to, seg0, h, lane);
+            } else {
+#pragma unroll
+                for (int r = 0; r < RH; ++r) {
+                    const PagedRow row = paged_row(p, cur, to, TR, 16 * r + n);
+                    if (!row.valid) continue;
+                    if (to.kind == kDirect) {
+                        const bool none = m[r] == -INFINITY && lsum[r] == 0.f;
+                        const float inv = none ? 0.f : 1.f / lsum[r];
+                        bf16_t *out = static_cast<bf16_t *>(p.out) + row.l * p.s_o.layer + (int64_t)row.hq * p.s_o.head + (int64_t)row.row * p.s_o.token + 4 * g;
+#pragma unroll
+                        for (int db = 0; db < NF; ++db)
+                            *reinterpret_cast<u32x2 *>(out + 16 * db) = u32x2{pack_bf16x2(o[r][db][0] * inv, o[r][db][1] * inv), pack_bf16x2(o[r][db][2] * inv, o[r][db][3] * inv)};
+                        if (p.lse && g == 0) p.lse[row.flat] = none ? -INFINITY : m[r] * p.scale + logf(lsum[r]);
+                    } else {
+                        float *po = to.o + row.o * D + 4 * g;
+#pragma unroll
+                        for (int db = 0; db < NF; ++db) *reinterpret_cast<f32x4 *>(po + 16 * db) = o[r][db];
+                        if (g < 2) to.ml[row.o * 2 + g] = g ? lsum[r] : m[r];
+                    }
+                }
+            }
+            if (!more) return;
+            rows(nh);
+        }
+        x = nx;
+        h = nh;
+    }
+}
+
+}  // namespace
+
+namespace kvc {
+
+int launch_paged_rows(const PagedAttnParams &p, int tile_rows, hipStream_t s)
+{
+    const dim3 grid((unsigned)p.n_waves), block(64);
+    const bool one = tile_rows == 16;
+    switch (p.D) {
+        case 64: return launch(one ? attn_paged_rows_kernel<64, 1> : attn_paged_rows_kernel<64, 2>, grid, block, 0, s, p);
+        case 128: return launch(one ? attn_paged_rows_kernel<128, 1> : attn_paged_rows_kernel<128, 2>, grid, block, 0, s, p);
+        default: return launch(attn_paged_rows_kernel<256, 1>, grid, block, 0, s, p);
+    }
+}
+
+}  // namespace kvc
