@@ -27,21 +27,24 @@ struct PagedAttnParams {
     // The plan.
     int32_t walked_prefix;   // halves of the prefix before a sequence's own: all of them or, where the prefix has items of its own, 0
     int32_t prefix_tiles;    // row tiles of the prefix's items on the wavefronts' axis
-    int32_t prefix_runs;     // or: runs that a tiles kernel cuts the prefix into
+    int32_t prefix_runs;     // or: runs that the tiles kernel cuts the prefix into
+    int32_t prefix_part;     // first part by rows that is the prefix's
+    int32_t tile_runs;       // runs of a sequence that the tiles kernel takes
     int32_t tile_rows;
     int32_t n_waves;         // runs of the axis
     int32_t most_rows;       // packed rows of the sequences that the launch takes
     int32_t max_items;       // of a (layer, kv head) on the axis, at most
     // Scratch, or null: then an item is the work of the wavefront in whose run it begins.  A row's part: D outputs; reference and sum.
     float *slot_o, *slot_ml;   // [n_waves][2][tile rows]
-    float *row_o, *row_ml;     // [0]: whole items of sequences, [1 ...]: of the prefix and its runs; [layer, query head, row]
+    float *row_o, *row_ml;     // parts by rows, [part][layer, query head, row]: whole items or the tiles kernel's runs of sequences, then the prefix's
     int32_t *items;            // [layer, kv head][max_items][2]: first and last wavefront of an item; kDirect, kWhole
-    int32_t *item_of;          // [n_rows][2]: item of its sequence's first tile, its number in the sequence
+    int32_t *item_of;          // [n_rows][2]: item of its sequence's first tile, its number in the sequence; kDirect, kWhole: the tiles kernel's
 };
 enum : int32_t { kDirect = -1, kWhole = -2 };   // its rows lie in `out`; in row_o
 
 // The rows of all sequences.
-__device__ __forceinline__ void all_rows(const PagedAttnParams &p, int &first, int &n)
+template <class P>   // PagedAttnParams, in any address space
+__device__ __forceinline__ void all_rows(const P &p, int &first, int &n)
 {
     first = p.batch.starts ? max(0, min(p.batch.starts[0], p.batch.n_rows)) : 0;
     n = p.batch.starts ? max(0, min(p.batch.starts[p.batch.n_seqs], p.batch.n_rows) - first) : p.batch.n_rows;
@@ -53,8 +56,8 @@ __device__ __forceinline__ int last_seen(int len, int n, int i, int cap) { retur
 // One row (sequence b, row `row` of the queries, query head hq) over the halves [h0, h1) by the formula, key by key, in fp32; what the row does not
 // see (`last`: the last token of its pages that it sees) is not looked at.  Whole rows: halves 0 ... of the prefix, then of the pages.
 // Returns reference and sum; lanes 0 ... D / 8 - 1 hold channels 8 * lane ... of the unnormalised output.
-template <typename T, int D>
-__device__ __forceinline__ void paged_exact_row(const PagedAttnParams &p, int l, int hkv, int hq, int row, int b, int last, int prefix_halves, int h0, int h1, int lane,
+template <typename T, int D, class P>
+__device__ __forceinline__ void paged_exact_row(const P &p, int l, int hkv, int hq, int row, int b, int last, int prefix_halves, int h0, int h1, int lane,
                                                 float &m, float &sum, float (&o)[8])
 {
     constexpr int CL = D / 8, EPV = Elem<T>::EPV;
@@ -62,15 +65,16 @@ __device__ __forceinline__ void paged_exact_row(const PagedAttnParams &p, int l,
     auto at = [&](int x, bool values) -> const T * {   // row of key x, counted from half 0; null: not there
         if (x < 32 * prefix_halves) {
             if (x >= p.n_prefix) return nullptr;
-            const Strides &s = values ? p.s_pv : p.s_pk;
-            return static_cast<const T *>(values ? p.prefix_v : p.prefix_k) + l * s.layer + hkv * s.head + (int64_t)x * s.token;
+            const int64_t layer = values ? p.s_pv.layer : p.s_pk.layer, head = values ? p.s_pv.head : p.s_pk.head, token = values ? p.s_pv.token : p.s_pk.token;
+            return static_cast<const T *>(values ? p.prefix_v : p.prefix_k) + l * layer + hkv * head + (int64_t)x * token;
         }
         const int t = x - 32 * prefix_halves;
         if (t > last) return nullptr;
         const int page = page_of(p.batch, b, t);
         if (page < 0) return nullptr;
-        const PoolStrides &s = values ? p.s_v : p.s_k;
-        return static_cast<const T *>(values ? p.v : p.k) + l * s.layer + hkv * s.head + (int64_t)page * s.page + (int64_t)(t & ((1 << p.batch.log_page) - 1)) * s.token;
+        const int64_t layer = values ? p.s_v.layer : p.s_k.layer, head = values ? p.s_v.head : p.s_k.head, token = values ? p.s_v.token : p.s_k.token;
+        return static_cast<const T *>(values ? p.v : p.k) + l * layer + hkv * head + (int64_t)page * (values ? p.s_v.page : p.s_k.page) +
+               (int64_t)(t & ((1 << p.batch.log_page) - 1)) * token;
     };
     auto load8 = [](const T *src, float (&x)[8]) {
 #pragma unroll
@@ -129,8 +133,8 @@ __device__ __forceinline__ void paged_exact_row(const PagedAttnParams &p, int l,
 }
 
 // The row's result.  A row that saw nothing: 0 and -infinity.
-template <typename T, int D>
-__device__ __forceinline__ void paged_store_row(const PagedAttnParams &p, int l, int hq, int row, int lane, float m, float sum, const float (&o)[8])
+template <typename T, int D, class P>
+__device__ __forceinline__ void paged_store_row(const P &p, int l, int hq, int row, int lane, float m, float sum, const float (&o)[8])
 {
     constexpr int EPV = Elem<T>::EPV;
     const bool none = m == -INFINITY && sum == 0.f;
@@ -355,7 +359,7 @@ __device__ __forceinline__ PagedPlace paged_place(const PagedAttnParams &p, cons
     if (!p.slot_o) return to;
     const int64_t wave = blockIdx.x;
     if (to.kind == kWhole) {
-        const int64_t all = (int64_t)p.L * p.Hkv * p.G * p.batch.n_rows * (it.b < 0 ? 1 : 0);
+        const int64_t all = (int64_t)p.L * p.Hkv * p.G * p.batch.n_rows * (it.b < 0 ? p.prefix_part : 0);
         to.o = p.row_o + all * p.D;
         to.ml = p.row_ml + all * 2;
     } else if (to.kind == 0) {
@@ -424,5 +428,162 @@ __device__ __forceinline__ void paged_exact_segment(const PagedAttnParams &p, co
         }
     }
 }
+
+// ------------------------------------------------------------------------------------------ tiles of many rows
+// attn_mfma_kernel (suffix_attn.hip) with Keys::kPaged: a block is a tile of rows and a run of 64-key tiles of one sequence's pages, or of the prefix.
+struct PagedTileParams : PagedAttnParams {   // row_o null: rows go to `out`.  Over the prefix: k, v and their strides are the prefix's, one page
+    int32_t over_prefix;
+    int32_t n_items;
+    int32_t n_splits;      // runs
+    int32_t more_rows;     // packed rows that the sequences of the launch have more than
+    int32_t part;          // by rows: of run 0
+    int32_t slot_mask;     // slot of a token in its page
+    divisor_t by_LH, by_splits;
+    // what the kernel's other forms have
+    static constexpr int32_t window = 0, n_sinks = 0;
+    static constexpr Strides s_ks = {0, 0, 0}, s_vs = {0, 0, 0};
+};
+
+struct PagedTile {
+    int tile, b, first, n, len, tokens;   // tokens: that exist
+    int cap;
+    bool prefix;
+    __device__ __forceinline__ int last(int i) const { return prefix ? tokens - 1 : last_seen(len, n, i, cap); }
+    // Entry of token t < tokens, as a vector load.
+    template <class P>
+    __device__ __forceinline__ int entry(const P &p, int t) const
+    {
+        if (prefix) return 0;
+        int i = t >> p.batch.log_page;
+        asm volatile("" : "+v"(i));
+        return p.batch.table[(int64_t)b * p.batch.table_stride + i];
+    }
+    // Does one of the tokens t0 ... t1 - 1 that this thread looks at have an entry that is no page?
+    template <class P>
+    __device__ __forceinline__ bool odd_entries(const P &p, int t0, int t1, int tid, int threads) const
+    {
+        bool odd = false;
+        if (!prefix && t0 < t1)
+            for (int i = (t0 >> p.batch.log_page) + tid; i <= (t1 - 1) >> p.batch.log_page; i += threads)
+                odd |= (uint32_t)p.batch.table[(int64_t)b * p.batch.table_stride + i] >= (uint32_t)p.batch.n_pages;
+        return odd;
+    }
+};
+
+// The u-th tile of BM packed rows of a launch, the last rows of a sequence first; false: there is none.
+template <int BM, class P>
+__device__ __forceinline__ bool find_paged_tile(const P &p, int u, int lane, PagedTile &x)
+{
+    x.prefix = p.over_prefix != 0;
+    x.cap = p.batch.cap;
+    if (x.prefix) {
+        all_rows(p, x.first, x.n);
+        x.first = __builtin_amdgcn_readfirstlane(x.first);
+        x.n = __builtin_amdgcn_readfirstlane(x.n);
+        x.tile = u;
+        x.b = -1;
+        x.len = 0;
+        x.tokens = p.n_prefix;
+        return u * BM < x.n * p.G;
+    }
+    for (int c = 0; c < p.batch.n_seqs; c += 64) {
+        int first = 0, n = 0, len = 0;
+        if (c + lane < p.batch.n_seqs) {
+            sequence_rows(p.batch, c + lane, first, n);
+            len = sequence_len(p.batch, c + lane);
+        }
+        const int tiles = n * p.G > p.more_rows ? (n * p.G + BM - 1) / BM : 0;
+        int upto = tiles;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int y = __shfl_up(upto, off);
+            if (lane >= off) upto += y;
+        }
+        const int sum = __builtin_amdgcn_readlane(upto, 63);
+        if (u < sum) {
+            const int j = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > u));
+            x.tile = __builtin_amdgcn_readlane(upto, j) - 1 - u;
+            x.b = c + j;
+            x.first = __builtin_amdgcn_readlane(first, j);
+            x.n = __builtin_amdgcn_readlane(n, j);
+            x.len = __builtin_amdgcn_readlane(len, j);
+            x.tokens = min(x.len, x.cap);
+            return true;
+        }
+        u -= sum;
+    }
+    return false;
+}
+
+// Of a row's part: (part, layer, query head, row).
+template <class P>
+__device__ __forceinline__ int64_t paged_part_row(const P &p, int l, int hkv, int g, int row, int split)
+{
+    const int64_t Hq = (int64_t)p.Hkv * p.G;
+    return ((int64_t)(p.part + split) * p.L * Hq + l * Hq + hkv * p.G + g) * p.batch.n_rows + row;
+}
+
+// For the combine kernel: the rows whose first head lies in the tile are this kernel's.
+template <int BM, class P>
+__device__ __forceinline__ void paged_note_rows(const P &p, const PagedTile &x, int tid)
+{
+    if (!p.item_of || x.prefix || tid >= BM) return;
+    const int i = div_by(x.tile * BM + p.G - 1, p.by_G) + tid;
+    if (i < x.n && i * p.G < (x.tile + 1) * BM) p.item_of[2 * (x.first + i)] = p.row_o ? kWhole : kDirect;
+}
+
+// A tile whose rows see nothing in this run.
+template <int D, class P>
+__device__ __forceinline__ void paged_empty_tile(const P &p, const PagedTile &x, int l, int hkv, int split, int bm, int tid, int threads)
+{
+    for (int r = tid; r < bm; r += threads) {
+        const int packed = x.tile * bm + r, i = div_by(packed, p.by_G), g = packed - i * p.G;
+        if (i >= x.n) return;
+        if (p.row_o) {
+            const int64_t at = paged_part_row(p, l, hkv, g, x.first + i, split);
+            p.row_ml[2 * at] = -INFINITY;
+            p.row_ml[2 * at + 1] = 0.f;
+        } else {
+            bf16_t *out = static_cast<bf16_t *>(p.out) + l * p.s_o.layer + (int64_t)(hkv * p.G + g) * p.s_o.head + (int64_t)(x.first + i) * p.s_o.token;
+            for (int c = 0; c < D; c += 8) *reinterpret_cast<u32x4 *>(out + c) = u32x4{0, 0, 0, 0};
+            if (p.lse) p.lse[((int64_t)l * p.Hkv * p.G + hkv * p.G + g) * p.batch.n_rows + x.first + i] = -INFINITY;
+        }
+    }
+}
+
+// The whole block's work by the formula, over the halves h0 ... h1 - 1; all that it needs formed again (see exact_tile()).
+template <int D, int BM>
+__device__ __forceinline__ void paged_exact_tile(int h0, int h1, int split, int tid, int n_waves)
+{
+    typedef const __attribute__((address_space(4))) PagedTileParams ParamT;
+    ParamT *ptr = (ParamT *)__builtin_amdgcn_kernarg_segment_ptr();
+    int block = blockIdx.x;
+    asm volatile("" : "+s"(ptr));
+    asm volatile("" : "+s"(block));
+    ParamT &p = *ptr;
+    const int lane = tid & 63, unit = div_by(block, p.by_LH), lh = block - unit * (p.L * p.Hkv), l = div_by(lh, p.by_Hkv), hkv = lh - l * p.Hkv;
+    PagedTile x;
+    if (!find_paged_tile<BM>(p, div_by(unit, p.by_splits), lane, x)) return;
+#pragma unroll 1
+    for (int r = __builtin_amdgcn_readfirstlane(tid >> 6); r < BM; r += n_waves) {
+        const int packed = x.tile * BM + r, i = div_by(packed, p.by_G), g = packed - i * p.G;
+        if (i >= x.n) return;
+        float m, sum, o[8];
+        paged_exact_row<bf16_t, D>(p, l, hkv, hkv * p.G + g, x.first + i, x.b, x.prefix ? -1 : x.last(i), x.prefix ? (p.n_prefix + 31) / 32 : 0, h0, h1, lane, m, sum, o);
+        if (!p.row_o) {
+            paged_store_row<bf16_t, D>(p, l, hkv * p.G + g, x.first + i, lane, m, sum, o);
+            continue;
+        }
+        const int64_t at = paged_part_row(p, l, hkv, g, x.first + i, split);
+        if (lane < D / 8) {
+            f32x4 *po = reinterpret_cast<f32x4 *>(p.row_o + at * D + 8 * lane);
+            po[0] = f32x4{o[0], o[1], o[2], o[3]};
+            po[1] = f32x4{o[4], o[5], o[6], o[7]};
+        }
+        if (lane < 2) p.row_ml[at * 2 + lane] = lane ? sum : m;
+    }
+}
+
+int launch_paged_tiles(const PagedTileParams &p, int tile_rows, unsigned n_blocks, hipStream_t s);
 
 }  // namespace kvc

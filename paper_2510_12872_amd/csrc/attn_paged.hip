@@ -54,8 +54,8 @@ __global__ __launch_bounds__(256) void attn_paged_combine_kernel(const PagedAttn
         const int last = max(0, min(w1, p.n_waves - 1)), from = min(w0, last);
         return Parts{from, last - from + 1, packed & (p.tile_rows - 1), false};
     };
-    const int packed = p.item_of[2 * row + 1] * p.G + g;
-    const Parts own = parts_of(p.item_of[2 * row] + (int)((uint32_t)packed / (uint32_t)p.tile_rows), packed);
+    const int item = p.item_of[2 * row], packed = p.item_of[2 * row + 1] * p.G + g;
+    const Parts own = item < 0 ? Parts{item, p.tile_runs, 0, true} : parts_of(item + (int)((uint32_t)packed / (uint32_t)p.tile_rows), packed);
     if (own.wave == kDirect) return;
     Parts before = {0, p.prefix_runs, 0, true};
     if (apart && p.prefix_tiles) {
@@ -68,7 +68,7 @@ __global__ __launch_bounds__(256) void attn_paged_combine_kernel(const PagedAttn
         const Parts &x = b ? before : own;
         if (b) k -= own.count;
         if (x.whole) {
-            const int64_t at = flat + (b ? 1 + k : 0) * all;
+            const int64_t at = flat + (b ? p.prefix_part + k : k) * all;
             o = p.row_o + at * D;
             ml = p.row_ml + at * 2;
         } else {
@@ -126,10 +126,17 @@ __global__ __launch_bounds__(256) void attn_paged_combine_kernel(const PagedAttn
     if (p.lse && lane == 0) p.lse[flat] = none ? -INFINITY : M * p.scale + logf(sum);
 }
 
-// How a call is carried out: the sizes that depend on the model, the batch's host side and the prefix's length alone.
+// How a call is carried out: what depends on the model, the batch's host side and the prefix's length alone.
+//   Sequences of up to kFewRows packed rows go to the wavefront kernel, longer ones, if there may be any, to the tiles kernel; the prefix, for the rows of all of them, to one
+//   or the other.
+constexpr int kFewRows = 32;
+
 struct Plan {
-    int tile_rows, n_waves, prefix_tiles;
-    int64_t max_items, row_parts;   // parts by rows: [row_parts][layer, query head, row]
+    int tile_rows, n_waves, prefix_tiles;   // of the wavefront kernel
+    bool tiles;                             // is the tiles kernel launched for sequences
+    int seq_rows, seq_runs, prefix_rows, prefix_runs;   // its row tiles and runs; prefix_runs 0: it is not launched for the prefix
+    int64_t seq_units, prefix_units;        // its blocks per (layer, kv head)
+    int64_t max_items, row_parts;           // parts by rows: [row_parts][layer, query head, row]
     size_t bytes;
 };
 
@@ -139,11 +146,32 @@ Plan plan_of(const kvcomm_model &m, const kvcomm_batch &b, int n_prefix)
     const int G = m.n_q_heads / m.n_kv_heads, D = m.head_dim;
     const int64_t LH = (int64_t)m.n_layers * m.n_kv_heads, rows = (int64_t)b.n_rows * G;
     const int64_t most = b.starts ? (b.max_rows ? std::min<int64_t>(b.max_rows, b.n_rows) : b.n_rows) * G : G;
-    pl.tile_rows = D < 256 && (most > 16 || (n_prefix && rows > 16)) ? 32 : 16;
+    pl.tiles = most > kFewRows;
+    pl.tile_rows = D < 256 && (most > 16 || (n_prefix && rows > 16 && rows <= kFewRows)) ? 32 : 16;
     pl.n_waves = kChipCUs * paged_rows_waves(D, pl.tile_rows);
-    pl.prefix_tiles = n_prefix ? (int)((rows + pl.tile_rows - 1) / pl.tile_rows) : 0;
-    pl.max_items = pl.prefix_tiles + (b.starts ? rows / pl.tile_rows + b.n_seqs : (int64_t)b.n_seqs * ((G + pl.tile_rows - 1) / pl.tile_rows));
-    pl.row_parts = n_prefix ? 2 : 0;
+    pl.max_items = b.starts ? (pl.tiles ? (int64_t)b.n_seqs * (kFewRows / pl.tile_rows) : rows / pl.tile_rows + b.n_seqs) : (int64_t)b.n_seqs * ((G + pl.tile_rows - 1) / pl.tile_rows);
+    pl.seq_runs = 1;
+    if (pl.tiles) {
+        pl.seq_rows = D == 256 || rows < 512 * (int64_t)b.n_seqs ? 128 : 256;
+        const int64_t tiles = rows / pl.seq_rows + std::min<int64_t>(b.n_seqs, rows / (kFewRows + 1) + 1), reach = (int64_t)b.table_width * b.page_size;
+        // Keys are cut where the row tiles are few.  (The lengths lie on the device: by what the table reaches, and into runs of 512 at least.)
+        while (pl.seq_runs < kTileMaxSplits && tiles * LH * pl.seq_runs * 2 <= kChipCUs && reach >= 1024 * pl.seq_runs) pl.seq_runs *= 2;
+        pl.seq_units = tiles * pl.seq_runs;
+    }
+    if (n_prefix && rows <= kFewRows) {
+        pl.prefix_tiles = (int)((rows + pl.tile_rows - 1) / pl.tile_rows);
+        pl.max_items += pl.prefix_tiles;
+    } else if (n_prefix) {
+        pl.prefix_rows = D == 256 || rows <= 128 ? 128 : 256;
+        const int64_t tiles = (rows + pl.prefix_rows - 1) / pl.prefix_rows, keys = (n_prefix + 63) / 64;
+        double best = INFINITY;
+        for (int ns = 1; ns == 1 || (ns <= kTileMaxSplits && tiles * LH <= 2 * kChipCUs && ns * kMinRunTiles <= keys); ++ns) {
+            const double t = pl.prefix_rows == 128 && D < 256 ? attn_tiles128_us(m, tiles * LH, keys, ns) : attn_tiles_us(m, tiles * LH, pl.prefix_rows, keys, ns);
+            if (t < 0.95 * best) best = t, pl.prefix_runs = ns;
+        }
+        pl.prefix_units = tiles * pl.prefix_runs;
+    }
+    pl.row_parts = n_prefix ? pl.seq_runs + std::max(1, pl.prefix_runs) : pl.seq_runs > 1 ? pl.seq_runs : 0;
     pl.bytes = sizeof(float) * (size_t)(D + 2) * ((size_t)pl.n_waves * 2 * pl.tile_rows + (size_t)(pl.row_parts * LH * rows)) +
                sizeof(int32_t) * ((size_t)(2 * LH * pl.max_items) + 2 * (size_t)b.n_rows);
     return pl;
@@ -210,24 +238,52 @@ int paged_attn(const kvcomm_model *model, const kvcomm_tensor &q, const kvcomm_t
     }
     const Plan pl = plan_of(*model, *batch, n_prefix);
     const bool scratch = workspace && aligned16(workspace) && workspace_bytes >= pl.bytes;
+    const int64_t LH = (int64_t)p.L * p.Hkv;
+    const double most_blocks = 4294967296.0 / 512;   // a launch holds fewer than 2^32 threads
+    if ((double)pl.seq_units * LH >= most_blocks || (double)pl.prefix_units * LH >= most_blocks || pl.max_items > INT32_MAX / 2) return KVCOMM_EUNSUPPORTED;
     p.tile_rows = pl.tile_rows;
     p.n_waves = pl.n_waves;
-    p.most_rows = INT32_MAX;
+    p.most_rows = scratch && pl.tiles ? kFewRows : INT32_MAX;
     p.max_items = (int32_t)pl.max_items;
-    if (scratch) {
-        float *x = static_cast<float *>(workspace);
-        auto take = [&](int64_t n) { float *y = x; x += n; return y; };
-        p.slot_o = take((int64_t)pl.n_waves * 2 * pl.tile_rows * D);
-        p.row_o = take(pl.row_parts * rows * D);
-        p.slot_ml = take((int64_t)pl.n_waves * 2 * pl.tile_rows * 2);
-        p.row_ml = take(pl.row_parts * rows * 2);
-        p.items = reinterpret_cast<int32_t *>(take(2 * (int64_t)p.L * p.Hkv * pl.max_items));
-        p.item_of = reinterpret_cast<int32_t *>(x);
-        p.prefix_tiles = pl.prefix_tiles;
-    } else {
+    if (!scratch) {
         p.walked_prefix = (n_prefix + 31) / 32;
+        return launch_paged_rows(p, pl.tile_rows, s);
     }
-    if ((st = launch_paged_rows(p, pl.tile_rows, s)) || !scratch) return st;
+    float *x = static_cast<float *>(workspace);
+    auto take = [&](int64_t n) { float *y = x; x += n; return y; };
+    p.slot_o = take((int64_t)pl.n_waves * 2 * pl.tile_rows * D);
+    p.row_o = take(pl.row_parts * rows * D);
+    p.slot_ml = take((int64_t)pl.n_waves * 2 * pl.tile_rows * 2);
+    p.row_ml = take(pl.row_parts * rows * 2);
+    p.items = reinterpret_cast<int32_t *>(take(2 * LH * pl.max_items));
+    p.item_of = reinterpret_cast<int32_t *>(x);
+    p.prefix_tiles = pl.prefix_tiles;
+    p.prefix_runs = pl.prefix_runs;
+    p.prefix_part = pl.seq_runs;
+    p.tile_runs = pl.seq_runs;
+    auto tiles_of = [&](bool over_prefix) {
+        PagedTileParams t{};
+        static_cast<PagedAttnParams &>(t) = p;
+        t.over_prefix = over_prefix;
+        t.n_items = 1;
+        t.n_splits = over_prefix ? pl.prefix_runs : pl.seq_runs;
+        t.more_rows = kFewRows;
+        t.part = over_prefix ? p.prefix_part : 0;
+        t.slot_mask = over_prefix ? INT32_MAX : (1 << p.batch.log_page) - 1;
+        t.by_LH = make_divisor((uint32_t)LH);
+        t.by_splits = make_divisor((uint32_t)t.n_splits);
+        if (over_prefix) {
+            t.k = p.prefix_k;
+            t.v = p.prefix_v;
+            t.s_k = PoolStrides{p.s_pk.layer, p.s_pk.head, 0, p.s_pk.token};
+            t.s_v = PoolStrides{p.s_pv.layer, p.s_pv.head, 0, p.s_pv.token};
+        }
+        if (!over_prefix && !n_prefix && pl.seq_runs == 1) t.row_o = nullptr;
+        return launch_paged_tiles(t, over_prefix ? pl.prefix_rows : pl.seq_rows, (unsigned)((over_prefix ? pl.prefix_units : pl.seq_units) * LH), s);
+    };
+    if (pl.tiles && (st = tiles_of(false))) return st;
+    if (pl.prefix_runs && (st = tiles_of(true))) return st;
+    if ((st = launch_paged_rows(p, pl.tile_rows, s))) return st;
     const dim3 grid((unsigned)((rows + 3) / 4)), block(256);
     switch (D) {
         case 64: return launch(attn_paged_combine_kernel<bf16_t, 64>, grid, block, 0, s, p);

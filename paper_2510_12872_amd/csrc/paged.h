@@ -19,7 +19,8 @@ struct Batch {
 };
 
 // Rows of a sequence, and its tokens.  Whatever starts and lens hold, rows stay in [0, n_rows).
-__device__ __forceinline__ void sequence_rows(const Batch &p, int b, int &first, int &n)
+template <class B>   // Batch, in any address space
+__device__ __forceinline__ void sequence_rows(const B &p, int b, int &first, int &n)
 {
     if (!p.starts) {
         first = b;
@@ -29,7 +30,8 @@ __device__ __forceinline__ void sequence_rows(const Batch &p, int b, int &first,
     first = max(0, min(p.starts[b], p.n_rows));
     n = max(0, min(p.starts[b + 1], p.n_rows) - first);
 }
-__device__ __forceinline__ int sequence_len(const Batch &p, int b) { return max(0, p.lens[b]); }
+template <class B>
+__device__ __forceinline__ int sequence_len(const B &p, int b) { return max(0, p.lens[b]); }
 
 // Sequence of a row, -1: none.  Each lane of the wavefront may ask for another row.
 __device__ __forceinline__ int sequence_of(const Batch &p, int row, int lane)
@@ -58,7 +60,8 @@ __device__ __forceinline__ int sequence_of(const Batch &p, int row, int lane)
 }
 
 // Page of token t >= 0 of the sequence, -1: none.
-__device__ __forceinline__ int page_of(const Batch &p, int b, int t)
+template <class B>
+__device__ __forceinline__ int page_of(const B &p, int b, int t)
 {
     if (t >= p.cap) return -1;
     const int e = p.table[(int64_t)b * p.table_stride + (t >> p.log_page)];

@@ -46,6 +46,7 @@
 
 #include "attn_exact.h"
 #include "attn_host.h"
+#include "attn_paged.h"
 
 namespace {
 
@@ -97,13 +98,15 @@ __device__ __forceinline__ void exact_tile()
 // rows again by attn_exact_rows(), because a hidden key's value may have been multiplied by its probability 0.
 // FORM: wavefronts per SIMD + form(KEYS) (one argument for both: a whole cache's kernels keep the names that the profiles have).
 constexpr int form(Keys keys) { return 16 * (int)keys; }
+template <int FORM>
+using ParamsOf = std::conditional_t<FORM / 16 == (int)Keys::kPaged, PagedTileParams, AttnParams>;
 template <int D, int NW, int FORM, bool PERSIST, bool SPLIT>
-__global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const AttnParams p_arg)
+__global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const ParamsOf<FORM> p_arg)
 {
     // PERSIST reads the parameters through an opaque pointer to the kernel-argument segment, once per item:
     // they are then re-loaded (scalar loads) for every item instead of being held in scalar registers for the
     // whole kernel, which the register budget does not allow.
-    using ParamT = std::conditional_t<PERSIST, const __attribute__((address_space(4))) AttnParams, const AttnParams>;
+    using ParamT = std::conditional_t<PERSIST, const __attribute__((address_space(4))) ParamsOf<FORM>, const ParamsOf<FORM>>;
     ParamT *p_ptr;
     if constexpr (PERSIST)
         p_ptr = (ParamT *)__builtin_amdgcn_kernarg_segment_ptr();
@@ -113,8 +116,10 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     constexpr Keys KEYS = (Keys)(FORM / 16);
     constexpr bool kWindow = KEYS == Keys::kWindow;
     constexpr bool kFp4 = KEYS == Keys::kFp4;
-    constexpr bool kChecked = kWindow || kFp4;   // blocks whose results are not all finite compute their rows again
+    constexpr bool kPaged = KEYS == Keys::kPaged;
+    constexpr bool kChecked = kWindow || kFp4 || kPaged;   // blocks whose results are not all finite compute their rows again
     static_assert(!(PERSIST && kChecked), "the persistent form reads its parameters in its own way");
+    static_assert(!kPaged || SPLIT, "a tile of a batch is a run of its keys, if only of all of them");
     using Cache = std::conditional_t<kFp4, uint8_t, bf16_t>;
     constexpr int NF = D / 16;       // K operands of a sub-step (contraction step, key half), V^T operands (16 channels)
     constexpr int BM = 32 * NW;      // query rows per block (32 per wavefront)
@@ -165,24 +170,40 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lane = tid & 63, n = lane & 15, g4 = lane >> 4;
     int split = 0;
-    if constexpr (SPLIT) {
+    [[maybe_unused]] PagedTile seq = {};
+    if constexpr (kPaged) {
+        // (layer, kv head) pairs fastest: where they are a multiple of 8, the row tiles of one run on one XCD here, too
+        const int unit = div_by(blockIdx.x, p.by_LH), run = div_by(unit, p.by_splits);
+        split = unit - run * p.n_splits;
+        if (!find_paged_tile<BM>(p, run, lane, seq)) return;   // the whole block
+        logical = blockIdx.x - unit * (p.L * p.Hkv);
+        if (logical == 0 && split == 0) paged_note_rows<BM>(p, seq, tid);
+    } else if constexpr (SPLIT) {
         const int rest = div_by(logical, p.by_splits);
         split = logical - rest * p.n_splits;
         logical = rest;
     }
-    const int lh = div_by(logical, p.by_row_tiles);
-    const int rt = p.n_row_tiles - 1 - (logical - lh * p.n_row_tiles);  // longest rows first
+    auto row_tiles = [&]() __attribute__((always_inline)) -> int { if constexpr (kPaged) return 1; else return p.n_row_tiles; };
+    const int lh = [&]() __attribute__((always_inline)) -> int { if constexpr (kPaged) return logical; else return div_by(logical, p.by_row_tiles); }();
+    const int rt = kPaged ? seq.tile : row_tiles() - 1 - (logical - lh * row_tiles());  // longest rows first
     const int l = div_by(lh, p.by_Hkv), hkv = lh - l * p.Hkv;
+    // Queries of the tile's (layer, head) group, the first one's position and the cache's length.
+    auto tq_ = [&]() __attribute__((always_inline)) -> int { if constexpr (kPaged) return seq.n; else return p.tq; };
+    auto ctx_ = [&]() __attribute__((always_inline)) -> int { if constexpr (kPaged) return 0; else return p.n_ctx; };
 
     const Cache *kb_ = static_cast<const Cache *>(p.k) + l * p.s_k.layer + hkv * p.s_k.head;
     const Cache *vb_ = static_cast<const Cache *>(p.v) + l * p.s_v.layer + hkv * p.s_v.head;
 
     // Every wavefront of the block walks the same tiles (one barrier per 64-key tile); the causal
     // mask is applied from the first 32-key sub-step that is partly hidden from some query of the block.
-    const int wg_imax = min(p.tq - 1, div_by(rt * BM + BM - 1, p.by_G));
-    const int wg_imin = min(p.tq - 1, div_by(rt * BM, p.by_G));
-    const int all_tiles = (p.n_ctx + wg_imax + 1 + 63) / 64;
-    const int first_hidden = (p.n_ctx + wg_imin) / 64 + 1;
+    int wg_imax = min(tq_() - 1, div_by(rt * BM + BM - 1, p.by_G));
+    int wg_imin = min(tq_() - 1, div_by(rt * BM, p.by_G));
+    if constexpr (kPaged) {   // from here on, the last tokens that those rows see (-1: none)
+        wg_imax = max(-1, seq.last(wg_imax));
+        wg_imin = max(-1, seq.last(wg_imin));
+    }
+    const int all_tiles = (ctx_() + wg_imax + 1 + 63) / 64;
+    const int first_hidden = (ctx_() + wg_imin) / 64 + 1;
     WindowUnits wu = {0, 0, 2 * all_tiles, 0, 0};   // in halves of tiles
     if constexpr (kWindow) wu = window_units(p, wg_imin, wg_imax, 32);
     const int walk_tiles = kWindow ? (wu.count + 1) / 2 : all_tiles;   // (a half too many lies behind the last query)
@@ -193,7 +214,12 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     const int tile0 = SPLIT ? bound(split) : 0;
     const int n_tiles = SPLIT ? bound(split + 1) - tile0 : walk_tiles;
     const int sink_halves = kWindow ? max(0, wu.sinks - 2 * tile0) : 0;   // of this run
-    if constexpr (SPLIT) {
+    if constexpr (kPaged) {
+        if (n_tiles <= 0) {   // the whole block: nothing to be seen in this run
+            paged_empty_tile<D>(p, seq, l, hkv, split, BM, tid, 64 * NW);
+            return;
+        }
+    } else if constexpr (SPLIT) {
         if (n_tiles <= 0) {   // the whole block: this run is empty
             if (lane < 32 && div_by(rt * BM + wave * 32 + lane, p.by_G) < p.tq) {
                 const int64_t part = ((int64_t)(lh * p.n_row_tiles + rt) * NW + wave) * p.n_splits + split;
@@ -207,15 +233,18 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     }
     // Half h of the run begins at key origin + 32 * h; a half of the sinks lies 32 * gap keys before that.
     const int origin = 64 * tile0 + 32 * wu.gap;
-    if constexpr (SPLIT || kWindow) {
+    if constexpr (!kPaged && (SPLIT || kWindow)) {
         kb_ += (int64_t)origin * p.s_k.token;
         vb_ += (int64_t)origin * p.s_v.token;
     }
     auto half_shift = [&](int h) __attribute__((always_inline)) -> int { return kWindow && h < sink_halves ? -32 * wu.gap : 0; };
     // Context length and cache length counted from key `origin` (n_ctx_() may be negative; without a window every query of
     // the tile still sees key 0 of the run).
-    auto n_ctx_ = [&]() __attribute__((always_inline)) -> int { return SPLIT || kWindow ? p.n_ctx - origin : p.n_ctx; };
-    auto N_ = [&]() __attribute__((always_inline)) -> int { return SPLIT || kWindow ? p.N - origin : p.N; };
+    auto n_ctx_ = [&]() __attribute__((always_inline)) -> int { return SPLIT || kWindow ? ctx_() - origin : ctx_(); };
+    auto N_ = [&]() __attribute__((always_inline)) -> int {
+        if constexpr (kPaged) return seq.tokens - origin;
+        else return SPLIT || kWindow ? p.N - origin : p.N;
+    };
     const int n_sub = 2 * n_tiles;
     const int sub_unmasked = (n_ctx_() + wg_imin + 1) / 32;  // sub-steps [0, sub_unmasked) are visible to all queries
 
@@ -255,8 +284,31 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     // still fall behind the end steps its offset back by whole rows.
     const int lq = lane / KCH;  // this lane's row inside a load
     const uint32_t k_row_bytes = (uint32_t)(p.s_k.token * 2), v_row_bytes = (uint32_t)(p.s_v.token * 2);
+    // Pages: every group of RW rows of a wavefront, from a multiple of RW on, lies in one (of 16 tokens at least).  Its entry of the table is requested when the
+    // group before it is, as a vector load, whose arrival the barrier of the tile awaits anyway; one that is no page is read as page 0, and the block
+    // computed again.
+    static_assert(!kPaged || RW <= 16, "");
+    [[maybe_unused]] int k_entry = 0, v_entry = 0;   // of the groups that are loaded next
+    [[maybe_unused]] auto k_group = [&](int key0) __attribute__((always_inline)) -> int { return key0 + 32 * (wave / (NW / 2)) + (wave % (NW / 2)) * RW; };   // first rows,
+    [[maybe_unused]] auto v_group = [&](int tile) __attribute__((always_inline)) -> int { return 64 * tile + wave * RW; };   // counted from `origin`
+    [[maybe_unused]] auto entry_of = [&](int row0) __attribute__((always_inline)) -> int {
+        if constexpr (kPaged) return seq.entry(p, origin + min(row0, N_() - 1));
+        return 0;
+    };
+    [[maybe_unused]] auto page_row = [&](const unsigned char *bytes, int64_t page_stride, int64_t tok_stride, int entry, int row) __attribute__((always_inline)) -> const unsigned char * {
+        if constexpr (kPaged) {
+            const int page = __builtin_amdgcn_readfirstlane(entry);
+            return bytes + ((int64_t)((uint32_t)page < (uint32_t)p.batch.n_pages ? page : 0) * page_stride + (int64_t)((origin + row) & p.slot_mask) * tok_stride) * 2;
+        }
+        return bytes;
+    };
     auto load_rows = [&](const unsigned char *bytes, int64_t tok_stride, uint32_t row_bytes, int row0, uint32_t voff,
-                         const lds_byte *dst, [[maybe_unused]] bool sink) __attribute__((always_inline)) {
+                         const lds_byte *dst, [[maybe_unused]] bool sink, [[maybe_unused]] int64_t page_stride = 0, [[maybe_unused]] int entry = 0) __attribute__((always_inline)) {
+        if constexpr (kPaged) {
+            const int row0c = min(row0, N_() - 1), excess = max(lq - (N_() - 1 - row0c), 0);
+            dma16_sbase(page_row(bytes, page_stride, tok_stride, entry, row0c), voff - (uint32_t)excess * row_bytes, dst);
+            return;
+        }
         if constexpr (kWindow) {   // likewise rows that no query sees: the nearest one that some query sees instead
             const int lo = sink ? -origin : wu.oldest - origin, hi = sink ? wu.sink_end - 1 - origin : N_() - 1;
             const int row0c = max(lo, min(row0, hi));
@@ -268,6 +320,8 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
         const int excess = max(lq - (N_() - 1 - row0c), 0);  // rows this lane would overshoot by
         dma16_sbase(bytes + (int64_t)row0c * tok_stride * 2, voff - (uint32_t)excess * row_bytes, dst);
     };
+    auto page_of_k = [&]() __attribute__((always_inline)) -> int64_t { if constexpr (kPaged) return p.s_k.page; else return 0; };
+    auto page_of_v = [&]() __attribute__((always_inline)) -> int64_t { if constexpr (kPaged) return p.s_v.page; else return 0; };
     auto load_k64 = [&](int key0) __attribute__((always_inline)) {
         const int h = key0 / 32 + wave / (NW / 2);
         if (h >= n_sub) return;  // wavefront-uniform
@@ -275,14 +329,14 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
 #pragma unroll
         for (int it = 0; it < LPT; ++it)
             load_rows(kbytes, p.s_k.token, k_row_bytes, 32 * h + half_shift(h) + rbase + it * RPL, ld_koff[it],
-                      kring + (h & 3) * HALFB + (rbase + it * RPL) * ROWB, h < sink_halves);
+                      kring + (h & 3) * HALFB + (rbase + it * RPL) * ROWB, h < sink_halves, page_of_k(), k_entry);
     };
     auto load_v64 = [&](int tile) __attribute__((always_inline)) {
         if (tile >= n_tiles) return;
 #pragma unroll
         for (int it = 0; it < LPT; ++it)
             load_rows(vbytes, p.s_v.token, v_row_bytes, 64 * tile + half_shift(2 * tile + wave / (NW / 2)) + wave * RW + it * RPL, ld_voff[it],
-                      vbuf + (tile & 1) * TILEB + (wave * RW + it * RPL) * ROWB, 2 * tile + wave / (NW / 2) < sink_halves);
+                      vbuf + (tile & 1) * TILEB + (wave * RW + it * RPL) * ROWB, 2 * tile + wave / (NW / 2) < sink_halves, page_of_v(), v_entry);
     };
     // ---- 4-bit caches: a thread holds the codes of CT channels of one row of a 64-key tile (NW threads a row) and their scales, requested a tile ahead
     // of their turn, decodes them at the start of a tile and stores them where the direct loads would have put them.
@@ -351,11 +405,23 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
         store_k(0, k0);
         store_k(1, k1);
         store_v(0, v0);
+    } else if constexpr (kPaged) {
+        const int k1 = entry_of(k_group(64)), k2 = entry_of(k_group(128)), v1 = entry_of(v_group(1));
+        k_entry = entry_of(k_group(0));
+        v_entry = entry_of(v_group(0));
+        load_k64(0);
+        load_v64(0);
+        k_entry = k1;
+        load_k64(64);
+        k_entry = k2;
+        v_entry = v1;
     } else {
     load_k64(0);    // halves 0, 1
     load_k64(64);   // halves 2, 3
     load_v64(0);
     }
+    [[maybe_unused]] bool no_page = false;   // some entry of the run is no page
+    if constexpr (kPaged) no_page = seq.odd_entries(p, 64 * tile0, min(seq.tokens, 64 * (tile0 + n_tiles)), tid, 64 * NW);
     // This lane's two query columns, n and 16 + n of the wavefront's 32: row r = i * G + g of the (layer, kv head) group.
     int qi[2];
     bf16x8 qf[2][NF / 2];
@@ -363,9 +429,10 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     for (int h = 0; h < 2; ++h) {
         const int r_row = rt * BM + wave * 32 + 16 * h + n;
         const int i_row = div_by(r_row, p.by_G);
-        qi[h] = min(i_row, p.tq - 1);
+        qi[h] = min(i_row, tq_() - 1);
         const int hq = hkv * p.G + r_row - i_row * p.G;
-        const bf16_t *qrow = static_cast<const bf16_t *>(p.q) + l * p.s_q.layer + (int64_t)(uint32_t)hq * p.s_q.head + (int64_t)(uint32_t)qi[h] * p.s_q.token;
+        const bf16_t *qrow = static_cast<const bf16_t *>(p.q) + l * p.s_q.layer + (int64_t)(uint32_t)hq * p.s_q.head + (int64_t)(uint32_t)(seq.first + qi[h]) * p.s_q.token;
+        if constexpr (kPaged) qi[h] = seq.last(qi[h]);   // (the last token that it sees, as a distance from the tokens' first)
 #pragma unroll
         for (int ks = 0; ks < NF / 2; ++ks) qf[h][ks] = as_bf16x8(load16(qrow + ks * 32 + g4 * 8));
     }
@@ -387,8 +454,12 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     const uint32_t kdst_a = __builtin_amdgcn_readfirstlane(k_rows + (0 + wave / (NW / 2)) * HALFB);
     const uint32_t kdst_b = __builtin_amdgcn_readfirstlane(k_rows + (2 + wave / (NW / 2)) * HALFB);
     const uint32_t vdst = __builtin_amdgcn_readfirstlane(lds0 + 4 * HALFB + wave * RW * ROWB);
-    auto load_kv_next = [&](uint32_t kdst, auto vb) __attribute__((always_inline)) {
+    auto load_kv_next = [&](uint32_t kdst, auto vb, [[maybe_unused]] int t_now) __attribute__((always_inline)) {
         constexpr int VB = decltype(vb)::value;  // V buffer, a literal
+        if constexpr (kPaged) {   // of tile t_now
+            kp = page_row(kbytes, page_of_k(), p.s_k.token, k_entry, k_group(64 * t_now + 128));
+            vp = page_row(vbytes, page_of_v(), p.s_v.token, v_entry, v_group(t_now + 1));
+        }
         static_for<0, LPT>([&](auto it) __attribute__((always_inline)) {
             constexpr int I = decltype(it)::value;
             if (I > 0) kp += k_rpl;
@@ -615,6 +686,12 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
     // starting at t forms the exponentials of sub-steps up to 2t+4 and loads keys up to 64t + 255.
     const int t_safe = N_() >= 256 ? (N_() - 128) / 64 : 0;
     const int t_plain = max(0, min(min((sub_unmasked - 1) >> 1, t_last), t_safe));
+    [[maybe_unused]] auto next_entries = [&](int t) __attribute__((always_inline)) {   // what tile t begins to load
+        if constexpr (kPaged) {
+            k_entry = entry_of(k_group(64 * t + 128));
+            v_entry = entry_of(v_group(t + 1));
+        }
+    };
     // Two tiles (four sub-steps) per trip so that ring slots and buffers are compile-time constants.
     auto tile_pair = [&](int t, auto plain) __attribute__((always_inline)) {
         constexpr bool PLAIN = decltype(plain)::value;
@@ -622,22 +699,24 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
         if constexpr (kFp4) {
             next_rows(t, 0);
         } else if (PLAIN) {
-            load_kv_next(kdst_a, template_int<1>{});  // K halves 2t+4, 2t+5, V tile t+1
+            load_kv_next(kdst_a, template_int<1>{}, t);  // K halves 2t+4, 2t+5, V tile t+1
         } else {
             load_k64(64 * t + 128);
             load_v64(t + 1);
         }
+        next_entries(t + 1);
         step(2 * t, u0, T_{}, T_{}, M_{});
         step(2 * t + 1, u1, T_{}, T_{}, M_{});
         tile_barrier();
         if constexpr (kFp4) {
             next_rows(t + 1, 1);
         } else if (PLAIN) {
-            load_kv_next(kdst_b, template_int<0>{});  // K halves 2t+6, 2t+7, V tile t+2
+            load_kv_next(kdst_b, template_int<0>{}, t + 1);  // K halves 2t+6, 2t+7, V tile t+2
         } else {
             load_k64(64 * t + 192);
             load_v64(t + 2);
         }
+        next_entries(t + 2);
         step(2 * t + 2, u2, T_{}, T_{}, M_{});
         step(2 * t + 3, u3, T_{}, T_{}, M_{});
         tile_barrier();
@@ -678,12 +757,33 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
             for (int i = 0; i < 4 * NF; ++i) zero = fmaf(o[h][i / 4][i % 4], 0.f, zero);
             odd |= state_is_odd(zero, m[h], query_sum(lsum[h]));
         }
-        if (__syncthreads_or(odd)) {
-            exact_tile<D, NW, SPLIT, KEYS>();
+        if (__syncthreads_or(odd || no_page)) {
+            if constexpr (kPaged)
+                paged_exact_tile<D, BM>(2 * tile0, 2 * (tile0 + n_tiles), split, tid, NW);
+            else
+                exact_tile<D, NW, SPLIT, KEYS>();
             return;
         }
     }
-    if constexpr (SPLIT) {
+    if constexpr (kPaged) {
+        if (p.row_o) {   // ---- a part of each row: accumulators as they are, reference and row sum
+            const int lane_e = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+            const int n_e = lane_e & 15, g_e = lane_e >> 4;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float ltot = query_sum(lsum[h]);
+                const int r_row = rt * BM + wave * 32 + 16 * h + n_e, i = div_by(r_row, p.by_G);
+                if (i < seq.n) {
+                    const int64_t flat = paged_part_row(p, l, hkv, r_row - i * p.G, seq.first + i, split);
+                    float *po = p.row_o + flat * D + 4 * g_e;
+#pragma unroll
+                    for (int db = 0; db < NF; ++db) *reinterpret_cast<f32x4 *>(po + 16 * db) = o[h][db];
+                    if (g_e < 2) p.row_ml[flat * 2 + g_e] = g_e ? ltot : m[h];
+                }
+            }
+            return;
+        }
+    } else if constexpr (SPLIT) {
         // ---- epilogue of a split: accumulators as they are (256-byte runs per store), reference and row sum.
         const int64_t part = ((int64_t)(lh * p.n_row_tiles + rt) * NW + wave) * p.n_splits + split;
         const int lane_e = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
@@ -723,11 +823,12 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
         for (int h = 0; h < 2; ++h) {
             const int row = 16 * h + n_e, r_row = rt * BM + wave * 32 + row;
             const uint32_t qi_e = (uint32_t)div_by(r_row, p.by_G), hq_e = (uint32_t)(hkv * p.G + r_row) - qi_e * (uint32_t)p.G;
-            const bool valid = qi_e < (uint32_t)p.tq;
-            bf16_t *orow = static_cast<bf16_t *>(p.out) + l * p.s_o.layer + (int64_t)hq_e * p.s_o.head + (int64_t)qi_e * p.s_o.token;
+            const bool valid = qi_e < (uint32_t)tq_();
+            bf16_t *orow = static_cast<bf16_t *>(p.out) + l * p.s_o.layer + (int64_t)hq_e * p.s_o.head + (int64_t)(seq.first + qi_e) * p.s_o.token;
             const float ltot = query_sum(lsum[h]);
             if (g_e == 0) ptab[row] = valid ? (uint64_t)(uintptr_t)orow : 0;
-            const float inv = 1.f / ltot;
+            const bool none = kPaged && m[h] == -INFINITY && ltot == 0.f;
+            const float inv = none ? 0.f : 1.f / ltot;
 #pragma unroll
             for (int db = 0; db < NF; ++db) {
                 u32x2 w;
@@ -735,8 +836,12 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Att
                 w[1] = pack_bf16x2(o[h][db][2] * inv, o[h][db][3] * inv);
                 *reinterpret_cast<u32x2 *>(stage + row * ROWB + ((4 * db + g_e) ^ (row & FM)) * 8) = w;
             }
-            if (p.lse && g_e == 0 && valid)
-                p.lse[((int64_t)l * p.Hkv * p.G + hq_e) * p.tq + qi_e] = m[h] * p.scale + logf(ltot);
+            if (p.lse && g_e == 0 && valid) {
+                if constexpr (kPaged)
+                    p.lse[((int64_t)l * p.Hkv * p.G + hq_e) * p.batch.n_rows + seq.first + qi_e] = none ? -INFINITY : m[h] * p.scale + logf(ltot);
+                else
+                    p.lse[((int64_t)l * p.Hkv * p.G + hq_e) * p.tq + qi_e] = m[h] * p.scale + logf(ltot);
+            }
         }
         // the reads below touch what other lanes of this wavefront wrote: LDS operations of a wavefront complete in order
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -820,6 +925,16 @@ int suffix_attn(const kvcomm_model *model, kvcomm_tensor q, kvcomm_tensor cache_
 }  // namespace
 
 namespace kvc {
+
+int launch_paged_tiles(const PagedTileParams &p, int tile_rows, unsigned n_blocks, hipStream_t s)
+{
+    constexpr int F = form(Keys::kPaged);
+    const dim3 grid(n_blocks);
+    if (p.D == 256) return launch(attn_mfma_kernel<256, 4, 1 + F, false, true>, grid, dim3(256), 0, s, p);
+    if (tile_rows == 128)
+        return p.D == 64 ? launch(attn_mfma_kernel<64, 4, 2 + F, false, true>, grid, dim3(256), 0, s, p) : launch(attn_mfma_kernel<128, 4, 2 + F, false, true>, grid, dim3(256), 0, s, p);
+    return p.D == 64 ? launch(attn_mfma_kernel<64, 8, 2 + F, false, true>, grid, dim3(512), 0, s, p) : launch(attn_mfma_kernel<128, 8, 2 + F, false, true>, grid, dim3(512), 0, s, p);
+}
 
 int launch_attn(const kvcomm_model &m, AttnParams &p, AttnPlan plan, const AttnPlan &uncut, int max_blocks, void *workspace, size_t workspace_bytes, hipStream_t s)
 {
