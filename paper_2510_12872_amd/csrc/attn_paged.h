@@ -32,6 +32,7 @@ struct PagedAttnParams {
     int32_t tile_runs;       // runs of a sequence that the tiles kernel takes
     int32_t tile_rows;
     int32_t n_waves;         // runs of the axis
+    float per_wave;          // 1 / n_waves and a little
     int32_t most_rows;       // packed rows of the sequences that the launch takes
     int32_t max_items;       // of a (layer, kv head) on the axis, at most
     // Scratch, or null: then an item is the work of the wavefront in whose run it begins.  A row's part: D outputs; reference and sum.
@@ -40,6 +41,21 @@ struct PagedAttnParams {
     int32_t *items;            // [layer, kv head][max_items][2]: first and last wavefront of an item; kDirect, kWhole
     int32_t *item_of;          // [n_rows][2]: item of its sequence's first tile, its number in the sequence; kDirect, kWhole: the tiles kernel's
 };
+// A wavefront kernel's parameters, where they are used: what is read once per item is loaded there and not kept in (or spilled from) scalar registers all along.
+typedef const __attribute__((address_space(4))) PagedAttnParams PagedArgs;
+__device__ __forceinline__ PagedArgs &paged_args()
+{
+    PagedArgs *p = (PagedArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *p;
+}
+__device__ __forceinline__ void await_paged_args(PagedArgs &p)   // see await_args(): a word of each 64-byte line
+{
+    auto word = [&](int line) { return *(const __attribute__((address_space(4))) uint32_t *)((const __attribute__((address_space(4))) char *)&p + 64 * line); };
+    constexpr int last = (sizeof(PagedAttnParams) - 1) / 64;
+    static_assert(last >= 5 && last <= 7, "six to eight lines");
+    await_args(word(0), word(1), word(2), word(3), word(4), word(5), word(last - 1), word(last));
+}
 enum : int32_t { kDirect = -1, kWhole = -2 };   // its rows lie in `out`; in row_o
 
 // The rows of all sequences.
@@ -152,6 +168,10 @@ __device__ __forceinline__ void paged_store_row(const P &p, int l, int hq, int r
 }
 
 // ------------------------------------------------------------------------------------------ the walk
+#ifndef KMIN
+#define KMIN 1
+#endif
+constexpr int kPagedMinRun = KMIN;   // halves of a wavefront's run at least
 typedef const __attribute__((address_space(4))) int32_t const_int;   // read through the scalar cache (whole-wavefront values)
 __device__ __forceinline__ const_int *scalar(const int32_t *x) { return (const_int *)(uintptr_t)x; }
 
@@ -166,103 +186,99 @@ struct PagedItem {
     int index;          // among the items of lh
 };
 
+// Sum over the lanes up to each one's.
+__device__ __forceinline__ int wave_scan(int x)
+{
+    auto add = [](int v, auto ctrl, auto rows) { return v + __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false); };
+    x = add(x, std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});   // from one, two, four, eight lanes before in each row of sixteen
+    x = add(x, std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+    x = add(x, std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+    x = add(x, std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+    x = add(x, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // a row's last lane to the second and the fourth row,
+    x = add(x, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // the second row's last to the third and the fourth
+    return x;
+}
+// x / d, both positive, the quotient below 2^31
+__device__ __forceinline__ int quotient(int64_t x, int64_t d)
+{
+    int64_t q = (int64_t)((double)x * __builtin_amdgcn_rcp((double)d));   // (next to it at least)
+    while (q * d > x) --q;
+    while ((q + 1) * d <= x) ++q;
+    return (int)q;
+}
+
+// The sizes are such that what one (layer, kv head) has on the axis fits 31 bits, and a run, too (plan_of()).
 template <int TR>   // packed rows of a tile
 struct PagedWalk {
-    const PagedAttnParams &p;
     const int lane;
-    int64_t width = 0;   // halves of a (layer, kv head) on the axis
-    int64_t run = 0;     // of a wavefront
+    int width = 0;   // halves of a (layer, kv head) on the axis
+    int run = 0;     // of a wavefront
     PagedItem item = {};
 
-    __device__ __forceinline__ PagedWalk(const PagedAttnParams &p, int lane) : p(p), lane(lane) {}
+    __device__ __forceinline__ explicit PagedWalk(int lane) : lane(lane) {}
 
-    __device__ __forceinline__ int tiles_of(int n) const
+    __device__ __forceinline__ static int tiles_of(PagedArgs &p, int n)
     {
         const int rows = n * p.G;
         return rows <= p.most_rows ? (rows + TR - 1) / TR : 0;
     }
-    __device__ __forceinline__ int count_of(int len) const { return max(1, p.walked_prefix + (min(len, p.batch.cap) + 31) / 32); }
-    __device__ __forceinline__ int prefix_count() const { return (p.n_prefix + 31) / 32; }
+    __device__ __forceinline__ static int count_of(PagedArgs &p, int len) { return max(1, p.walked_prefix + (min(len, p.batch.cap) + 31) / 32); }
+    __device__ __forceinline__ static int prefix_count(PagedArgs &p) { return (p.n_prefix + 31) / 32; }
 
     // Halves of the sequences c ... c + 63 up to each lane's, and that lane's row tiles.
-    __device__ __forceinline__ int64_t scan(int c, int &tiles) const
+    __device__ __forceinline__ int scan(PagedArgs &p, int c, int &tiles) const
     {
         const int b = c + lane;
-        int64_t x = 0;
+        int x = 0;
         tiles = 0;
         if (b < p.batch.n_seqs) {
             int first, n;
             sequence_rows(p.batch, b, first, n);
-            tiles = tiles_of(n);
-            x = (int64_t)tiles * count_of(sequence_len(p.batch, b));
+            tiles = tiles_of(p, n);
+            x = tiles * count_of(p, sequence_len(p.batch, b));
         }
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int64_t y = __shfl_up(x, off);
-            if (lane >= off) x += y;
-        }
-        return x;
-    }
-    __device__ __forceinline__ static int64_t uniform(int64_t x)
-    {
-        return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x) | (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32);
-    }
-    __device__ __forceinline__ static int64_t of_lane(int64_t x, int lane)
-    {
-        return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32);
-    }
-    // x / d for 0 <= x < 2^53, d > 0
-    __device__ __forceinline__ static int64_t quotient(int64_t x, int64_t d)
-    {
-        int64_t q = (int64_t)((double)x / (double)d);
-        q -= q * d > x;
-        return q + ((q + 1) * d <= x);
+        return wave_scan(x);
     }
 
-    // The first item that wavefront `wave` works on, and its halves of it; false: none.  min_run: halves of a run at least.
-    __device__ __forceinline__ bool begin(int wave, int min_run, int64_t &pos, int64_t &end, int &h0)
+    // The first item that wavefront `wave` works on, and its halves of it; false: none.
+    __device__ __forceinline__ bool begin(int wave, int64_t &pos, int64_t &end, int &h0)
     {
-        const int64_t ahead = (int64_t)p.prefix_tiles * prefix_count();
+        PagedArgs &p = paged_args();
+        const int ahead = p.prefix_tiles * prefix_count(p);
         int tiles;
-        int64_t upto = scan(0, tiles);   // (kept: most batches have no more)
-        width = ahead + of_lane(upto, 63);
+        int upto = scan(p, 0, tiles);   // (kept: most batches have no more)
+        width = ahead + __builtin_amdgcn_readlane(upto, 63);
         for (int c = 64; c < p.batch.n_seqs; c += 64) {
             int t;
-            width += of_lane(scan(c, t), 63);
+            width += __builtin_amdgcn_readlane(scan(p, c, t), 63);
         }
-        const int64_t total = width * p.L * p.Hkv;
-        run = max((int64_t)min_run, quotient(total + p.n_waves - 1, p.n_waves));
-        pos = run * wave;
+        const int64_t total = (int64_t)width * (p.L * p.Hkv);
+        // (a little more than its share each, so that rounding leaves nothing)
+        run = max(kPagedMinRun, __builtin_amdgcn_readfirstlane((int)((float)total * p.per_wave)) + 1);
+        pos = (int64_t)run * wave;
         end = min(pos + run, total);
         if (pos >= end) return false;
-        item.lh = (int)quotient(pos, width);
-        int64_t at = pos - (int64_t)item.lh * width;
+        item.lh = __builtin_amdgcn_readfirstlane(quotient(pos, width));
+        int at = (int)(pos - (int64_t)item.lh * width);
         if (at < ahead) {
-            const int count = prefix_count();
-            set_prefix((int)quotient(at, count));
-            h0 = (int)(at - (int64_t)item.tile * count);
+            const int count = prefix_count(p);
+            set_prefix(p, __builtin_amdgcn_readfirstlane(at / count));
+            h0 = at - item.tile * count;
         } else {
             at -= ahead;
             int index = p.prefix_tiles;
             for (int c = 0;; c += 64) {
-                if (c) upto = scan(c, tiles);
-                const int64_t sum = of_lane(upto, 63);
-                const bool here = at < sum;
-                // row tiles up to each lane's
-                int before = tiles;
-#pragma unroll
-                for (int off = 1; off < 64; off <<= 1) {
-                    const int y = __shfl_up(before, off);
-                    if (lane >= off) before += y;
-                }
-                if (here) {
+                if (c) upto = scan(p, c, tiles);
+                const int sum = __builtin_amdgcn_readlane(upto, 63), before = wave_scan(tiles);
+                if (at < sum) {
                     const int j = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > at));
-                    at -= j ? of_lane(upto, j - 1) : 0;
+                    at -= j ? __builtin_amdgcn_readlane(upto, j - 1) : 0;
                     item.index = index + (j ? __builtin_amdgcn_readlane(before, j - 1) : 0);
-                    set_sequence(c + j);
-                    item.tile = (int)quotient(at, item.count);
-                    item.index += item.tile;
-                    h0 = (int)(at - (int64_t)item.tile * item.count);
+                    const int of_item = item.index;
+                    set_sequence(p, c + j);
+                    item.tile = item.tiles == 1 ? 0 : __builtin_amdgcn_readfirstlane(at / item.count);
+                    item.index = of_item + item.tile;
+                    h0 = at - item.tile * item.count;
                     break;
                 }
                 at -= sum;
@@ -280,6 +296,7 @@ struct PagedWalk {
     // The item behind it; false: there is none.
     __device__ __forceinline__ bool next()
     {
+        PagedArgs &p = paged_args();
         ++item.index;
         if (item.tile + 1 < item.tiles) {
             ++item.tile;
@@ -292,21 +309,21 @@ struct PagedWalk {
                 item.index = 0;
                 b = -1;
                 if (p.prefix_tiles) {
-                    set_prefix(0);
+                    set_prefix(p, 0);
                     return true;
                 }
                 continue;
             }
             int first, n;
-            rows_of(b, first, n);
-            if (tiles_of(n) > 0) break;
+            rows_of(p, b, first, n);
+            if (tiles_of(p, n) > 0) break;
         }
-        set_sequence(b);
+        set_sequence(p, b);
         return true;
     }
 
 private:
-    __device__ __forceinline__ void rows_of(int b, int &first, int &n) const
+    __device__ __forceinline__ static void rows_of(PagedArgs &p, int b, int &first, int &n)
     {
         if (!p.batch.starts) {
             first = b;
@@ -316,46 +333,47 @@ private:
         first = max(0, min(scalar(p.batch.starts)[b], p.batch.n_rows));
         n = max(0, min(scalar(p.batch.starts)[b + 1], p.batch.n_rows) - first);
     }
-    __device__ __forceinline__ void set_prefix(int tile)
+    __device__ __forceinline__ void set_prefix(PagedArgs &p, int tile)
     {
         item.b = -1;
         item.tile = tile;
         item.tiles = p.prefix_tiles;
         item.index = tile;
-        item.count = item.walk = prefix_count();
+        item.count = item.walk = prefix_count(p);
         item.len = 0;
         all_rows(p, item.first, item.n);
     }
-    __device__ __forceinline__ void set_sequence(int b)
+    __device__ __forceinline__ void set_sequence(PagedArgs &p, int b)
     {
         item.b = b;
-        rows_of(b, item.first, item.n);
+        rows_of(p, b, item.first, item.n);
         item.tile = 0;
-        item.tiles = tiles_of(item.n);
+        item.tiles = tiles_of(p, item.n);
         item.len = max(0, scalar(p.batch.lens)[b]);
         item.walk = p.walked_prefix;
-        item.count = count_of(item.len);
+        item.count = count_of(p, item.len);
     }
 };
 
 // Wavefronts of attn_paged_rows_kernel that a compute unit holds: by LDS, and by registers.
-constexpr int paged_rows_waves(int D, int rows) { return D == 256 ? 5 : rows == 32 ? 8 : D == 128 ? 10 : 16; }
+#ifndef KW128
+#define KW128 8
+#endif
+constexpr int paged_rows_waves(int D, int rows) { return D == 256 ? 5 : rows == 32 ? 8 : D == 128 ? KW128 : 16; }
 
 int launch_paged_rows(const PagedAttnParams &p, int tile_rows, hipStream_t s);
-
-constexpr int kPagedMinRun = 4;   // halves of a wavefront's run at least
 
 // Where the results of a segment, halves seg0 ... h of an item, go.  pos: the axis behind the segment, run: a wavefront's run of it.
 struct PagedPlace {
     int kind;        // kDirect; kWhole: row_o; 0: a slot of the wavefront
     float *o, *ml;   // of the slot's rows, or of rows by (layer, query head, row)
 };
-template <int TR>
-__device__ __forceinline__ PagedPlace paged_place(const PagedAttnParams &p, const PagedItem &it, int seg0, int h, int64_t pos, int64_t run, int lane)
+template <int TR, class P>
+__device__ __forceinline__ PagedPlace paged_place(const P &p, const PagedItem &it, int seg0, int h, int64_t pos, int run, int lane)
 {
     const bool ends = h + 1 == it.count, whole = ends && seg0 == 0;
-    const bool apart = p.n_prefix > 0 && p.walked_prefix == 0;   // the prefix has items of its own: every row is joined
-    PagedPlace to = {whole ? apart ? kWhole : kDirect : 0, nullptr, nullptr};
+    // (a prefix with items of its own on this axis: every row is joined; with parts by rows: they are there already)
+    PagedPlace to = {whole ? p.prefix_tiles ? kWhole : kDirect : 0, nullptr, nullptr};
     if (!p.slot_o) return to;
     const int64_t wave = blockIdx.x;
     if (to.kind == kWhole) {
@@ -370,7 +388,7 @@ __device__ __forceinline__ PagedPlace paged_place(const PagedAttnParams &p, cons
     if (ends) {
         if (lane < 2 && it.index < p.max_items) {
             const int64_t begin = pos - it.count;   // of the item, on the axis
-            const int first = to.kind ? to.kind : (int)PagedWalk<TR>::quotient(begin, run);
+            const int first = to.kind ? to.kind : quotient(begin, run);
             p.items[((int64_t)it.lh * p.max_items + it.index) * 2 + lane] = lane ? (int)wave : first;
         }
         if (it.lh == 0 && it.b >= 0) {   // the rows whose first head lies in this tile
@@ -384,6 +402,17 @@ __device__ __forceinline__ PagedPlace paged_place(const PagedAttnParams &p, cons
     return to;
 }
 
+// Another part of a row, (m2, l2), joined to (m, l): its outputs are to be multiplied by f2 (and left out where that is 0: they may never have been written), the
+// row's own by f.  A reference of -infinity has seen no key and has sum 0, or nothing but NaN scores and a sum that says so.
+__device__ __forceinline__ void join_part(float &m, float &l, float m2, float l2, float scale_log2, float &f, float &f2)
+{
+    const float M = fmaxf(m, m2);
+    f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - M) * scale_log2);
+    f2 = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m2 - M) * scale_log2);
+    l = (m == -INFINITY ? l : l * f) + (m2 == -INFINITY ? l2 : l2 * f2);
+    m = M;
+}
+
 // Row r of an item's tile, in that place.
 struct PagedRow {
     bool valid;
@@ -391,7 +420,8 @@ struct PagedRow {
     int64_t flat;   // (layer, query head, row)
     int64_t o;      // in the place
 };
-__device__ __forceinline__ PagedRow paged_row(const PagedAttnParams &p, const PagedItem &it, const PagedPlace &to, int tile_rows, int r)
+template <class P>
+__device__ __forceinline__ PagedRow paged_row(const P &p, const PagedItem &it, const PagedPlace &to, int tile_rows, int r)
 {
     PagedRow x;
     const int packed = it.tile * tile_rows + r;
@@ -407,8 +437,8 @@ __device__ __forceinline__ PagedRow paged_row(const PagedAttnParams &p, const Pa
 }
 
 // The segment by the formula.
-template <typename T, int D, int TR>
-__device__ __forceinline__ void paged_exact_segment(const PagedAttnParams &p, const PagedItem &it, const PagedPlace &to, int seg0, int h, int lane)
+template <typename T, int D, int TR, class P>
+__device__ __forceinline__ void paged_exact_segment(const P &p, const PagedItem &it, const PagedPlace &to, int seg0, int h, int lane)
 {
 #pragma unroll 1
     for (int r = 0; r < TR; ++r) {
@@ -417,6 +447,13 @@ __device__ __forceinline__ void paged_exact_segment(const PagedAttnParams &p, co
         float m, sum, o[8];
         paged_exact_row<T, D>(p, row.l, it.lh - row.l * p.Hkv, row.hq, row.row, it.b, it.b < 0 ? -1 : last_seen(it.len, it.n, row.i, p.batch.cap), it.walk, seg0, h + 1, lane, m, sum, o);
         if (to.kind == kDirect) {
+            for (int run = 0; run < p.prefix_runs; ++run) {
+                const int64_t at = row.flat + (int64_t)(p.prefix_part + run) * p.L * p.Hkv * p.G * p.batch.n_rows;
+                float f, f2;
+                join_part(m, sum, p.row_ml[2 * at], p.row_ml[2 * at + 1], p.scale_log2, f, f2);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = o[j] * f + (f2 != 0.f && lane < D / 8 ? f2 * p.row_o[at * D + 8 * lane + j] : 0.f);
+            }
             paged_store_row<T, D>(p, row.l, row.hq, row.row, lane, m, sum, o);
         } else {
             if (lane < D / 8) {
@@ -437,6 +474,8 @@ struct PagedTileParams : PagedAttnParams {   // row_o null: rows go to `out`.  O
     int32_t n_splits;      // runs
     int32_t more_rows;     // packed rows that the sequences of the launch have more than
     int32_t part;          // by rows: of run 0
+    int32_t join_runs, join_part;   // rows that go to `out` are joined with these parts
+    float *join_o, *join_ml;
     int32_t slot_mask;     // slot of a token in its page
     divisor_t by_LH, by_splits;
     // what the kernel's other forms have
@@ -517,10 +556,10 @@ __device__ __forceinline__ bool find_paged_tile(const P &p, int u, int lane, Pag
 
 // Of a row's part: (part, layer, query head, row).
 template <class P>
-__device__ __forceinline__ int64_t paged_part_row(const P &p, int l, int hkv, int g, int row, int split)
+__device__ __forceinline__ int64_t paged_part_row(const P &p, int l, int hkv, int g, int row, int part)
 {
     const int64_t Hq = (int64_t)p.Hkv * p.G;
-    return ((int64_t)(p.part + split) * p.L * Hq + l * Hq + hkv * p.G + g) * p.batch.n_rows + row;
+    return ((int64_t)part * p.L * Hq + l * Hq + hkv * p.G + g) * p.batch.n_rows + row;
 }
 
 // For the combine kernel: the rows whose first head lies in the tile are this kernel's.
@@ -540,13 +579,29 @@ __device__ __forceinline__ void paged_empty_tile(const P &p, const PagedTile &x,
         const int packed = x.tile * bm + r, i = div_by(packed, p.by_G), g = packed - i * p.G;
         if (i >= x.n) return;
         if (p.row_o) {
-            const int64_t at = paged_part_row(p, l, hkv, g, x.first + i, split);
+            const int64_t at = paged_part_row(p, l, hkv, g, x.first + i, p.part + split);
             p.row_ml[2 * at] = -INFINITY;
             p.row_ml[2 * at + 1] = 0.f;
         } else {
-            bf16_t *out = static_cast<bf16_t *>(p.out) + l * p.s_o.layer + (int64_t)(hkv * p.G + g) * p.s_o.head + (int64_t)(x.first + i) * p.s_o.token;
-            for (int c = 0; c < D; c += 8) *reinterpret_cast<u32x4 *>(out + c) = u32x4{0, 0, 0, 0};
-            if (p.lse) p.lse[((int64_t)l * p.Hkv * p.G + hkv * p.G + g) * p.batch.n_rows + x.first + i] = -INFINITY;
+            const int hq = hkv * p.G + g;
+            bf16_t *out = static_cast<bf16_t *>(p.out) + l * p.s_o.layer + (int64_t)hq * p.s_o.head + (int64_t)(x.first + i) * p.s_o.token;
+            float m = -INFINITY, sum = 0.f, f, f2;
+            for (int run = 0; run < p.join_runs; ++run) {
+                const int64_t at = paged_part_row(p, l, hkv, g, x.first + i, p.join_part + run);
+                join_part(m, sum, p.join_ml[2 * at], p.join_ml[2 * at + 1], p.scale_log2, f, f2);
+            }
+            for (int c = 0; c < D; c += 8) {
+                float o[8] = {};
+                for (int run = 0; run < p.join_runs; ++run) {
+                    const int64_t at = paged_part_row(p, l, hkv, g, x.first + i, p.join_part + run);
+                    const float mr = p.join_ml[2 * at];
+                    if (mr != -INFINITY)
+                        for (int j = 0; j < 8; ++j) o[j] += __builtin_amdgcn_exp2f((mr - m) * p.scale_log2) * p.join_o[at * D + c + j];
+                }
+                for (int j = 0; j < 8; ++j) o[j] = m == -INFINITY && sum == 0.f ? 0.f : o[j] / sum;
+                *reinterpret_cast<u32x4 *>(out + c) = pack<bf16_t>(o);
+            }
+            if (p.lse) p.lse[((int64_t)l * p.Hkv * p.G + hq) * p.batch.n_rows + x.first + i] = m == -INFINITY && sum == 0.f ? -INFINITY : m * p.scale + logf(sum);
         }
     }
 }
@@ -571,10 +626,17 @@ __device__ __forceinline__ void paged_exact_tile(int h0, int h1, int split, int 
         float m, sum, o[8];
         paged_exact_row<bf16_t, D>(p, l, hkv, hkv * p.G + g, x.first + i, x.b, x.prefix ? -1 : x.last(i), x.prefix ? (p.n_prefix + 31) / 32 : 0, h0, h1, lane, m, sum, o);
         if (!p.row_o) {
+            for (int run = 0; run < p.join_runs; ++run) {
+                const int64_t at = paged_part_row(p, l, hkv, g, x.first + i, p.join_part + run);
+                float f, f2;
+                join_part(m, sum, p.join_ml[2 * at], p.join_ml[2 * at + 1], p.scale_log2, f, f2);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = o[j] * f + (f2 != 0.f && lane < D / 8 ? f2 * p.join_o[at * D + 8 * lane + j] : 0.f);
+            }
             paged_store_row<bf16_t, D>(p, l, hkv * p.G + g, x.first + i, lane, m, sum, o);
             continue;
         }
-        const int64_t at = paged_part_row(p, l, hkv, g, x.first + i, split);
+        const int64_t at = paged_part_row(p, l, hkv, g, x.first + i, p.part + split);
         if (lane < D / 8) {
             f32x4 *po = reinterpret_cast<f32x4 *>(p.row_o + at * D + 8 * lane);
             po[0] = f32x4{o[0], o[1], o[2], o[3]};

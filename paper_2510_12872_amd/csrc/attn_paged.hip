@@ -27,103 +27,141 @@ __global__ __launch_bounds__(256) void attn_paged_row_kernel(const PagedAttnPara
 }
 
 // The results of rows whose keys went to several wavefronts or runs: out = sum_s f_s O_s / sum_s f_s l_s, f_s = exp2((m_s - max m) scale log2 e), parts in
-// a fixed order.  One wavefront per row; D / 4 lanes hold its channels, and the 64 / (D / 4) such groups take the parts in turn.
+// a fixed order.  A wavefront takes `heads` query heads of a (layer, row); D / 4 lanes hold an output's channels, and the 64 / (D / 4) such groups take the
+// parts in turn.
+struct CombineParams : PagedAttnParams {
+    int32_t heads, chunks;   // query heads of a wavefront, such pieces of a row
+    divisor_t by_chunks, by_rows;
+};
 template <typename T, int D>
-__global__ __launch_bounds__(256) void attn_paged_combine_kernel(const PagedAttnParams p)
+__global__ __launch_bounds__(256) void attn_paged_combine_kernel(const CombineParams p)
 {
-    constexpr int CL = D / 4, NG = 64 / CL, U = 4;
+    constexpr int CL = D / 4, NG = 64 / CL, U = 8;
     const int lane = threadIdx.x & 63, Hq = p.Hkv * p.G, n_rows = p.batch.n_rows;
-    const int64_t flat = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int64_t all = (int64_t)p.L * Hq * n_rows;
-    if (flat >= all) return;
-    const int row = (int)(flat % n_rows), head = (int)(flat / n_rows), l = head / Hq, hq = head - l * Hq, hkv = div_by(hq, p.by_G), g = hq - hkv * p.G;
+    const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    const int lr = div_by(wave, p.by_chunks), chunk = wave - lr * p.chunks, l = div_by(lr, p.by_rows), row = lr - l * n_rows;
+    if (l >= p.L) return;
+    // (One row of up to tile_rows heads per sequence: its item is known.  Else, for rows of no sequence, item_of holds whatever.)
+    const bool known = !p.batch.starts && p.G <= p.tile_rows;
+    const int item = known ? p.prefix_tiles + row : p.item_of[2 * row], number = known ? 0 : p.item_of[2 * row + 1];
     int first, n;
     all_rows(p, first, n);
-    if (row < first || row >= first + n) return;
+    if (row < first || row >= first + n || item == kDirect) return;
     const bool apart = p.n_prefix > 0 && p.walked_prefix == 0;
-    // What the walks left of an item: `count` slots from wavefront `wave` on, the last of them an item's end; or one part by rows.  (Clamped: item_of is not
+    // What the walks left of an item: `count` slots from wavefront `wave` on, the last of them an item's end; or parts by rows.  (Clamped: item_of is not
     // written for every row where starts decreases.)
     struct Parts {
         int wave, count, row;
         bool whole;
     };
-    auto parts_of = [&](int index, int packed) -> Parts {
-        const int32_t *e = p.items + ((int64_t)(l * p.Hkv + hkv) * p.max_items + max(0, min(index, p.max_items - 1))) * 2;
-        const int w0 = e[0], w1 = e[1];
-        if (w0 < 0) return Parts{w0, 1, 0, true};
-        const int last = max(0, min(w1, p.n_waves - 1)), from = min(w0, last);
-        return Parts{from, last - from + 1, packed & (p.tile_rows - 1), false};
-    };
-    const int item = p.item_of[2 * row], packed = p.item_of[2 * row + 1] * p.G + g;
-    const Parts own = item < 0 ? Parts{item, p.tile_runs, 0, true} : parts_of(item + (int)((uint32_t)packed / (uint32_t)p.tile_rows), packed);
-    if (own.wave == kDirect) return;
-    Parts before = {0, p.prefix_runs, 0, true};
-    if (apart && p.prefix_tiles) {
-        const int at = (row - first) * p.G + g;
-        before = parts_of((int)((uint32_t)at / (uint32_t)p.tile_rows), at);
-    }
-    const int count = own.count + (apart ? before.count : 0);
-    auto place = [&](int k, const float *&o, const float *&ml) {
-        const bool b = k >= own.count;
-        const Parts &x = b ? before : own;
-        if (b) k -= own.count;
-        if (x.whole) {
-            const int64_t at = flat + (b ? p.prefix_part + k : k) * all;
-            o = p.row_o + at * D;
-            ml = p.row_ml + at * 2;
-        } else {
-            const int64_t at = (2 * (int64_t)(x.wave + k) + (k + 1 < x.count ? 1 : 0)) * p.tile_rows + x.row;
-            o = p.slot_o + at * D;
-            ml = p.slot_ml + at * 2;
-        }
-    };
-    float M = -INFINITY;
-    for (int k = lane; k < count; k += 64) {
-        const float *o, *ml;
-        place(k, o, ml);
-        M = fmaxf(M, ml[0]);
-    }
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
+    const int64_t all = (int64_t)p.L * Hq * n_rows;
     const int group = lane / CL, c = 4 * (lane % CL);
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
-    for (int k0 = group; k0 < count; k0 += NG * U) {
-        f32x4 os[U];
-        float ms[U], ls[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const float *o, *ml;
-            place(min(k0 + u * NG, count - 1), o, ml);
-            ms[u] = ml[0];
-            ls[u] = ml[1];
-            os[u] = *reinterpret_cast<const f32x4 *>(o + c);
+    for (int hq = chunk * p.heads; hq < min(Hq, (chunk + 1) * p.heads); ++hq) {
+        const int hkv = div_by(hq, p.by_G), g = hq - hkv * p.G;
+        const int64_t flat = ((int64_t)l * Hq + hq) * n_rows + row;
+        auto parts_of = [&](int index, int packed) -> Parts {
+            const int32_t *e = p.items + ((int64_t)(l * p.Hkv + hkv) * p.max_items + max(0, min(index, p.max_items - 1))) * 2;
+            const int w0 = e[0], w1 = e[1];
+            if (w0 < 0) return Parts{w0, 1, 0, true};
+            const int last = max(0, min(w1, p.n_waves - 1)), from = min(w0, last);
+            return Parts{from, last - from + 1, packed & (p.tile_rows - 1), false};
+        };
+        const int packed = number * p.G + g;
+        const Parts own = item < 0 ? Parts{item, p.tile_runs, 0, true} : parts_of(item + (int)((uint32_t)packed / (uint32_t)p.tile_rows), packed);
+        if (own.wave == kDirect) continue;
+        Parts before = {0, p.prefix_runs, 0, true};
+        if (p.prefix_tiles) {
+            const int at = (row - first) * p.G + g;
+            before = parts_of((int)((uint32_t)at / (uint32_t)p.tile_rows), at);
         }
+        const int count = own.count + (apart ? before.count : 0);
+        auto place = [&](int k, const float *&o, const float *&ml) {
+            const bool b = k >= own.count;
+            const Parts &x = b ? before : own;
+            if (b) k -= own.count;
+            if (x.whole) {
+                const int64_t at = flat + (b ? p.prefix_part + k : k) * all;
+                o = p.row_o + at * D;
+                ml = p.row_ml + at * 2;
+            } else {
+                const int64_t at = (2 * (int64_t)(x.wave + k) + (k + 1 < x.count ? 1 : 0)) * p.tile_rows + x.row;
+                o = p.slot_o + at * D;
+                ml = p.slot_ml + at * 2;
+            }
+        };
+        // Parts k0 ... of this group, whose loads are all in flight at once, against the largest reference so far.
+        float M = -INFINITY, sum = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int k0 = group; k0 < count; k0 += NG * U) {
+            f32x4 os[U];
+            float ms[U], ls[U], top = M;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (k0 + u * NG < count && (ms[u] != -INFINITY || ls[u] != 0.f)) {   // (reference -inf, sum 0: nothing seen; NaN: NaN scores)
-                const float f = __builtin_amdgcn_exp2f((ms[u] - M) * p.scale_log2);
-                sum = fmaf(f, ls[u], sum);
-                acc += f * os[u];
+            for (int u = 0; u < U; ++u) {
+                const float *o, *ml;
+                place(min(k0 + u * NG, count - 1), o, ml);
+                ms[u] = ml[0];
+                ls[u] = ml[1];
+                os[u] = *reinterpret_cast<const f32x4 *>(o + c);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) top = fmaxf(top, ms[u]);
+            const float f0 = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - top) * p.scale_log2);
+            sum = M == -INFINITY ? sum : sum * f0;   // (nothing seen: 0; nothing but NaN scores: NaN)
+            acc *= f0;
+            M = top;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (k0 + u * NG >= count) continue;
+                if (ms[u] != -INFINITY) {
+                    const float f = __builtin_amdgcn_exp2f((ms[u] - M) * p.scale_log2);
+                    sum = fmaf(f, ls[u], sum);
+                    acc += f * os[u];
+                } else {
+                    sum += ls[u];   // (outputs of a part that has seen nothing may never have been written)
+                }
             }
         }
-    }
 #pragma unroll
-    for (int off = CL; off < 64; off <<= 1) {
-        sum += __shfl_xor(sum, off);
+        for (int off = CL; off < 64; off <<= 1) {   // the groups
+            float f, f2;
+            const float m2 = __shfl_xor(M, off), l2 = __shfl_xor(sum, off);
+            join_part(M, sum, m2, l2, p.scale_log2, f, f2);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], off);
+            for (int i = 0; i < 4; ++i) {
+                const float a2 = __shfl_xor(acc[i], off);
+                acc[i] = acc[i] * f + a2 * f2;
+            }
+        }
+        const bool none = M == -INFINITY && sum == 0.f;
+        if (group == 0) {
+            const float inv = none ? 0.f : 1.f / sum;
+            T *out = static_cast<T *>(p.out) + l * p.s_o.layer + (int64_t)hq * p.s_o.head + (int64_t)row * p.s_o.token + c;
+            if constexpr (sizeof(T) == 2)
+                *reinterpret_cast<u32x2 *>(out) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+            else
+                *reinterpret_cast<f32x4 *>(out) = acc * inv;
+        }
+        if (p.lse && lane == 0) p.lse[flat] = none ? -INFINITY : M * p.scale + logf(sum);
     }
-    const bool none = M == -INFINITY && sum == 0.f;
-    if (group == 0) {
-        const float inv = none ? 0.f : 1.f / sum;
-        T *out = static_cast<T *>(p.out) + l * p.s_o.layer + (int64_t)hq * p.s_o.head + (int64_t)row * p.s_o.token + c;
-        if constexpr (sizeof(T) == 2)
-            *reinterpret_cast<u32x2 *>(out) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
-        else
-            *reinterpret_cast<f32x4 *>(out) = acc * inv;
+}
+
+template <typename T>
+int launch_combine(const PagedAttnParams &a, hipStream_t s)
+{
+    CombineParams p{};
+    static_cast<PagedAttnParams &>(p) = a;
+    const int Hq = a.Hkv * a.G;
+    const int64_t rows = (int64_t)a.L * a.batch.n_rows;
+    p.heads = (int)std::min<int64_t>(Hq, std::max<int64_t>(1, rows * Hq / 4096));   // a wavefront's: as many as leave a few per SIMD
+    p.chunks = (Hq + p.heads - 1) / p.heads;
+    p.by_chunks = make_divisor((uint32_t)p.chunks);
+    p.by_rows = make_divisor((uint32_t)a.batch.n_rows);
+    const dim3 grid((unsigned)((rows * p.chunks + 3) / 4)), block(256);
+    switch (a.D) {
+        case 64: return launch(attn_paged_combine_kernel<T, 64>, grid, block, 0, s, p);
+        case 128: return launch(attn_paged_combine_kernel<T, 128>, grid, block, 0, s, p);
+        default: return launch(attn_paged_combine_kernel<T, 256>, grid, block, 0, s, p);
     }
-    if (p.lse && lane == 0) p.lse[flat] = none ? -INFINITY : M * p.scale + logf(sum);
 }
 
 // How a call is carried out: what depends on the model, the batch's host side and the prefix's length alone.
@@ -136,7 +174,7 @@ struct Plan {
     bool tiles;                             // is the tiles kernel launched for sequences
     int seq_rows, seq_runs, prefix_rows, prefix_runs;   // its row tiles and runs; prefix_runs 0: it is not launched for the prefix
     int64_t seq_units, prefix_units;        // its blocks per (layer, kv head)
-    int64_t max_items, row_parts;           // parts by rows: [row_parts][layer, query head, row]
+    int64_t max_items, seq_parts, row_parts;   // parts by rows: [row_parts][layer, query head, row], sequences' first
     size_t bytes;
 };
 
@@ -171,7 +209,8 @@ Plan plan_of(const kvcomm_model &m, const kvcomm_batch &b, int n_prefix)
         }
         pl.prefix_units = tiles * pl.prefix_runs;
     }
-    pl.row_parts = n_prefix ? pl.seq_runs + std::max(1, pl.prefix_runs) : pl.seq_runs > 1 ? pl.seq_runs : 0;
+    pl.seq_parts = pl.prefix_tiles ? 1 : pl.seq_runs > 1 ? pl.seq_runs : 0;
+    pl.row_parts = pl.seq_parts + (pl.prefix_tiles ? 1 : pl.prefix_runs);
     pl.bytes = sizeof(float) * (size_t)(D + 2) * ((size_t)pl.n_waves * 2 * pl.tile_rows + (size_t)(pl.row_parts * LH * rows)) +
                sizeof(int32_t) * ((size_t)(2 * LH * pl.max_items) + 2 * (size_t)b.n_rows);
     return pl;
@@ -241,8 +280,13 @@ int paged_attn(const kvcomm_model *model, const kvcomm_tensor &q, const kvcomm_t
     const int64_t LH = (int64_t)p.L * p.Hkv;
     const double most_blocks = 4294967296.0 / 512;   // a launch holds fewer than 2^32 threads
     if ((double)pl.seq_units * LH >= most_blocks || (double)pl.prefix_units * LH >= most_blocks || pl.max_items > INT32_MAX / 2) return KVCOMM_EUNSUPPORTED;
+    // The axis: halves of a (layer, kv head) in 31 bits, and of a run.
+    const int64_t most_tiles = batch->starts ? rows / ((int64_t)p.L * p.Hkv * pl.tile_rows) + batch->n_seqs : (int64_t)batch->n_seqs * ((p.G + pl.tile_rows - 1) / pl.tile_rows);
+    const double axis = (double)most_tiles * ((double)(p.batch.cap + 31) / 32 + (scratch ? 0.0 : (double)(n_prefix + 31) / 32) + 1) + (double)pl.prefix_tiles * ((n_prefix + 31) / 32);
+    if (axis >= 2147483647.0 || axis * LH / pl.n_waves >= 2147483000.0) return KVCOMM_EUNSUPPORTED;
     p.tile_rows = pl.tile_rows;
     p.n_waves = pl.n_waves;
+    p.per_wave = 1.000001f / (float)pl.n_waves;
     p.most_rows = scratch && pl.tiles ? kFewRows : INT32_MAX;
     p.max_items = (int32_t)pl.max_items;
     if (!scratch) {
@@ -259,7 +303,7 @@ int paged_attn(const kvcomm_model *model, const kvcomm_tensor &q, const kvcomm_t
     p.item_of = reinterpret_cast<int32_t *>(x);
     p.prefix_tiles = pl.prefix_tiles;
     p.prefix_runs = pl.prefix_runs;
-    p.prefix_part = pl.seq_runs;
+    p.prefix_part = (int32_t)pl.seq_parts;
     p.tile_runs = pl.seq_runs;
     auto tiles_of = [&](bool over_prefix) {
         PagedTileParams t{};
@@ -278,18 +322,19 @@ int paged_attn(const kvcomm_model *model, const kvcomm_tensor &q, const kvcomm_t
             t.s_k = PoolStrides{p.s_pk.layer, p.s_pk.head, 0, p.s_pk.token};
             t.s_v = PoolStrides{p.s_pv.layer, p.s_pv.head, 0, p.s_pv.token};
         }
-        if (!over_prefix && !n_prefix && pl.seq_runs == 1) t.row_o = nullptr;
+        if (!over_prefix && pl.seq_runs == 1) {   // (then a prefix has parts by rows: its rows are more than kFewRows)
+            t.row_o = nullptr;
+            t.join_runs = pl.prefix_runs;
+            t.join_part = p.prefix_part;
+            t.join_o = p.row_o;
+            t.join_ml = p.row_ml;
+        }
         return launch_paged_tiles(t, over_prefix ? pl.prefix_rows : pl.seq_rows, (unsigned)((over_prefix ? pl.prefix_units : pl.seq_units) * LH), s);
     };
-    if (pl.tiles && (st = tiles_of(false))) return st;
     if (pl.prefix_runs && (st = tiles_of(true))) return st;
+    if (pl.tiles && (st = tiles_of(false))) return st;
     if ((st = launch_paged_rows(p, pl.tile_rows, s))) return st;
-    const dim3 grid((unsigned)((rows + 3) / 4)), block(256);
-    switch (D) {
-        case 64: return launch(attn_paged_combine_kernel<bf16_t, 64>, grid, block, 0, s, p);
-        case 128: return launch(attn_paged_combine_kernel<bf16_t, 128>, grid, block, 0, s, p);
-        default: return launch(attn_paged_combine_kernel<bf16_t, 256>, grid, block, 0, s, p);
-    }
+    return launch_combine<bf16_t>(p, s);
 }
 
 size_t workspace_of(const kvcomm_model *model, const kvcomm_batch *batch, int32_t n_prefix)

@@ -18,12 +18,19 @@ __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)"
 // their number per compute unit is what fits LDS.
 // What bounds it is HBM.  A half lies in one page or in two, whose entries are read, through the scalar cache, a half ahead.
 template <int D, int RH>
-__global__ __launch_bounds__(64, RH == 2 || D == 256 ? 2 : D == 128 ? 3 : 4) void attn_paged_rows_kernel(const PagedAttnParams p)
+__global__ __launch_bounds__(64, RH == 2 || D >= 128 ? 2 : 4) void attn_paged_rows_kernel(const PagedAttnParams)
 {
+    PagedArgs &p = paged_args();
+    await_paged_args(p);
     constexpr int TR = 16 * RH;
     constexpr int NF = D / 16, KCH = D / 8, ROWB = D * 2, HALFB = 32 * ROWB;
     constexpr int RPL = 64 / KCH, LPT = 32 / RPL;              // key rows filled by one wavefront-wide direct load, loads of a half
     constexpr int KD = 16 / RPL, VD = RPL < 8 ? 8 / RPL : 1;   // loads after which the swizzle pattern of the rows repeats
+#ifdef KNT
+    constexpr bool NT = false;
+#else
+    constexpr bool NT = true;
+#endif
     auto k_swz = [](int key) __attribute__((always_inline)) -> int { return D == 64 ? (key >> 1) & 7 : key & 15; };
     auto v_swz = [](int key) __attribute__((always_inline)) -> int {
         return D == 64 ? (2 * (key & 2)) | ((key >> 1) & 2) : 4 * (key & 3) | ((key >> 1) & 2);
@@ -32,18 +39,17 @@ __global__ __launch_bounds__(64, RH == 2 || D == 256 ? 2 : D == 128 ? 3 : 4) voi
     const int lane = threadIdx.x, n = lane & 15, g = lane >> 4, lq = lane / KCH;
     lds_byte *kbuf = (lds_byte *)smem, *vbuf = kbuf + HALFB;
 
-    PagedWalk<TR> walk(p, lane);
+    PagedWalk<TR> walk(lane);
     int64_t pos, end;
     int h;
-    if (!walk.begin(blockIdx.x, kPagedMinRun, pos, end, h)) return;
-    // What nobody reads again and the last-level cache does not hold is not kept there.
-    const bool nt = walk.width * p.L * p.Hkv * (HALFB * 2) > (int64_t)256 << 20;
+    if (!walk.begin(blockIdx.x, pos, end, h)) return;
 
     // ---- where the halves of an item lie
     const unsigned char *kp, *vp, *kf, *vf;   // (layer, head) of the pools and of the prefix
     const_int *table = nullptr;
     int tokens = 0;                           // of the sequence that exist
     auto enter = [&]() __attribute__((always_inline)) {   // walk.item
+        PagedArgs &p = paged_args();
         const PagedItem &it = walk.item;
         const int l = div_by(it.lh, p.by_Hkv), hkv = it.lh - l * p.Hkv;
         kp = reinterpret_cast<const unsigned char *>(static_cast<const bf16_t *>(p.k) + l * p.s_k.layer + hkv * p.s_k.head);
@@ -54,15 +60,15 @@ __global__ __launch_bounds__(64, RH == 2 || D == 256 ? 2 : D == 128 ? 3 : 4) voi
         table = scalar(p.batch.table) + (int64_t)max(it.b, 0) * p.batch.table_stride;
     };
     struct Half {       // of an item, to be loaded
-        int at;         // key of the prefix or token of the pages
+        int at, limit;  // first key of the prefix or token of the pages, and how many there are: 0: an item without tokens, nothing is read
         bool prefix;
         int page[2];    // of the tokens at ... and at + 16 ...
     };
-    // (Tokens behind the last one that exists are read as that one, see load(); an item without tokens reads nothing.)
     auto half_at = [&](int h_) __attribute__((always_inline)) -> Half {
-        Half x = {32 * h_, h_ < walk.item.walk, {0, 0}};
+        Half x = {32 * h_, p.n_prefix, h_ < walk.item.walk, {0, 0}};
         if (!x.prefix) {
             x.at -= 32 * walk.item.walk;
+            x.limit = tokens;
             if (tokens > 0) {
                 x.page[0] = table[x.at >> p.batch.log_page];
                 x.page[1] = table[min(x.at + 16, tokens - 1) >> p.batch.log_page];
@@ -70,48 +76,41 @@ __global__ __launch_bounds__(64, RH == 2 || D == 256 ? 2 : D == 128 ? 3 : 4) voi
         }
         return x;
     };
+    auto is_page = [&](int e) __attribute__((always_inline)) -> bool { return (uint32_t)e < (uint32_t)p.batch.n_pages; };
     uint32_t k_chunk[KD], v_chunk[VD];   // bytes inside a row that this lane fetches
 #pragma unroll
     for (int i = 0; i < KD; ++i) k_chunk[i] = ((lane % KCH) ^ k_swz(i * RPL + lq)) * 16;
 #pragma unroll
     for (int i = 0; i < VD; ++i) v_chunk[i] = ((lane % KCH) ^ v_swz(i * RPL + lq)) * 16;
     bool no_page = false;   // of the segment
-    auto load_rows = [&](auto nt_c, const unsigned char *row, int64_t tok, int count, uint32_t chunk, lds_byte *dst) __attribute__((always_inline)) {
-        // `count` rows exist from `row` on (1 at least); a lane whose row does not reads the last one
-        dma16_sbase<decltype(nt_c)::value>(row, (uint32_t)min(lq, count - 1) * (uint32_t)(tok * 2) + chunk, dst);
-    };
-    auto load_as = [&](auto nt_c, const Half &x, const unsigned char *pool, int64_t page_stride, int64_t tok, const unsigned char *pre, int64_t pre_tok, auto &chunk,
-                       lds_byte *dst) __attribute__((always_inline)) {
+    // The rows of a half from `base` on, pages (of one prefix: none) and rows so many bytes apart.  Rows behind the last one are read as that one.
+    auto load = [&](const Half &x, const unsigned char *base, int64_t page_bytes, uint32_t row_bytes, auto &chunk, auto swz, lds_byte *dst) __attribute__((always_inline)) {
         constexpr int NC = sizeof(chunk) / sizeof(chunk[0]);
-        if (x.prefix) {
-#pragma unroll
-            for (int i = 0; i < LPT; ++i) {
-                const int row = min(x.at + i * RPL, p.n_prefix - 1);
-                load_rows(nt_c, pre + (int64_t)row * pre_tok * 2, pre_tok, p.n_prefix - row, chunk[i % NC], dst + i * RPL * ROWB);
-            }
-        } else if (tokens > 0) {
+        const int mask = x.prefix ? INT32_MAX : (1 << p.batch.log_page) - 1;
+        if (x.at + 32 <= x.limit) {
+            const uint32_t in = (uint32_t)lq * row_bytes;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const bool there = (uint32_t)x.page[half] < (uint32_t)p.batch.n_pages;
-                const int first = min(x.at + 16 * half, tokens - 1);   // (of the page that page[half] is)
-                const unsigned char *base = pool + (int64_t)(there ? x.page[half] : 0) * page_stride * 2;
+                const int page = is_page(x.page[half]) ? x.page[half] : 0;
+                const unsigned char *row = base + (x.prefix ? 0 : page * page_bytes) + (uint64_t)(uint32_t)((x.at + 16 * half) & mask) * row_bytes;
 #pragma unroll
-                for (int i = half * LPT / 2; i < (half + 1) * LPT / 2; ++i) {
-                    const int row = max(first, min(x.at + i * RPL, tokens - 1));
-                    load_rows(nt_c, base + (int64_t)(row & ((1 << p.batch.log_page) - 1)) * tok * 2, tok, tokens - row, chunk[i % NC], dst + i * RPL * ROWB);
-                }
+                for (int i = half * LPT / 2; i < (half + 1) * LPT / 2; ++i, row += RPL * (uint64_t)row_bytes) dma16_sbase<NT>(row, in + chunk[i % NC], dst + i * RPL * ROWB);
+            }
+        } else if (x.limit > 0) {
+#pragma unroll 1
+            for (int i = 0; i < LPT; ++i) {
+                const int r = min(x.at + i * RPL, x.limit - 1), e = x.page[r >= x.at + 16];   // (page[1] where that is behind the last one: the last one's)
+                const unsigned char *row = base + (x.prefix ? 0 : (is_page(e) ? e : 0) * page_bytes) + (uint64_t)(uint32_t)(r & mask) * row_bytes;
+                dma16_sbase<NT>(row, (uint32_t)min(lq, x.limit - 1 - r) * row_bytes + ((lane % KCH) ^ swz(i * RPL + lq)) * 16, dst + i * RPL * ROWB);
             }
         }
     };
-    auto load = [&](const Half &x, const unsigned char *pool, int64_t page_stride, int64_t tok, const unsigned char *pre, int64_t pre_tok, auto &chunk,
-                    lds_byte *dst) __attribute__((always_inline)) {
-        if (nt)
-            load_as(std::true_type{}, x, pool, page_stride, tok, pre, pre_tok, chunk, dst);
-        else
-            load_as(std::false_type{}, x, pool, page_stride, tok, pre, pre_tok, chunk, dst);
+    auto load_k = [&](const Half &x) __attribute__((always_inline)) {
+        load(x, x.prefix ? kf : kp, p.s_k.page * 2, (uint32_t)(x.prefix ? p.s_pk.token : p.s_k.token) * 2, k_chunk, k_swz, kbuf);
     };
-    auto load_k = [&](const Half &x) __attribute__((always_inline)) { load(x, kp, p.s_k.page, p.s_k.token, kf, p.s_pk.token, k_chunk, kbuf); };
-    auto load_v = [&](const Half &x) __attribute__((always_inline)) { load(x, vp, p.s_v.page, p.s_v.token, vf, p.s_pv.token, v_chunk, vbuf); };
+    auto load_v = [&](const Half &x) __attribute__((always_inline)) {
+        load(x, x.prefix ? vf : vp, p.s_v.page * 2, (uint32_t)(x.prefix ? p.s_pv.token : p.s_v.token) * 2, v_chunk, v_swz, vbuf);
+    };
 
     // ---- the rows of an item
     PagedItem cur;
@@ -121,6 +120,7 @@ __global__ __launch_bounds__(64, RH == 2 || D == 256 ? 2 : D == 128 ? 3 : 4) voi
     float m[RH], mc[RH], lsum[RH];   // lsum: this lane's quarter of the row sum
     int seg0 = 0;                    // first half of the segment
     auto rows = [&](int first_half) __attribute__((always_inline)) {
+        PagedArgs &p = paged_args();
         cur = walk.item;
         seg0 = first_half;
         no_page = false;
@@ -165,12 +165,7 @@ __global__ __launch_bounds__(64, RH == 2 || D == 256 ? 2 : D == 128 ? 3 : 4) voi
         ++pos;
         bool more = pos < end || (!p.slot_o && !ends);
         int nh = h + 1;
-        if (!x.prefix) no_page |= tokens > 0 && ((uint32_t)x.page[0] >= (uint32_t)p.batch.n_pages || (uint32_t)x.page[1] >= (uint32_t)p.batch.n_pages);
-        // Keys of this half that a row sees: those before its limit (counted from this lane's first).
-        const int edge = x.prefix ? p.n_prefix - 1 - x.at : last_min - x.at;
-        int limit[RH];
-#pragma unroll
-        for (int i = 0; i < RH; ++i) limit[i] = (x.prefix ? p.n_prefix - 1 : last[i]) - x.at - 4 * g;
+        if (!x.prefix) no_page |= x.limit > 0 && !(is_page(x.page[0]) && is_page(x.page[1]));
         if (more && ends) {
             more = walk.next();
             nh = 0;
@@ -191,12 +186,14 @@ __global__ __launch_bounds__(64, RH == 2 || D == 256 ? 2 : D == 128 ? 3 : 4) voi
 #pragma unroll
             for (int r = 0; r < RH; ++r)
                 s[r][i & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[i], qf[r][i >> 1], i < 2 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[r][i & 1], 0, 0, 0);
-        if (edge < 31) {                 // some key is hidden from some row
+        if ((x.prefix ? p.n_prefix - 1 : last_min) - x.at < 31) {   // some key is hidden from some row
 #pragma unroll
-            for (int r = 0; r < RH; ++r)
+            for (int r = 0; r < RH; ++r) {
+                const int limit = (x.prefix ? p.n_prefix - 1 : last[r]) - x.at - 4 * g;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (16 * (j >> 2) + (j & 3) > limit[r]) s[r][j >> 2][j & 3] = -INFINITY;
+                    if (16 * (j >> 2) + (j & 3) > limit) s[r][j >> 2][j & 3] = -INFINITY;
+            }
         }
         float mx[RH];
         bool grows = false;
@@ -253,6 +250,7 @@ __global__ __launch_bounds__(64, RH == 2 || D == 256 ? 2 : D == 128 ? 3 : 4) voi
 
         if (ends || !more) {
             // ---- the segment [seg0, h] of the item is done
+            PagedArgs &p = paged_args();
             const PagedPlace to = paged_place<TR>(p, cur, seg0, h, pos, walk.run, lane);
             bool odd = no_page;
 #pragma unroll
@@ -271,6 +269,17 @@ __global__ __launch_bounds__(64, RH == 2 || D == 256 ? 2 : D == 128 ? 3 : 4) voi
                     const PagedRow row = paged_row(p, cur, to, TR, 16 * r + n);
                     if (!row.valid) continue;
                     if (to.kind == kDirect) {
+                        for (int run = 0; run < p.prefix_runs; ++run) {
+                            const int64_t at = row.flat + (int64_t)(p.prefix_part + run) * p.L * p.Hkv * p.G * p.batch.n_rows;
+                            float f, f2;
+                            join_part(m[r], lsum[r], p.row_ml[2 * at], p.row_ml[2 * at + 1], p.scale_log2, f, f2);
+                            const f32x4 *po = reinterpret_cast<const f32x4 *>(p.row_o + at * D) + g;
+#pragma unroll
+                            for (int db = 0; db < NF; ++db) {
+                                o[r][db] *= f;
+                                if (f2 != 0.f) o[r][db] += f2 * po[4 * db];
+                            }
+                        }
                         const bool none = m[r] == -INFINITY && lsum[r] == 0.f;
                         const float inv = none ? 0.f : 1.f / lsum[r];
                         bf16_t *out = static_cast<bf16_t *>(p.out) + row.l * p.s_o.layer + (int64_t)row.hq * p.s_o.head + (int64_t)row.row * p.s_o.token + 4 * g;

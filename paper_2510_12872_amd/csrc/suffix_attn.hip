@@ -774,7 +774,7 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Par
                 const float ltot = query_sum(lsum[h]);
                 const int r_row = rt * BM + wave * 32 + 16 * h + n_e, i = div_by(r_row, p.by_G);
                 if (i < seq.n) {
-                    const int64_t flat = paged_part_row(p, l, hkv, r_row - i * p.G, seq.first + i, split);
+                    const int64_t flat = paged_part_row(p, l, hkv, r_row - i * p.G, seq.first + i, p.part + split);
                     float *po = p.row_o + flat * D + 4 * g_e;
 #pragma unroll
                     for (int db = 0; db < NF; ++db) *reinterpret_cast<f32x4 *>(po + 16 * db) = o[h][db];
@@ -825,7 +825,21 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Par
             const uint32_t qi_e = (uint32_t)div_by(r_row, p.by_G), hq_e = (uint32_t)(hkv * p.G + r_row) - qi_e * (uint32_t)p.G;
             const bool valid = qi_e < (uint32_t)tq_();
             bf16_t *orow = static_cast<bf16_t *>(p.out) + l * p.s_o.layer + (int64_t)hq_e * p.s_o.head + (int64_t)(seq.first + qi_e) * p.s_o.token;
-            const float ltot = query_sum(lsum[h]);
+            float ltot = query_sum(lsum[h]);
+            if constexpr (kPaged) {
+                for (int run = 0; run < p.join_runs; ++run) {
+                    if (!valid) break;
+                    const int64_t at = paged_part_row(p, l, 0, (int)hq_e, (int)(seq.first + qi_e), p.join_part + run);
+                    float f, f2;
+                    join_part(m[h], ltot, p.join_ml[2 * at], p.join_ml[2 * at + 1], p.scale_log2, f, f2);
+                    const f32x4 *po = reinterpret_cast<const f32x4 *>(p.join_o + at * D) + g_e;
+#pragma unroll
+                    for (int db = 0; db < NF; ++db) {
+                        o[h][db] *= f;
+                        if (f2 != 0.f) o[h][db] += f2 * po[4 * db];
+                    }
+                }
+            }
             if (g_e == 0) ptab[row] = valid ? (uint64_t)(uintptr_t)orow : 0;
             const bool none = kPaged && m[h] == -INFINITY && ltot == 0.f;
             const float inv = none ? 0.f : 1.f / ltot;
