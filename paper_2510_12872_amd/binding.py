@@ -146,7 +146,7 @@ def _load_native(lib):
                       "calls take longer on the host without it", RuntimeWarning, stacklevel=3)
         return _Declines()
     _marshal.bind({n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in _NATIVE_CALLS}, Model, torch.cuda.current_device,
-                  _raw_current_stream)
+                  _raw_current_stream, Batch)
     return _marshal
 
 
@@ -155,7 +155,8 @@ _NATIVE_CALLS = ("kvcomm_weight_slots", "kvcomm_suffix_attn_workspace", "kvcomm_
                  "kvcomm_align_kv_q8", "kvcomm_suffix_attn", "kvcomm_suffix_attn_confined_ws", "kvcomm_anchor_predict",
                  "kvcomm_capture_offsets", "kvcomm_quantize_deltas", "kvcomm_place_qkv", "kvcomm_quantize_kv4", "kvcomm_dequantize_kv4",
                  "kvcomm_suffix_attn_kv4_workspace", "kvcomm_suffix_attn_kv4", "kvcomm_suffix_attn_window_workspace",
-                 "kvcomm_suffix_attn_window")
+                 "kvcomm_suffix_attn_window", "kvcomm_place_qkv_paged", "kvcomm_paged_attn_workspace", "kvcomm_paged_attn",
+                 "kvcomm_paged_attn_prefix_workspace", "kvcomm_paged_attn_prefix")
 
 
 def library_path():
@@ -1083,6 +1084,8 @@ def kvcomm_place_qkv_paged(model, q, k, v, batch, pages_k, pages_v, first_pos=0,
             q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
             if batch.starts is not None:   # rows of no sequence stay as they were: zeros
                 q_out.zero_()
+    if _done(_native.place_qkv_paged(model, q, k, v, batch, pages_k, pages_v, first_pos, q_out, q_weight, k_weight, norm_eps, stream)):
+        return q_out
     n = _int32(next((x.shape[2] for x in (q, k, v) if x is not None), 0), "rows")
     pool = pages_k if pages_k is not None else pages_v
     none, no_pages = _CTensor(None, 0, 0, 0), _CPages(None, 0, 0, 0, 0)
@@ -1134,6 +1137,12 @@ def _paged_attn(model, q, prefix_k, prefix_v, pages_k, pages_v, batch, softmax_s
                 for t, new in zip((out, lse_out), made):
                     if new and t is not None:
                         t.zero_()
+    need = 0   # bytes of scratch to be made here; None: the native module has declined the call
+    if workspace is None:
+        need = _native.paged_attn_workspace(model, q, prefix_k, prefix_v, pages_k, pages_v, batch)
+        workspace = _attn_scratch(need, q.device, stream) if need else None
+    if need is not None and _done(_native.paged_attn(model, q, prefix_k, prefix_v, pages_k, pages_v, batch, softmax_scale, out, lse_out, workspace, stream)):
+        return (out, lse_out) if want_lse else out
     ck, cv = _pages_of(model, pages_k, pages_v)
     n = _int32(q.shape[2], "rows")
     cbatch, cmodel = _batch(batch, n, pages_k.shape[3], pages_k.shape[2]), model.c()

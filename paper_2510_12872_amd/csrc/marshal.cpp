@@ -49,13 +49,19 @@ struct Library {
     decltype(&kvcomm_suffix_attn_kv4) suffix_attn_kv4;
     decltype(&kvcomm_suffix_attn_window_workspace) attn_window_workspace;
     decltype(&kvcomm_suffix_attn_window) suffix_attn_window;
-    PyObject *model_type, *current_device, *current_stream;
+    decltype(&kvcomm_place_qkv_paged) place_qkv_paged;
+    decltype(&kvcomm_paged_attn_workspace) paged_attn_workspace;
+    decltype(&kvcomm_paged_attn) paged_attn;
+    decltype(&kvcomm_paged_attn_prefix_workspace) paged_attn_prefix_workspace;
+    decltype(&kvcomm_paged_attn_prefix) paged_attn_prefix;
+    PyObject *model_type, *current_device, *current_stream, *batch_type;
 } lib;
 
 struct Names {
     PyObject *n_layers, *n_kv_heads, *n_q_heads, *head_dim, *dtype, *rope_theta, *cuda_stream, *device_index;
     PyObject *seg_base_k, *anchor_base_k, *anchor_len, *base_k, *base_v, *anchor_dk, *anchor_dv, *anchor_dk8, *anchor_dv8, *scale_k,
         *scale_v, *weights, *delta_pos, *anchor_delta_pos, *out_k, *out_v;
+    PyObject *table, *lens, *starts, *max_rows;
 } names;
 
 // ------------------------------------------------------------------------------------------ plain values
@@ -89,6 +95,19 @@ const at::Tensor &as_tensor(PyObject *o)
     return t;
 }
 
+struct py {   // owned reference
+    PyObject *o;
+    explicit py(PyObject *p) : o(p) {}
+    py(py &&r) : o(r.o) { r.o = nullptr; }
+    ~py() { Py_XDECREF(o); }
+};
+py attribute(PyObject *o, PyObject *name)
+{
+    PyObject *v = PyObject_GetAttr(o, name);
+    if (!v) throw Decline{};
+    return py(v);
+}
+
 struct Call {   // the model of a call and its tensors' type
     kvcomm_model m;
     at::ScalarType dtype;
@@ -96,11 +115,7 @@ struct Call {   // the model of a call and its tensors' type
     explicit Call(PyObject *model)
     {
         if (Py_TYPE(model) != (PyTypeObject *)lib.model_type) throw Decline{};
-        auto get = [&](PyObject *name) {
-            PyObject *v = PyObject_GetAttr(model, name);
-            if (!v) throw Decline{};
-            return py(v);
-        };
+        auto get = [&](PyObject *name) { return attribute(model, name); };
         m.n_layers = as_int(get(names.n_layers).o);
         m.n_kv_heads = as_int(get(names.n_kv_heads).o);
         m.n_q_heads = as_int(get(names.n_q_heads).o);
@@ -120,13 +135,6 @@ struct Call {   // the model of a call and its tensors' type
         return t;
     }
 
-private:
-    struct py {   // owned reference
-        PyObject *o;
-        explicit py(PyObject *p) : o(p) {}
-        py(py &&r) : o(r.o) { r.o = nullptr; }
-        ~py() { Py_XDECREF(o); }
-    };
 };
 
 // [layer, head, token, channel] tensor with contiguous channels
@@ -586,6 +594,29 @@ PyObject *suffix_attn_window(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// The norm of a placement: weights of queries and keys [D] or [L, D], or None, and eps
+struct Norm {
+    const void *w[2] = {};
+    int64_t stride[2] = {};
+    float eps;
+    Norm(const Call &c, PyObject *q_weight, PyObject *k_weight, PyObject *norm_eps)
+    {
+        PyObject *const o[2] = {q_weight, k_weight};
+        for (int i = 0; i < 2; ++i) {
+            if (o[i] == Py_None) continue;
+            const at::Tensor &t = c.on(as_tensor(o[i]));
+            const int64_t d = t.dim();
+            if (t.scalar_type() != c.dtype || d < 1 || d > 2 || t.size(d - 1) != c.m.head_dim || t.stride(d - 1) != 1 || (d == 2 && t.size(0) != c.m.n_layers))
+                throw Decline{};
+            w[i] = t.data_ptr();
+            stride[i] = d == 2 ? t.stride(0) : 0;
+        }
+        const double x = as_double(norm_eps);
+        eps = (float)x;
+        if (eps == 0.f && x != 0.0) throw Decline{};   // (would mean no norm)
+    }
+};
+
 // (model, q, k, v, first_pos, q_weight, k_weight, norm_eps, q_out, k_out, v_out, stream); None in the place of a pair or a weight that is not given
 PyObject *place_qkv(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -603,24 +634,135 @@ PyObject *place_qkv(PyObject *, PyObject *const *args, Py_ssize_t n)
             out[i] = sized(c, y, c.dtype, heads, tokens, c.m.head_dim);
         }
         if (tokens < 0) throw Decline{};
-        const void *w[2] = {};
-        int64_t ws[2] = {};
-        for (int i = 0; i < 2; ++i) {
-            if (a[5 + i] == Py_None) continue;
-            const at::Tensor &t = c.on(as_tensor(a[5 + i]));
-            const int64_t d = t.dim();
-            if (t.scalar_type() != c.dtype || d < 1 || d > 2 || t.size(d - 1) != c.m.head_dim || t.stride(d - 1) != 1 || (d == 2 && t.size(0) != c.m.n_layers))
-                throw Decline{};
-            w[i] = t.data_ptr();
-            ws[i] = d == 2 ? t.stride(0) : 0;
-        }
+        const Norm norm(c, a[5], a[6], a[7]);
         const int32_t first = as_int(a[4]);
-        const double norm_eps = as_double(a[7]);
-        const float eps = (float)norm_eps;
-        if (eps == 0.f && norm_eps != 0.0) throw Decline{};   // (would mean no norm)
         void *stream = stream_of(c, a[11]);
         return unlocked([&] {
-            return lib.place_qkv(&c.m, in[0], in[1], in[2], (int32_t)tokens, first, w[0], w[1], ws[0], ws[1], eps, out[0], out[1], out[2], stream);
+            return lib.place_qkv(&c.m, in[0], in[1], in[2], (int32_t)tokens, first, norm.w[0], norm.w[1], norm.stride[0], norm.stride[1], norm.eps, out[0], out[1], out[2], stream);
+        });
+    });
+}
+
+// A pool [L, Hkv, pages, slots, D]; n_pages, page_size: of the pools seen before, or negative
+kvcomm_pages pages(const Call &c, PyObject *o, int64_t &n_pages, int64_t &page_size)
+{
+    const at::Tensor &t = c.on(as_tensor(o));
+    if (t.dim() != 5 || t.scalar_type() != c.dtype || t.size(0) != c.m.n_layers || t.size(1) != c.m.n_kv_heads || t.size(4) != c.m.head_dim || t.stride(4) != 1)
+        throw Decline{};
+    if (n_pages < 0) {
+        n_pages = t.size(2);
+        page_size = t.size(3);
+    }
+    if (t.size(2) != n_pages || t.size(3) != page_size || n_pages > INT32_MAX || page_size > INT32_MAX) throw Decline{};
+    return kvcomm_pages{t.data_ptr(), t.stride(0), t.stride(1), t.stride(2), t.stride(3)};
+}
+
+// A Batch over pools of these pages
+kvcomm_batch batch_of(const Call &c, PyObject *o, int32_t n_rows, int64_t n_pages, int64_t page_size)
+{
+    if (Py_TYPE(o) != (PyTypeObject *)lib.batch_type) throw Decline{};
+    auto ints = [&](PyObject *x, int64_t dim) -> const at::Tensor & {
+        const at::Tensor &t = c.on(as_tensor(x));
+        if (t.scalar_type() != at::kInt || t.dim() != dim || (t.size(dim - 1) > 1 && t.stride(dim - 1) != 1)) throw Decline{};
+        return t;
+    };
+    const py table_o = attribute(o, names.table), lens_o = attribute(o, names.lens), starts_o = attribute(o, names.starts), most_o = attribute(o, names.max_rows);
+    const at::Tensor &table = ints(table_o.o, 2), &lens = ints(lens_o.o, 1);
+    const int64_t B = lens.size(0);
+    if (table.size(0) != B || B > INT32_MAX || table.size(1) > INT32_MAX) throw Decline{};
+    const void *starts = nullptr;
+    if (starts_o.o != Py_None) {
+        const at::Tensor &t = ints(starts_o.o, 1);
+        if (t.size(0) != B + 1) throw Decline{};
+        starts = t.data_ptr();
+    }
+    return kvcomm_batch{static_cast<const int32_t *>(table.data_ptr()), static_cast<const int32_t *>(lens.data_ptr()), static_cast<const int32_t *>(starts),
+                        B > 1 ? table.stride(0) : 0, (int32_t)table.size(1), (int32_t)B, n_rows, (int32_t)page_size, (int32_t)n_pages, as_int(most_o.o)};
+}
+
+// (model, q, k, v, batch, pages_k, pages_v, first_pos, q_out, q_weight, k_weight, norm_eps, stream); None in the place of a pair or a weight that is not given
+PyObject *place_qkv_paged(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return entry<13>(args, n, [](PyObject *const *a) {
+        const Call c(a[0]);
+        int64_t rows = -1, n_pages = -1, page_size = 16;
+        kvcomm_tensor in[3] = {}, out = {};
+        kvcomm_pages pool[2] = {};
+        PyObject *const to[3] = {a[8], a[5], a[6]};
+        for (int i = 0; i < 3; ++i) {
+            PyObject *x = a[1 + i], *y = to[i];
+            if ((x == Py_None) != (y == Py_None)) throw Decline{};
+            if (x == Py_None) continue;
+            if (rows < 0) rows = tokens_of(as_tensor(x));
+            const int64_t heads = i == 0 ? c.m.n_q_heads : c.m.n_kv_heads;
+            in[i] = sized(c, x, c.dtype, heads, rows, c.m.head_dim);
+            if (i)
+                pool[i - 1] = pages(c, y, n_pages, page_size);
+            else
+                out = sized(c, y, c.dtype, heads, rows, c.m.head_dim);
+        }
+        if (rows < 0) throw Decline{};
+        const kvcomm_batch b = batch_of(c, a[4], (int32_t)rows, std::max<int64_t>(n_pages, 0), page_size);
+        const Norm norm(c, a[9], a[10], a[11]);
+        const int32_t first = as_int(a[7]);
+        void *stream = stream_of(c, a[12]);
+        return unlocked([&] {
+            return lib.place_qkv_paged(&c.m, in[0], in[1], in[2], &b, first, norm.w[0], norm.w[1], norm.stride[0], norm.stride[1], norm.eps, out, pool[0], pool[1], stream);
+        });
+    });
+}
+
+// What the attention calls over pages share, from (model, q, prefix_k or None, prefix_v, pages_k, pages_v, batch)
+struct Paged {
+    Call c;
+    int32_t rows, n_prefix = 0;
+    kvcomm_tensor q, pk = {}, pv = {};
+    kvcomm_pages k, v;
+    kvcomm_batch b;
+    explicit Paged(PyObject *const *a) : c(a[0]), rows(tokens_of(as_tensor(a[1])))
+    {
+        q = sized(c, a[1], c.dtype, c.m.n_q_heads, rows, c.m.head_dim);
+        if (a[2] != Py_None) {
+            n_prefix = tokens_of(as_tensor(a[2]));
+            if (n_prefix == 0) throw Decline{};
+            pk = sized(c, a[2], c.dtype, c.m.n_kv_heads, n_prefix, c.m.head_dim);
+            pv = sized(c, a[3], c.dtype, c.m.n_kv_heads, n_prefix, c.m.head_dim);
+        }
+        int64_t n_pages = -1, page_size = -1;
+        k = pages(c, a[4], n_pages, page_size);
+        v = pages(c, a[5], n_pages, page_size);
+        b = batch_of(c, a[6], rows, n_pages, page_size);
+    }
+};
+
+PyObject *paged_attn_workspace(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return entry<7>(args, n, [](PyObject *const *a) {
+        const Paged p(a);
+        return (long long)(p.n_prefix ? lib.paged_attn_prefix_workspace(&p.c.m, p.n_prefix, &p.b) : lib.paged_attn_workspace(&p.c.m, &p.b));
+    });
+}
+
+// (..., softmax_scale, out, lse_out, workspace, stream)
+PyObject *paged_attn(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return entry<12>(args, n, [](PyObject *const *a) {
+        const Paged p(a);
+        const Call &c = p.c;
+        const float scale = (float)as_double(a[7]);
+        const kvcomm_tensor out = sized(c, a[8], c.dtype, c.m.n_q_heads, p.rows, c.m.head_dim);
+        float *lse = nullptr;
+        if (a[9] != Py_None) {
+            const at::Tensor &t = c.on(as_tensor(a[9]));
+            if (t.scalar_type() != at::kFloat || !t.is_contiguous() || t.numel() != (int64_t)c.m.n_layers * c.m.n_q_heads * p.rows) throw Decline{};
+            lse = static_cast<float *>(t.data_ptr());
+        }
+        const Scratch ws(a[10]);
+        if (a[10] != Py_None) c.on(as_tensor(a[10]));
+        void *stream = stream_of(c, a[11]);
+        return unlocked([&] {
+            return p.n_prefix ? lib.paged_attn_prefix(&c.m, p.q, p.pk, p.pv, p.n_prefix, p.k, p.v, &p.b, scale, out, lse, ws.ptr, ws.bytes, stream)
+                              : lib.paged_attn(&c.m, p.q, p.k, p.v, &p.b, scale, out, lse, ws.ptr, ws.bytes, stream);
         });
     });
 }
@@ -725,11 +867,11 @@ PyObject *apart(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
-// bind(addresses by entry point's name, Model, current_device, current_stream or None)
+// bind(addresses by entry point's name, Model, current_device, current_stream or None, Batch); without Batch the calls on batches are declined
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    if (n != 4 || !PyDict_CheckExact(a[0])) {
-        PyErr_SetString(PyExc_TypeError, "bind(dict, Model, current_device, current_stream)");
+    if (n < 4 || n > 5 || !PyDict_CheckExact(a[0])) {
+        PyErr_SetString(PyExc_TypeError, "bind(dict, Model, current_device, current_stream, Batch)");
         return nullptr;
     }
     auto set = [&](auto &fn, const char *name) {
@@ -748,14 +890,18 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
         !set(lib.quantize_deltas, "kvcomm_quantize_deltas") || !set(lib.place_qkv, "kvcomm_place_qkv") ||
         !set(lib.quantize_kv4, "kvcomm_quantize_kv4") || !set(lib.dequantize_kv4, "kvcomm_dequantize_kv4") ||
         !set(lib.attn_kv4_workspace, "kvcomm_suffix_attn_kv4_workspace") || !set(lib.suffix_attn_kv4, "kvcomm_suffix_attn_kv4") ||
-        !set(lib.attn_window_workspace, "kvcomm_suffix_attn_window_workspace") || !set(lib.suffix_attn_window, "kvcomm_suffix_attn_window")) {
+        !set(lib.attn_window_workspace, "kvcomm_suffix_attn_window_workspace") || !set(lib.suffix_attn_window, "kvcomm_suffix_attn_window") ||
+        !set(lib.place_qkv_paged, "kvcomm_place_qkv_paged") || !set(lib.paged_attn_workspace, "kvcomm_paged_attn_workspace") ||
+        !set(lib.paged_attn, "kvcomm_paged_attn") || !set(lib.paged_attn_prefix_workspace, "kvcomm_paged_attn_prefix_workspace") ||
+        !set(lib.paged_attn_prefix, "kvcomm_paged_attn_prefix")) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_KeyError, "an entry point of the library is missing");
         return nullptr;
     }
-    for (int i = 1; i < 4; ++i) Py_INCREF(a[i]);   // kept until the process ends
+    for (int i = 1; i < n; ++i) Py_INCREF(a[i]);   // kept until the process ends
     lib.model_type = a[1];
     lib.current_device = a[2];
     lib.current_stream = a[3];
+    lib.batch_type = n == 5 ? a[4] : nullptr;
     Py_RETURN_NONE;
 }
 
@@ -779,6 +925,9 @@ PyMethodDef methods[] = {FAST("bind", bind),
                          FAST("suffix_attn_kv4", suffix_attn_kv4),
                          FAST("suffix_attn_window_workspace", suffix_attn_window_workspace),
                          FAST("suffix_attn_window", suffix_attn_window),
+                         FAST("place_qkv_paged", place_qkv_paged),
+                         FAST("paged_attn_workspace", paged_attn_workspace),
+                         FAST("paged_attn", paged_attn),
                          FAST("apart", apart),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -792,7 +941,7 @@ PyMODINIT_FUNC PyInit__marshal(void)
     NAME(n_layers); NAME(n_kv_heads); NAME(n_q_heads); NAME(head_dim); NAME(dtype); NAME(rope_theta); NAME(cuda_stream); NAME(device_index);
     NAME(seg_base_k); NAME(anchor_base_k); NAME(anchor_len); NAME(base_k); NAME(base_v); NAME(anchor_dk); NAME(anchor_dv);
     NAME(anchor_dk8); NAME(anchor_dv8); NAME(scale_k); NAME(scale_v); NAME(weights); NAME(delta_pos); NAME(anchor_delta_pos);
-    NAME(out_k); NAME(out_v);
+    NAME(out_k); NAME(out_v); NAME(table); NAME(lens); NAME(starts); NAME(max_rows);
 #undef NAME
     PyObject *m = PyModule_Create(&module);
     if (m && PyModule_AddStringConstant(m, "built_for", KVC_BUILT_FOR) < 0) {
