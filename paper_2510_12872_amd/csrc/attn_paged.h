@@ -361,7 +361,10 @@ private:
 #endif
 constexpr int paged_rows_waves(int D, int rows) { return D == 256 ? 5 : rows == 32 ? 8 : D == 128 ? KW128 : 16; }
 
+constexpr int paged_f32_waves(int D) { return D == 256 ? 4 : 8; }
+
 int launch_paged_rows(const PagedAttnParams &p, int tile_rows, hipStream_t s);
+int launch_paged_f32(const PagedAttnParams &p, hipStream_t s);   // tiles of 16 rows
 
 // Where the results of a segment, halves seg0 ... h of an item, go.  pos: the axis behind the segment, run: a wavefront's run of it.
 struct PagedPlace {
@@ -434,6 +437,39 @@ __device__ __forceinline__ PagedRow paged_row(const P &p, const PagedItem &it, c
     x.flat = ((int64_t)x.l * p.Hkv * p.G + x.hq) * p.batch.n_rows + x.row;
     x.o = to.kind == 0 ? r : x.flat;
     return x;
+}
+
+// A row's results: the lanes g = 0 ... 3 of a row hold reference, sum and, in pieces of four channels from channel(i) on, its outputs.
+template <typename T, int D, class P, class C>
+__device__ __forceinline__ void paged_finish_row(const P &p, const PagedPlace &to, const PagedRow &row, int g, float m, float l, f32x4 (&o)[D / 16], C channel)
+{
+    if (to.kind != kDirect) {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4 *>(to.o + row.o * D + channel(i)) = o[i];
+        if (g < 2) to.ml[row.o * 2 + g] = g ? l : m;
+        return;
+    }
+    for (int run = 0; run < p.prefix_runs; ++run) {
+        const int64_t at = row.flat + (int64_t)(p.prefix_part + run) * p.L * p.Hkv * p.G * p.batch.n_rows;
+        float f, f2;
+        join_part(m, l, p.row_ml[2 * at], p.row_ml[2 * at + 1], p.scale_log2, f, f2);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            o[i] *= f;
+            if (f2 != 0.f) o[i] += f2 * *reinterpret_cast<const f32x4 *>(p.row_o + at * D + channel(i));
+        }
+    }
+    const bool none = m == -INFINITY && l == 0.f;
+    const float inv = none ? 0.f : 1.f / l;
+    T *out = static_cast<T *>(p.out) + row.l * p.s_o.layer + (int64_t)row.hq * p.s_o.head + (int64_t)row.row * p.s_o.token;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+        if constexpr (sizeof(T) == 2)
+            *reinterpret_cast<u32x2 *>(out + channel(i)) = u32x2{pack_bf16x2(o[i][0] * inv, o[i][1] * inv), pack_bf16x2(o[i][2] * inv, o[i][3] * inv)};
+        else
+            *reinterpret_cast<f32x4 *>(out + channel(i)) = o[i] * inv;
+    }
+    if (p.lse && g == 0) p.lse[row.flat] = none ? -INFINITY : m * p.scale + logf(l);
 }
 
 // The segment by the formula.

@@ -6,26 +6,6 @@ namespace {
 
 using namespace kvc;
 
-// One wavefront per (layer, query head, row).
-template <typename T, int D>
-__global__ __launch_bounds__(256) void attn_paged_row_kernel(const PagedAttnParams p)
-{
-    const int lane = threadIdx.x & 63, Hq = p.Hkv * p.G;
-    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (item >= (int64_t)p.L * Hq * p.batch.n_rows) return;
-    const int row = (int)(item % p.batch.n_rows), head = (int)(item / p.batch.n_rows), l = head / Hq, hq = head - l * Hq;
-    const int b = sequence_of(p.batch, row, lane);
-    if (b < 0) return;
-    int first, n;
-    sequence_rows(p.batch, b, first, n);
-    if (row < first || row >= first + n) return;
-    const int len = sequence_len(p.batch, b), last = last_seen(len, n, row - first, p.batch.cap);
-    const int prefix_halves = (p.n_prefix + 31) / 32;
-    float m, sum, o[8];
-    paged_exact_row<T, D>(p, l, hq / p.G, hq, row, b, last, prefix_halves, 0, prefix_halves + (last + 32) / 32, lane, m, sum, o);
-    paged_store_row<T, D>(p, l, hq, row, lane, m, sum, o);
-}
-
 // The results of rows whose keys went to several wavefronts or runs: out = sum_s f_s O_s / sum_s f_s l_s, f_s = exp2((m_s - max m) scale log2 e), parts in
 // a fixed order.  A wavefront takes `heads` query heads of a (layer, row); D / 4 lanes hold an output's channels, and the 64 / (D / 4) such groups take the
 // parts in turn.
@@ -56,23 +36,28 @@ __global__ __launch_bounds__(256) void attn_paged_combine_kernel(const CombinePa
     };
     const int64_t all = (int64_t)p.L * Hq * n_rows;
     const int group = lane / CL, c = 4 * (lane % CL);
-    for (int hq = chunk * p.heads; hq < min(Hq, (chunk + 1) * p.heads); ++hq) {
-        const int hkv = div_by(hq, p.by_G), g = hq - hkv * p.G;
+    auto parts_of = [&](int hkv, int index, int packed) -> Parts {
+        const int32_t *e = p.items + ((int64_t)(l * p.Hkv + hkv) * p.max_items + max(0, min(index, p.max_items - 1))) * 2;
+        const int w0 = e[0], w1 = e[1];
+        if (w0 < 0) return Parts{w0, 1, 0, true};
+        const int last = max(0, min(w1, p.n_waves - 1)), from = min(w0, last);
+        return Parts{from, last - from + 1, packed & (p.tile_rows - 1), false};
+    };
+    auto own_of = [&](int hq) -> Parts {
+        if (item < 0) return Parts{item, p.tile_runs, 0, true};
+        const int hkv = div_by(hq, p.by_G), packed = number * p.G + hq - hkv * p.G;
+        return parts_of(hkv, item + (int)((uint32_t)packed / (uint32_t)p.tile_rows), packed);
+    };
+    // A head per lane: which of them are not done (of most large batches nearly all are).
+    const int head0 = chunk * p.heads, head = head0 + lane;
+    for (uint64_t todo = __builtin_amdgcn_ballot_w64(lane < p.heads && head < Hq && own_of(min(head, Hq - 1)).wave != kDirect); todo; todo &= todo - 1) {
+        const int hq = head0 + __builtin_ctzll(todo), hkv = div_by(hq, p.by_G), g = hq - hkv * p.G;
         const int64_t flat = ((int64_t)l * Hq + hq) * n_rows + row;
-        auto parts_of = [&](int index, int packed) -> Parts {
-            const int32_t *e = p.items + ((int64_t)(l * p.Hkv + hkv) * p.max_items + max(0, min(index, p.max_items - 1))) * 2;
-            const int w0 = e[0], w1 = e[1];
-            if (w0 < 0) return Parts{w0, 1, 0, true};
-            const int last = max(0, min(w1, p.n_waves - 1)), from = min(w0, last);
-            return Parts{from, last - from + 1, packed & (p.tile_rows - 1), false};
-        };
-        const int packed = number * p.G + g;
-        const Parts own = item < 0 ? Parts{item, p.tile_runs, 0, true} : parts_of(item + (int)((uint32_t)packed / (uint32_t)p.tile_rows), packed);
-        if (own.wave == kDirect) continue;
+        const Parts own = own_of(hq);
         Parts before = {0, p.prefix_runs, 0, true};
         if (p.prefix_tiles) {
             const int at = (row - first) * p.G + g;
-            before = parts_of((int)((uint32_t)at / (uint32_t)p.tile_rows), at);
+            before = parts_of(hkv, (int)((uint32_t)at / (uint32_t)p.tile_rows), at);
         }
         const int count = own.count + (apart ? before.count : 0);
         auto place = [&](int k, const float *&o, const float *&ml) {
@@ -152,7 +137,7 @@ int launch_combine(const PagedAttnParams &a, hipStream_t s)
     static_cast<PagedAttnParams &>(p) = a;
     const int Hq = a.Hkv * a.G;
     const int64_t rows = (int64_t)a.L * a.batch.n_rows;
-    p.heads = (int)std::min<int64_t>(Hq, std::max<int64_t>(1, rows * Hq / 4096));   // a wavefront's: as many as leave a few per SIMD
+    p.heads = (int)std::min<int64_t>(std::min(Hq, 64), std::max<int64_t>(1, rows * Hq / 4096));   // a wavefront's: as many as leave a few per SIMD
     p.chunks = (Hq + p.heads - 1) / p.heads;
     p.by_chunks = make_divisor((uint32_t)p.chunks);
     p.by_rows = make_divisor((uint32_t)a.batch.n_rows);
@@ -184,9 +169,10 @@ Plan plan_of(const kvcomm_model &m, const kvcomm_batch &b, int n_prefix)
     const int G = m.n_q_heads / m.n_kv_heads, D = m.head_dim;
     const int64_t LH = (int64_t)m.n_layers * m.n_kv_heads, rows = (int64_t)b.n_rows * G;
     const int64_t most = b.starts ? (b.max_rows ? std::min<int64_t>(b.max_rows, b.n_rows) : b.n_rows) * G : G;
-    pl.tiles = most > kFewRows;
-    pl.tile_rows = D < 256 && (most > 16 || (n_prefix && rows > 16 && rows <= kFewRows)) ? 32 : 16;
-    pl.n_waves = kChipCUs * paged_rows_waves(D, pl.tile_rows);
+    const bool f32 = m.dtype == KVCOMM_F32;   // the wavefront kernel takes it all
+    pl.tiles = !f32 && most > kFewRows;
+    pl.tile_rows = f32 ? 16 : D < 256 && (most > 16 || (n_prefix && rows > 16 && rows <= kFewRows)) ? 32 : 16;
+    pl.n_waves = kChipCUs * (f32 ? paged_f32_waves(D) : paged_rows_waves(D, pl.tile_rows));
     pl.max_items = b.starts ? (pl.tiles ? (int64_t)b.n_seqs * (kFewRows / pl.tile_rows) : rows / pl.tile_rows + b.n_seqs) : (int64_t)b.n_seqs * ((G + pl.tile_rows - 1) / pl.tile_rows);
     pl.seq_runs = 1;
     if (pl.tiles) {
@@ -196,7 +182,7 @@ Plan plan_of(const kvcomm_model &m, const kvcomm_batch &b, int n_prefix)
         while (pl.seq_runs < kTileMaxSplits && tiles * LH * pl.seq_runs * 2 <= kChipCUs && reach >= 1024 * pl.seq_runs) pl.seq_runs *= 2;
         pl.seq_units = tiles * pl.seq_runs;
     }
-    if (n_prefix && rows <= kFewRows) {
+    if (n_prefix && (f32 || rows <= kFewRows)) {
         pl.prefix_tiles = (int)((rows + pl.tile_rows - 1) / pl.tile_rows);
         pl.max_items += pl.prefix_tiles;
     } else if (n_prefix) {
@@ -266,15 +252,6 @@ int paged_attn(const kvcomm_model *model, const kvcomm_tensor &q, const kvcomm_t
     p.D = D;
     const int64_t rows = (int64_t)p.L * p.Hkv * p.G * p.batch.n_rows;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (dt == KVCOMM_F32) {
-        if (rows >= 67108864) return KVCOMM_EUNSUPPORTED;
-        const dim3 grid((unsigned)((rows + 3) / 4)), block(256);
-        switch (D) {
-            case 64: return launch(attn_paged_row_kernel<float, 64>, grid, block, 0, s, p);
-            case 128: return launch(attn_paged_row_kernel<float, 128>, grid, block, 0, s, p);
-            default: return launch(attn_paged_row_kernel<float, 256>, grid, block, 0, s, p);
-        }
-    }
     const Plan pl = plan_of(*model, *batch, n_prefix);
     const bool scratch = workspace && aligned16(workspace) && workspace_bytes >= pl.bytes;
     const int64_t LH = (int64_t)p.L * p.Hkv;
@@ -291,7 +268,7 @@ int paged_attn(const kvcomm_model *model, const kvcomm_tensor &q, const kvcomm_t
     p.max_items = (int32_t)pl.max_items;
     if (!scratch) {
         p.walked_prefix = (n_prefix + 31) / 32;
-        return launch_paged_rows(p, pl.tile_rows, s);
+        return dt == KVCOMM_F32 ? launch_paged_f32(p, s) : launch_paged_rows(p, pl.tile_rows, s);
     }
     float *x = static_cast<float *>(workspace);
     auto take = [&](int64_t n) { float *y = x; x += n; return y; };
@@ -333,6 +310,10 @@ int paged_attn(const kvcomm_model *model, const kvcomm_tensor &q, const kvcomm_t
     };
     if (pl.prefix_runs && (st = tiles_of(true))) return st;
     if (pl.tiles && (st = tiles_of(false))) return st;
+    if (dt == KVCOMM_F32) {
+        st = launch_paged_f32(p, s);
+        return st ? st : launch_combine<float>(p, s);
+    }
     if ((st = launch_paged_rows(p, pl.tile_rows, s))) return st;
     return launch_combine<bf16_t>(p, s);
 }
@@ -340,7 +321,7 @@ int paged_attn(const kvcomm_model *model, const kvcomm_tensor &q, const kvcomm_t
 size_t workspace_of(const kvcomm_model *model, const kvcomm_batch *batch, int32_t n_prefix)
 {
     Batch b;
-    if (check_model(model) || check_batch(batch, b) || n_prefix < 0 || (int64_t)n_prefix + b.cap > kMaxPagedTokens || model->dtype != KVCOMM_BF16 || !countable(*model, *batch)) return 0;
+    if (check_model(model) || check_batch(batch, b) || n_prefix < 0 || (int64_t)n_prefix + b.cap > kMaxPagedTokens || !countable(*model, *batch)) return 0;
     return plan_of(*model, *batch, n_prefix).bytes;
 }
 

@@ -267,32 +267,7 @@ __global__ __launch_bounds__(64, RH == 2 || D >= 128 ? 2 : 4) void attn_paged_ro
 #pragma unroll
                 for (int r = 0; r < RH; ++r) {
                     const PagedRow row = paged_row(p, cur, to, TR, 16 * r + n);
-                    if (!row.valid) continue;
-                    if (to.kind == kDirect) {
-                        for (int run = 0; run < p.prefix_runs; ++run) {
-                            const int64_t at = row.flat + (int64_t)(p.prefix_part + run) * p.L * p.Hkv * p.G * p.batch.n_rows;
-                            float f, f2;
-                            join_part(m[r], lsum[r], p.row_ml[2 * at], p.row_ml[2 * at + 1], p.scale_log2, f, f2);
-                            const f32x4 *po = reinterpret_cast<const f32x4 *>(p.row_o + at * D) + g;
-#pragma unroll
-                            for (int db = 0; db < NF; ++db) {
-                                o[r][db] *= f;
-                                if (f2 != 0.f) o[r][db] += f2 * po[4 * db];
-                            }
-                        }
-                        const bool none = m[r] == -INFINITY && lsum[r] == 0.f;
-                        const float inv = none ? 0.f : 1.f / lsum[r];
-                        bf16_t *out = static_cast<bf16_t *>(p.out) + row.l * p.s_o.layer + (int64_t)row.hq * p.s_o.head + (int64_t)row.row * p.s_o.token + 4 * g;
-#pragma unroll
-                        for (int db = 0; db < NF; ++db)
-                            *reinterpret_cast<u32x2 *>(out + 16 * db) = u32x2{pack_bf16x2(o[r][db][0] * inv, o[r][db][1] * inv), pack_bf16x2(o[r][db][2] * inv, o[r][db][3] * inv)};
-                        if (p.lse && g == 0) p.lse[row.flat] = none ? -INFINITY : m[r] * p.scale + logf(lsum[r]);
-                    } else {
-                        float *po = to.o + row.o * D + 4 * g;
-#pragma unroll
-                        for (int db = 0; db < NF; ++db) *reinterpret_cast<f32x4 *>(po + 16 * db) = o[r][db];
-                        if (g < 2) to.ml[row.o * 2 + g] = g ? lsum[r] : m[r];
-                    }
+                    if (row.valid) paged_finish_row<bf16_t, D>(p, to, row, g, m[r], lsum[r], o[r], [&](int i) { return 16 * i + 4 * g; });
                 }
             }
             if (!more) return;
