@@ -168,10 +168,7 @@ __device__ __forceinline__ void paged_store_row(const P &p, int l, int hq, int r
 }
 
 // ------------------------------------------------------------------------------------------ the walk
-#ifndef KMIN
-#define KMIN 1
-#endif
-constexpr int kPagedMinRun = KMIN;   // halves of a wavefront's run at least
+constexpr int kPagedShortRun = 8;   // halves of runs that are cut within items, at most
 typedef const __attribute__((address_space(4))) int32_t const_int;   // read through the scalar cache (whole-wavefront values)
 __device__ __forceinline__ const_int *scalar(const int32_t *x) { return (const_int *)(uintptr_t)x; }
 
@@ -213,6 +210,7 @@ struct PagedWalk {
     const int lane;
     int width = 0;   // halves of a (layer, kv head) on the axis
     int run = 0;     // of a wavefront
+    int pad = 1;     // items begin at multiples of this on the axis: 1, or `run`
     PagedItem item = {};
 
     __device__ __forceinline__ explicit PagedWalk(int lane) : lane(lane) {}
@@ -225,60 +223,77 @@ struct PagedWalk {
     __device__ __forceinline__ static int count_of(PagedArgs &p, int len) { return max(1, p.walked_prefix + (min(len, p.batch.cap) + 31) / 32); }
     __device__ __forceinline__ static int prefix_count(PagedArgs &p) { return (p.n_prefix + 31) / 32; }
 
-    // Halves of the sequences c ... c + 63 up to each lane's, and that lane's row tiles.
-    __device__ __forceinline__ int scan(PagedArgs &p, int c, int &tiles) const
+    __device__ __forceinline__ int padded(int count) const { return pad == 1 ? count : (int)((uint32_t)(count + pad - 1) / (uint32_t)pad) * pad; }
+
+    // Halves of the sequences c ... c + 63 up to each lane's, that lane's row tiles, and its halves of one.
+    __device__ __forceinline__ int scan(PagedArgs &p, int c, int &tiles, int &count) const
     {
         const int b = c + lane;
-        int x = 0;
         tiles = 0;
+        count = 1;
         if (b < p.batch.n_seqs) {
             int first, n;
             sequence_rows(p.batch, b, first, n);
             tiles = tiles_of(p, n);
-            x = tiles * count_of(p, sequence_len(p.batch, b));
+            count = count_of(p, sequence_len(p.batch, b));
         }
-        return wave_scan(x);
+        return wave_scan(tiles * padded(count));
     }
 
     // The first item that wavefront `wave` works on, and its halves of it; false: none.
     __device__ __forceinline__ bool begin(int wave, int64_t &pos, int64_t &end, int &h0)
     {
         PagedArgs &p = paged_args();
-        const int ahead = p.prefix_tiles * prefix_count(p);
-        int tiles;
-        int upto = scan(p, 0, tiles);   // (kept: most batches have no more)
+        const int heads = p.L * p.Hkv;
+        int tiles, count, items = p.prefix_tiles, ahead = p.prefix_tiles * prefix_count(p);
+        int upto = scan(p, 0, tiles, count);   // (kept: most batches have no more)
+        int before = wave_scan(tiles);
         width = ahead + __builtin_amdgcn_readlane(upto, 63);
+        items += __builtin_amdgcn_readlane(before, 63);
         for (int c = 64; c < p.batch.n_seqs; c += 64) {
-            int t;
-            width += __builtin_amdgcn_readlane(scan(p, c, t), 63);
+            int t, n;
+            width += __builtin_amdgcn_readlane(scan(p, c, t, n), 63);
+            items += __builtin_amdgcn_readlane(wave_scan(t), 63);
         }
-        const int64_t total = (int64_t)width * (p.L * p.Hkv);
+        int64_t total = (int64_t)width * heads;
         // (a little more than its share each, so that rounding leaves nothing)
-        run = max(kPagedMinRun, __builtin_amdgcn_readfirstlane((int)((float)total * p.per_wave)) + 1);
+        run = __builtin_amdgcn_readfirstlane((int)((float)total * p.per_wave)) + 1;
+        // Short runs are cut within items: a wavefront that ends one item and begins another takes as long as two.  The items' last runs may be short then, so there have
+        // to be wavefronts enough for one more of each.
+        if (run <= kPagedShortRun && p.slot_o && 2 * (int64_t)items * heads <= p.n_waves) {
+            run = pad = __builtin_amdgcn_readfirstlane((int)((uint32_t)total / (uint32_t)(p.n_waves - items * heads)) + 1);
+            ahead = p.prefix_tiles * padded(prefix_count(p));
+            upto = wave_scan(tiles * padded(count));
+            width = ahead + __builtin_amdgcn_readlane(upto, 63);
+            for (int c = 64; c < p.batch.n_seqs; c += 64) {
+                int t, n;
+                width += __builtin_amdgcn_readlane(scan(p, c, t, n), 63);
+            }
+            total = (int64_t)width * heads;
+        }
         pos = (int64_t)run * wave;
         end = min(pos + run, total);
         if (pos >= end) return false;
         item.lh = __builtin_amdgcn_readfirstlane(quotient(pos, width));
         int at = (int)(pos - (int64_t)item.lh * width);
         if (at < ahead) {
-            const int count = prefix_count(p);
-            set_prefix(p, __builtin_amdgcn_readfirstlane(at / count));
-            h0 = at - item.tile * count;
+            const int each = padded(prefix_count(p));
+            set_prefix(p, __builtin_amdgcn_readfirstlane(at / each));
+            h0 = at - item.tile * each;
         } else {
             at -= ahead;
             int index = p.prefix_tiles;
             for (int c = 0;; c += 64) {
-                if (c) upto = scan(p, c, tiles);
-                const int sum = __builtin_amdgcn_readlane(upto, 63), before = wave_scan(tiles);
+                if (c) upto = scan(p, c, tiles, count), before = wave_scan(tiles);
+                const int sum = __builtin_amdgcn_readlane(upto, 63);
                 if (at < sum) {
                     const int j = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > at));
                     at -= j ? __builtin_amdgcn_readlane(upto, j - 1) : 0;
-                    item.index = index + (j ? __builtin_amdgcn_readlane(before, j - 1) : 0);
-                    const int of_item = item.index;
+                    const int of_item = index + (j ? __builtin_amdgcn_readlane(before, j - 1) : 0), each = padded(__builtin_amdgcn_readlane(count, j));
                     set_sequence(p, c + j);
-                    item.tile = item.tiles == 1 ? 0 : __builtin_amdgcn_readfirstlane(at / item.count);
+                    item.tile = item.tiles == 1 ? 0 : __builtin_amdgcn_readfirstlane(at / each);
                     item.index = of_item + item.tile;
-                    h0 = at - item.tile * item.count;
+                    h0 = at - item.tile * each;
                     break;
                 }
                 at -= sum;

@@ -8,18 +8,18 @@ using namespace kvc;
 
 // The results of rows whose keys went to several wavefronts or runs: out = sum_s f_s O_s / sum_s f_s l_s, f_s = exp2((m_s - max m) scale log2 e), parts in
 // a fixed order.  A wavefront takes `heads` query heads of a (layer, row); D / 4 lanes hold an output's channels, and the 64 / (D / 4) such groups take the
-// parts in turn.
+// parts in turn.  W = 4: the four wavefronts of a block share one head's parts, where there are few rows (8 sequences, 32 heads, up to 49 parts of a row: see launch_combine()).
 struct CombineParams : PagedAttnParams {
     int32_t heads, chunks;   // query heads of a wavefront, such pieces of a row
     divisor_t by_chunks, by_rows;
 };
-template <typename T, int D>
+template <typename T, int D, int W>
 __global__ __launch_bounds__(256) void attn_paged_combine_kernel(const CombineParams p)
 {
     constexpr int CL = D / 4, NG = 64 / CL, U = 8;
     const int lane = threadIdx.x & 63, Hq = p.Hkv * p.G, n_rows = p.batch.n_rows;
-    const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-    const int lr = div_by(wave, p.by_chunks), chunk = wave - lr * p.chunks, l = div_by(lr, p.by_rows), row = lr - l * n_rows;
+    const int sub = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), unit = W == 4 ? blockIdx.x : blockIdx.x * 4 + sub;
+    const int lr = div_by(unit, p.by_chunks), chunk = unit - lr * p.chunks, l = div_by(lr, p.by_rows), row = lr - l * n_rows;
     if (l >= p.L) return;
     // (One row of up to tile_rows heads per sequence: its item is known.  Else, for rows of no sequence, item_of holds whatever.)
     const bool known = !p.batch.starts && p.G <= p.tile_rows;
@@ -36,6 +36,8 @@ __global__ __launch_bounds__(256) void attn_paged_combine_kernel(const CombinePa
     };
     const int64_t all = (int64_t)p.L * Hq * n_rows;
     const int group = lane / CL, c = 4 * (lane % CL);
+    __shared__ float joined_ml[W][2];
+    __shared__ __align__(16) float joined_o[W][D];
     auto parts_of = [&](int hkv, int index, int packed) -> Parts {
         const int32_t *e = p.items + ((int64_t)(l * p.Hkv + hkv) * p.max_items + max(0, min(index, p.max_items - 1))) * 2;
         const int w0 = e[0], w1 = e[1];
@@ -77,13 +79,13 @@ __global__ __launch_bounds__(256) void attn_paged_combine_kernel(const CombinePa
         // Parts k0 ... of this group, whose loads are all in flight at once, against the largest reference so far.
         float M = -INFINITY, sum = 0.f;
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int k0 = group; k0 < count; k0 += NG * U) {
+        for (int k0 = W == 4 ? sub * NG + group : group; k0 < count; k0 += W * NG * U) {
             f32x4 os[U];
             float ms[U], ls[U], top = M;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const float *o, *ml;
-                place(min(k0 + u * NG, count - 1), o, ml);
+                place(min(k0 + u * W * NG, count - 1), o, ml);
                 ms[u] = ml[0];
                 ls[u] = ml[1];
                 os[u] = *reinterpret_cast<const f32x4 *>(o + c);
@@ -96,7 +98,7 @@ __global__ __launch_bounds__(256) void attn_paged_combine_kernel(const CombinePa
             M = top;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                if (k0 + u * NG >= count) continue;
+                if (k0 + u * W * NG >= count) continue;
                 if (ms[u] != -INFINITY) {
                     const float f = __builtin_amdgcn_exp2f((ms[u] - M) * p.scale_log2);
                     sum = fmaf(f, ls[u], sum);
@@ -115,6 +117,18 @@ __global__ __launch_bounds__(256) void attn_paged_combine_kernel(const CombinePa
             for (int i = 0; i < 4; ++i) {
                 const float a2 = __shfl_xor(acc[i], off);
                 acc[i] = acc[i] * f + a2 * f2;
+            }
+        }
+        if constexpr (W > 1) {   // the wavefronts (heads is 1 then, and the block goes through here together)
+            if (lane == 0) joined_ml[sub][0] = M, joined_ml[sub][1] = sum;
+            if (group == 0) *reinterpret_cast<f32x4 *>(&joined_o[sub][c]) = acc;
+            __syncthreads();
+            if (sub) return;
+#pragma unroll
+            for (int w = 1; w < W; ++w) {
+                float f, f2;
+                join_part(M, sum, joined_ml[w][0], joined_ml[w][1], p.scale_log2, f, f2);
+                acc = acc * f + *reinterpret_cast<const f32x4 *>(&joined_o[w][c]) * f2;
             }
         }
         const bool none = M == -INFINITY && sum == 0.f;
@@ -137,15 +151,18 @@ int launch_combine(const PagedAttnParams &a, hipStream_t s)
     static_cast<PagedAttnParams &>(p) = a;
     const int Hq = a.Hkv * a.G;
     const int64_t rows = (int64_t)a.L * a.batch.n_rows;
-    p.heads = (int)std::min<int64_t>(std::min(Hq, 64), std::max<int64_t>(1, rows * Hq / 4096));   // a wavefront's: as many as leave a few per SIMD
+    // Few rows: a block per head.  us, 8 sequences of 600 to 3100 tokens, one layer COMB_FEW; many: as many heads of a wavefront as leave 16384 of them (64 sequences behind a prefix,
+    // 32 layers: COMB_MANY).
+    const bool few = rows * Hq <= 4096;
+    p.heads = few ? 1 : (int)std::min<int64_t>(std::min(Hq, 64), std::max<int64_t>(1, rows * Hq / 16384));
     p.chunks = (Hq + p.heads - 1) / p.heads;
     p.by_chunks = make_divisor((uint32_t)p.chunks);
     p.by_rows = make_divisor((uint32_t)a.batch.n_rows);
-    const dim3 grid((unsigned)((rows * p.chunks + 3) / 4)), block(256);
+    const dim3 grid((unsigned)(few ? rows * p.chunks : (rows * p.chunks + 3) / 4)), block(256);
     switch (a.D) {
-        case 64: return launch(attn_paged_combine_kernel<T, 64>, grid, block, 0, s, p);
-        case 128: return launch(attn_paged_combine_kernel<T, 128>, grid, block, 0, s, p);
-        default: return launch(attn_paged_combine_kernel<T, 256>, grid, block, 0, s, p);
+        case 64: return launch(few ? attn_paged_combine_kernel<T, 64, 4> : attn_paged_combine_kernel<T, 64, 1>, grid, block, 0, s, p);
+        case 128: return launch(few ? attn_paged_combine_kernel<T, 128, 4> : attn_paged_combine_kernel<T, 128, 1>, grid, block, 0, s, p);
+        default: return launch(few ? attn_paged_combine_kernel<T, 256, 4> : attn_paged_combine_kernel<T, 256, 1>, grid, block, 0, s, p);
     }
 }
 

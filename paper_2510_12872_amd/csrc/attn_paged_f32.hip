@@ -121,7 +121,7 @@ __global__ __launch_bounds__(64, D == 256 ? 1 : 2) void attn_paged_f32_kernel(co
     while (true) {
         const bool ends = part == 1 && h + 1 == cur.count;   // the item
         pos += part;
-        bool more = part == 0 || pos < end || (!p.slot_o && !ends);
+        bool more = part == 0 || (pos < end && !(ends && walk.pad > 1)) || (!p.slot_o && !ends);
         int nh = h + part;
         const int npart = part ^ 1;
         no_page |= !x.page;
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(64, D == 256 ? 1 : 2) void attn_paged_f32_kernel(co
             float zero = lsum * 0.f;
 #pragma unroll
             for (int i = 0; i < 16 * NT; ++i) zero = fmaf(o[i / 16][i / 4 % 4][i % 4], 0.f, zero);
-            if (__builtin_amdgcn_ballot_w64(no_page || state_is_odd(zero, m, lsum)) != 0) {
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(no_page || state_is_odd(zero, m, lsum)) != 0, 0)) {
                 paged_exact_segment<float, D, TR>(p, cur, to, seg0, h, lane);
             } else {
                 const PagedRow row = paged_row(p, cur, to, TR, n);

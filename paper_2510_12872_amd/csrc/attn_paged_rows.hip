@@ -87,7 +87,7 @@ __global__ __launch_bounds__(64, RH == 2 || D >= 128 ? 2 : 4) void attn_paged_ro
     auto load = [&](const Half &x, const unsigned char *base, int64_t page_bytes, uint32_t row_bytes, auto &chunk, auto swz, lds_byte *dst) __attribute__((always_inline)) {
         constexpr int NC = sizeof(chunk) / sizeof(chunk[0]);
         const int mask = x.prefix ? INT32_MAX : (1 << p.batch.log_page) - 1;
-        if (x.at + 32 <= x.limit) {
+        if (__builtin_expect(x.at + 32 <= x.limit, 1)) {
             const uint32_t in = (uint32_t)lq * row_bytes;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(64, RH == 2 || D >= 128 ? 2 : 4) void attn_paged_ro
     while (true) {
         const bool ends = h + 1 == cur.count;   // the item
         ++pos;
-        bool more = pos < end || (!p.slot_o && !ends);
+        bool more = (pos < end && !(ends && walk.pad > 1)) || (!p.slot_o && !ends);
         int nh = h + 1;
         if (!x.prefix) no_page |= x.limit > 0 && !(is_page(x.page[0]) && is_page(x.page[1]));
         if (more && ends) {
@@ -261,7 +261,7 @@ __global__ __launch_bounds__(64, RH == 2 || D >= 128 ? 2 : 4) void attn_paged_ro
                 for (int i = 0; i < 4 * NF; ++i) zero = fmaf(o[r][i / 4][i % 4], 0.f, zero);
                 odd |= state_is_odd(zero, m[r], lsum[r]);
             }
-            if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, 0)) {
                 paged_exact_segment<bf16_t, D, TR>(p, cur, to, seg0, h, lane);
             } else {
 #pragma unroll
