@@ -69,16 +69,24 @@ __device__ __forceinline__ void all_rows(const P &p, int &first, int &n)
 // A sequence's tokens from row i of n on: the last one that it sees, -1 or less: none.
 __device__ __forceinline__ int last_seen(int len, int n, int i, int cap) { return min(len - n + i, min(len, cap) - 1); }
 
+// The same parameters, loaded again where they are used from here on: nothing of them is kept in (or spilled from) scalar registers across this.
+template <class P>
+__device__ __forceinline__ P &again(P &p)
+{
+    P *q = &p;
+    asm volatile("" : "+s"(q));
+    return *q;
+}
+
 // One row (sequence b, row `row` of the queries, query head hq) over the halves [h0, h1) by the formula, key by key, in fp32; what the row does not
 // see (`last`: the last token of its pages that it sees) is not looked at.  Whole rows: halves 0 ... of the prefix, then of the pages.
 // Returns reference and sum; lanes 0 ... D / 8 - 1 hold channels 8 * lane ... of the unnormalised output.
 template <typename T, int D, class P>
-__device__ __forceinline__ void paged_exact_row(const P &p, int l, int hkv, int hq, int row, int b, int last, int prefix_halves, int h0, int h1, int lane,
+__device__ __forceinline__ void paged_exact_row(const P &p0, int l, int hkv, int hq, int row, int b, int last, int prefix_halves, int h0, int h1, int lane,
                                                 float &m, float &sum, float (&o)[8])
 {
     constexpr int CL = D / 8, EPV = Elem<T>::EPV;
-    const T *q = static_cast<const T *>(p.q) + l * p.s_q.layer + (int64_t)hq * p.s_q.head + (int64_t)row * p.s_q.token;
-    auto at = [&](int x, bool values) -> const T * {   // row of key x, counted from half 0; null: not there
+    auto at = [&](const P &p, int x, bool values) __attribute__((always_inline)) -> const T * {   // row of key x, counted from half 0; null: not there
         if (x < 32 * prefix_halves) {
             if (x >= p.n_prefix) return nullptr;
             const int64_t layer = values ? p.s_pv.layer : p.s_pk.layer, head = values ? p.s_pv.head : p.s_pk.head, token = values ? p.s_pv.token : p.s_pk.token;
@@ -108,7 +116,9 @@ __device__ __forceinline__ void paged_exact_row(const P &p, int l, int hkv, int 
     const int end = (int)min((int64_t)32 * h1, (int64_t)32 * prefix_halves + last + 1);
 #pragma unroll 1
     for (int x0 = 32 * h0; x0 < end && sum == sum; x0 += 64) {   // a key per lane; a sum that is not a number stays so, and the row with it
-        const T *kr = x0 + lane < end ? at(x0 + lane, false) : nullptr;
+        const P &p = again(p0);
+        const T *q = static_cast<const T *>(p.q) + l * p.s_q.layer + (int64_t)hq * p.s_q.head + (int64_t)row * p.s_q.token;
+        const T *kr = x0 + lane < end ? at(p, x0 + lane, false) : nullptr;
         const bool seen = kr != nullptr;
         float s = -INFINITY;
         if (seen) {
@@ -140,7 +150,7 @@ __device__ __forceinline__ void paged_exact_row(const P &p, int l, int hkv, int 
             const float pj = __shfl(e, j);
             if (lane < CL) {
                 float vv[8];
-                load8(at(x0 + j, true) + 8 * lane, vv);
+                load8(at(again(p0), x0 + j, true) + 8 * lane, vv);
 #pragma unroll
                 for (int c = 0; c < 8; ++c) o[c] = fmaf(pj, vv[c], o[c]);
             }
@@ -204,7 +214,9 @@ __device__ __forceinline__ int quotient(int64_t x, int64_t d)
     return (int)q;
 }
 
-// The sizes are such that what one (layer, kv head) has on the axis fits 31 bits, and a run, too (plan_of()).
+// The sizes are such that what one (layer, kv head) has on the axis fits 31 bits, and a run, too (paged_attn()).
+// What bounds its start is the way to memory: arguments, then rows and lengths of 64 sequences at a time, a lane each, all requested together; from then on
+// they are read from the lanes.  (Loaded where they were used, scalars among them, a wavefront took 8 to 15 us to its first item.)
 template <int TR>   // packed rows of a tile
 struct PagedWalk {
     const int lane;
@@ -215,84 +227,63 @@ struct PagedWalk {
 
     __device__ __forceinline__ explicit PagedWalk(int lane) : lane(lane) {}
 
-    __device__ __forceinline__ static int tiles_of(PagedArgs &p, int n)
-    {
-        const int rows = n * p.G;
-        return rows <= p.most_rows ? (rows + TR - 1) / TR : 0;
-    }
-    __device__ __forceinline__ static int count_of(PagedArgs &p, int len) { return max(1, p.walked_prefix + (min(len, p.batch.cap) + 31) / 32); }
-    __device__ __forceinline__ static int prefix_count(PagedArgs &p) { return (p.n_prefix + 31) / 32; }
-
-    __device__ __forceinline__ int padded(int count) const { return pad == 1 ? count : (int)((uint32_t)(count + pad - 1) / (uint32_t)pad) * pad; }
-
-    // Halves of the sequences c ... c + 63 up to each lane's, that lane's row tiles, and its halves of one.
-    __device__ __forceinline__ int scan(PagedArgs &p, int c, int &tiles, int &count) const
-    {
-        const int b = c + lane;
-        tiles = 0;
-        count = 1;
-        if (b < p.batch.n_seqs) {
-            int first, n;
-            sequence_rows(p.batch, b, first, n);
-            tiles = tiles_of(p, n);
-            count = count_of(p, sequence_len(p.batch, b));
-        }
-        return wave_scan(tiles * padded(count));
-    }
-
-    // The first item that wavefront `wave` works on, and its halves of it; false: none.
+    // The item at `pos` of the axis (negative: where the run of wavefront `wave` begins) and its half there; false: the run ends before.
     __device__ __forceinline__ bool begin(int wave, int64_t &pos, int64_t &end, int &h0)
     {
-        PagedArgs &p = paged_args();
-        const int heads = p.L * p.Hkv;
-        int tiles, count, items = p.prefix_tiles, ahead = p.prefix_tiles * prefix_count(p);
-        int upto = scan(p, 0, tiles, count);   // (kept: most batches have no more)
-        int before = wave_scan(tiles);
+        const Args a;
+        pad = 1;
+        load(a, 0);
+        const int before0 = a.prefix_tiles * a.prefix_count();
+        int upto = wave_scan(tiles(a) * count(a, len)), before = wave_scan(tiles(a));   // (kept: most batches have no more)
+        int ahead = before0, items = a.prefix_tiles + __builtin_amdgcn_readlane(before, 63);
         width = ahead + __builtin_amdgcn_readlane(upto, 63);
-        items += __builtin_amdgcn_readlane(before, 63);
-        for (int c = 64; c < p.batch.n_seqs; c += 64) {
-            int t, n;
-            width += __builtin_amdgcn_readlane(scan(p, c, t, n), 63);
-            items += __builtin_amdgcn_readlane(wave_scan(t), 63);
+        for (int c = 64; c < a.n_seqs; c += 64) {
+            load(a, c);
+            width += __builtin_amdgcn_readlane(wave_scan(tiles(a) * count(a, len)), 63);
+            items += __builtin_amdgcn_readlane(wave_scan(tiles(a)), 63);
         }
-        int64_t total = (int64_t)width * heads;
+        int64_t total = (int64_t)width * a.heads;
         // (a little more than its share each, so that rounding leaves nothing)
-        run = __builtin_amdgcn_readfirstlane((int)((float)total * p.per_wave)) + 1;
+        run = __builtin_amdgcn_readfirstlane((int)((float)total * a.per_wave)) + 1;
         // Short runs are cut within items: a wavefront that ends one item and begins another takes as long as two.  The items' last runs may be short then, so there have
         // to be wavefronts enough for one more of each.
-        if (run <= kPagedShortRun && p.slot_o && 2 * (int64_t)items * heads <= p.n_waves) {
-            run = pad = __builtin_amdgcn_readfirstlane((int)((uint32_t)total / (uint32_t)(p.n_waves - items * heads)) + 1);
-            ahead = p.prefix_tiles * padded(prefix_count(p));
-            upto = wave_scan(tiles * padded(count));
-            width = ahead + __builtin_amdgcn_readlane(upto, 63);
-            for (int c = 64; c < p.batch.n_seqs; c += 64) {
-                int t, n;
-                width += __builtin_amdgcn_readlane(scan(p, c, t, n), 63);
+        if (run <= kPagedShortRun && a.slots && 2 * (int64_t)items * a.heads <= a.n_waves) {
+            run = pad = __builtin_amdgcn_readfirstlane((int)((uint32_t)total / (uint32_t)(a.n_waves - items * a.heads)) + 1);
+            ahead = a.prefix_tiles * padded(a.prefix_count());
+            width = ahead;
+            for (int c = 0; c < a.n_seqs; c += 64) {
+                if (chunk != c) load(a, c);
+                const int x = wave_scan(tiles(a) * padded(count(a, len)));
+                if (c == 0) upto = x;
+                width += __builtin_amdgcn_readlane(x, 63);
             }
-            total = (int64_t)width * heads;
+            total = (int64_t)width * a.heads;
         }
-        pos = (int64_t)run * wave;
-        end = min(pos + run, total);
+        end = min((int64_t)run * wave + run, total);
+        if (pos < 0) pos = (int64_t)run * wave;
         if (pos >= end) return false;
         item.lh = __builtin_amdgcn_readfirstlane(quotient(pos, width));
         int at = (int)(pos - (int64_t)item.lh * width);
         if (at < ahead) {
-            const int each = padded(prefix_count(p));
-            set_prefix(p, __builtin_amdgcn_readfirstlane(at / each));
+            const int each = padded(a.prefix_count());
+            set_prefix(a, __builtin_amdgcn_readfirstlane(at / each));
             h0 = at - item.tile * each;
         } else {
             at -= ahead;
-            int index = p.prefix_tiles;
+            int index = a.prefix_tiles;
             for (int c = 0;; c += 64) {
-                if (c) upto = scan(p, c, tiles, count), before = wave_scan(tiles);
+                if (chunk != c) load(a, c);
+                if (c) upto = wave_scan(tiles(a) * padded(count(a, len))), before = wave_scan(tiles(a));
                 const int sum = __builtin_amdgcn_readlane(upto, 63);
                 if (at < sum) {
                     const int j = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > at));
                     at -= j ? __builtin_amdgcn_readlane(upto, j - 1) : 0;
-                    const int of_item = index + (j ? __builtin_amdgcn_readlane(before, j - 1) : 0), each = padded(__builtin_amdgcn_readlane(count, j));
-                    set_sequence(p, c + j);
+                    index += j ? __builtin_amdgcn_readlane(before, j - 1) : 0;
+                    todo = __builtin_amdgcn_ballot_w64(tiles(a) > 0 && lane > j);
+                    set_sequence(a, j);
+                    const int each = padded(item.count);
                     item.tile = item.tiles == 1 ? 0 : __builtin_amdgcn_readfirstlane(at / each);
-                    item.index = of_item + item.tile;
+                    item.index = index + item.tile;
                     h0 = at - item.tile * each;
                     break;
                 }
@@ -300,7 +291,7 @@ struct PagedWalk {
                 index += __builtin_amdgcn_readlane(before, 63);
             }
         }
-        if (!p.slot_o && h0 > 0) {   // the item is another one's: on to the next
+        if (!a.slots && h0 > 0) {   // the item is another one's: on to the next
             pos += item.count - h0;
             h0 = 0;
             if (pos >= end) return false;
@@ -311,70 +302,114 @@ struct PagedWalk {
     // The item behind it; false: there is none.
     __device__ __forceinline__ bool next()
     {
-        PagedArgs &p = paged_args();
         ++item.index;
         if (item.tile + 1 < item.tiles) {
             ++item.tile;
             return true;
         }
-        int b = item.b;   // (the prefix: -1)
-        while (true) {
-            if (++b == p.batch.n_seqs) {
-                if (++item.lh >= p.L * p.Hkv) return false;
+        const Args a;
+        if (item.b < 0) enter(a, 0);   // (from the prefix)
+        while (todo == 0) {
+            int c = chunk + 64;
+            if (c >= a.n_seqs) {
+                if (++item.lh >= a.heads) return false;
                 item.index = 0;
-                b = -1;
-                if (p.prefix_tiles) {
-                    set_prefix(p, 0);
+                if (a.prefix_tiles) {
+                    set_prefix(a, 0);
                     return true;
                 }
-                continue;
+                c = 0;
             }
-            int first, n;
-            rows_of(p, b, first, n);
-            if (tiles_of(p, n) > 0) break;
+            enter(a, c);
         }
-        set_sequence(p, b);
+        const int j = __builtin_ctzll(todo);
+        todo &= todo - 1;
+        set_sequence(a, j);
         return true;
     }
 
 private:
-    __device__ __forceinline__ static void rows_of(PagedArgs &p, int b, int &first, int &n)
-    {
-        if (!p.batch.starts) {
-            first = b;
-            n = 1;
-            return;
+    int chunk = -1;           // the sequences chunk ... chunk + 63 in the lanes: their rows and lengths
+    int first = 0, n = 0, len = 0;
+    uint64_t todo = 0;        // those behind the item's that have items here
+
+    struct Args {   // of the launch, requested together
+        const int32_t *starts, *lens;
+        int n_seqs, n_rows, cap, G, most_rows, walked, prefix_tiles, n_prefix, heads, n_waves;
+        float per_wave;
+        bool slots;
+        __device__ __forceinline__ Args()
+        {
+            PagedArgs &p = paged_args();
+            starts = p.batch.starts, lens = p.batch.lens;
+            n_seqs = p.batch.n_seqs, n_rows = p.batch.n_rows, cap = p.batch.cap, G = p.G, most_rows = p.most_rows, walked = p.walked_prefix;
+            prefix_tiles = p.prefix_tiles, n_prefix = p.n_prefix, heads = p.L * p.Hkv, n_waves = p.n_waves, per_wave = p.per_wave;
+            slots = p.slot_o != nullptr;
+            asm volatile("" : : "s"(starts), "s"(lens), "s"(n_seqs), "s"(n_rows), "s"(cap), "s"(G), "s"(most_rows), "s"(walked), "s"(prefix_tiles), "s"(n_prefix), "s"(heads),
+                         "s"(n_waves), "s"(per_wave));
         }
-        first = max(0, min(scalar(p.batch.starts)[b], p.batch.n_rows));
-        n = max(0, min(scalar(p.batch.starts)[b + 1], p.batch.n_rows) - first);
+        __device__ __forceinline__ int prefix_count() const { return (n_prefix + 31) / 32; }
+    };
+
+    __device__ __forceinline__ void load(const Args &a, int c)
+    {
+        chunk = c;
+        const int b = min(c + lane, a.n_seqs - 1);
+        const int l = a.lens[b];
+        first = b;
+        n = 1;
+        if (a.starts) {
+            const int s0 = a.starts[b], s1 = a.starts[b + 1];
+            first = max(0, min(s0, a.n_rows));
+            n = max(0, min(s1, a.n_rows) - first);
+        }
+        n = c + lane < a.n_seqs ? n : 0;
+        len = max(0, l);
     }
-    __device__ __forceinline__ void set_prefix(PagedArgs &p, int tile)
+    __device__ __forceinline__ void enter(const Args &a, int c)
+    {
+        if (chunk != c) load(a, c);
+        todo = __builtin_amdgcn_ballot_w64(tiles(a) > 0);
+    }
+    __device__ __forceinline__ int tiles(const Args &a) const   // of the lane's sequence
+    {
+        const int rows = n * a.G;
+        return rows <= a.most_rows ? (rows + TR - 1) / TR : 0;
+    }
+    __device__ __forceinline__ static int count(const Args &a, int len) { return max(1, a.walked + (min(len, a.cap) + 31) / 32); }
+    __device__ __forceinline__ int padded(int count) const { return pad == 1 ? count : (int)((uint32_t)(count + pad - 1) / (uint32_t)pad) * pad; }
+    __device__ __forceinline__ void set_prefix(const Args &a, int tile)
     {
         item.b = -1;
         item.tile = tile;
-        item.tiles = p.prefix_tiles;
+        item.tiles = a.prefix_tiles;
         item.index = tile;
-        item.count = item.walk = prefix_count(p);
+        item.count = item.walk = a.prefix_count();
         item.len = 0;
-        all_rows(p, item.first, item.n);
+        item.first = 0;
+        item.n = a.n_rows;
+        if (a.starts) {
+            const_int *s = scalar(a.starts);
+            item.first = max(0, min(s[0], a.n_rows));
+            item.n = max(0, min(s[a.n_seqs], a.n_rows) - item.first);
+        }
     }
-    __device__ __forceinline__ void set_sequence(PagedArgs &p, int b)
+    __device__ __forceinline__ void set_sequence(const Args &a, int j)   // of lane j
     {
-        item.b = b;
-        rows_of(p, b, item.first, item.n);
+        item.b = chunk + j;
+        item.first = __builtin_amdgcn_readlane(first, j);
+        item.n = __builtin_amdgcn_readlane(n, j);
+        item.len = __builtin_amdgcn_readlane(len, j);
         item.tile = 0;
-        item.tiles = tiles_of(p, item.n);
-        item.len = max(0, scalar(p.batch.lens)[b]);
-        item.walk = p.walked_prefix;
-        item.count = count_of(p, item.len);
+        item.tiles = (item.n * a.G + TR - 1) / TR;
+        item.walk = a.walked;
+        item.count = count(a, item.len);
     }
 };
 
+constexpr int kPagedBlockWaves = 4;   // of a wavefront kernel's block, which share nothing
 // Wavefronts of attn_paged_rows_kernel that a compute unit holds: by LDS, and by registers.
-#ifndef KW128
-#define KW128 8
-#endif
-constexpr int paged_rows_waves(int D, int rows) { return D == 256 ? 5 : rows == 32 ? 8 : D == 128 ? KW128 : 16; }
+constexpr int paged_rows_waves(int D, int rows) { return D == 256 ? 4 : D == 128 || rows == 32 ? 8 : 16; }
 
 constexpr int paged_f32_waves(int D) { return D == 256 ? 4 : 8; }
 
@@ -387,13 +422,12 @@ struct PagedPlace {
     float *o, *ml;   // of the slot's rows, or of rows by (layer, query head, row)
 };
 template <int TR, class P>
-__device__ __forceinline__ PagedPlace paged_place(const P &p, const PagedItem &it, int seg0, int h, int64_t pos, int run, int lane)
+__device__ __forceinline__ PagedPlace paged_place(const P &p, const PagedItem &it, int seg0, int h, int64_t pos, int run, int64_t wave, int lane)
 {
     const bool ends = h + 1 == it.count, whole = ends && seg0 == 0;
     // (a prefix with items of its own on this axis: every row is joined; with parts by rows: they are there already)
     PagedPlace to = {whole ? p.prefix_tiles ? kWhole : kDirect : 0, nullptr, nullptr};
     if (!p.slot_o) return to;
-    const int64_t wave = blockIdx.x;
     if (to.kind == kWhole) {
         const int64_t all = (int64_t)p.L * p.Hkv * p.G * p.batch.n_rows * (it.b < 0 ? p.prefix_part : 0);
         to.o = p.row_o + all * p.D;
@@ -489,10 +523,11 @@ __device__ __forceinline__ void paged_finish_row(const P &p, const PagedPlace &t
 
 // The segment by the formula.
 template <typename T, int D, int TR, class P>
-__device__ __forceinline__ void paged_exact_segment(const P &p, const PagedItem &it, const PagedPlace &to, int seg0, int h, int lane)
+__device__ __forceinline__ void paged_exact_segment(const P &p0, const PagedItem &it, const PagedPlace &to, int seg0, int h, int lane)
 {
 #pragma unroll 1
     for (int r = 0; r < TR; ++r) {
+        const P &p = again(p0);
         const PagedRow row = paged_row(p, it, to, TR, r);
         if (!row.valid) return;
         float m, sum, o[8];

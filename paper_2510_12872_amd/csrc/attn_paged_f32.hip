@@ -11,16 +11,16 @@ using namespace kvc;
 // when this one's operands have been multiplied.  What bounds it: matrix cores where there is much of it (fp32 MFMA, 1/16 of the bf16 rate), else the chain of
 // one wavefront.
 template <int D>
-__global__ __launch_bounds__(64, D == 256 ? 1 : 2) void attn_paged_f32_kernel(const PagedAttnParams)
+__global__ __launch_bounds__(64 * kPagedBlockWaves, D == 256 ? 1 : 2) void attn_paged_f32_kernel(const PagedAttnParams)
 {
     PagedArgs &p = paged_args();
     await_paged_args(p);
     constexpr int TR = 16, NJ = D / 16, NT = D / 64;   // 16-byte pieces of a K row in a lane, loads of a V row
-    const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)blockIdx.x * kPagedBlockWaves + (int)(threadIdx.x >> 6));
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     PagedWalk<TR> walk(lane);
-    int64_t pos, end;
+    int64_t pos = -1, end;
     int h;
-    if (!walk.begin(blockIdx.x, pos, end, h)) return;
 
     // ---- the keys: a sub-step is 16 of them, two to a half
     const float *kp, *vp, *kf, *vf;
@@ -39,11 +39,11 @@ __global__ __launch_bounds__(64, D == 256 ? 1 : 2) void attn_paged_f32_kernel(co
     };
     struct Sub {
         int at, limit;   // first key, and how many there are (0: nothing is read)
-        bool prefix, page;
+        int prefix, page;   // truth values (as bool they left bytes between, which were copied through memory)
         int64_t k, v;    // elements from the (layer, head)'s begin to the first key's row
     };
     auto sub_at = [&](int h_, int part) __attribute__((always_inline)) -> Sub {
-        Sub x = {32 * h_ + 16 * part, p.n_prefix, h_ < walk.item.walk, true, 0, 0};
+        Sub x = {32 * h_ + 16 * part, p.n_prefix, h_ < walk.item.walk, 1, 0, 0};
         if (x.prefix) {
             const int64_t t = min(x.at, p.n_prefix - 1);   // (the second half of the last one may lie behind it)
             x.k = t * p.s_pk.token;
@@ -105,6 +105,7 @@ __global__ __launch_bounds__(64, D == 256 ? 1 : 2) void attn_paged_f32_kernel(co
         lsum = 0.f;
     };
 
+    while (walk.begin(wave, pos, end, h)) {   // (again where a segment has been computed by the formula: nothing is kept for the walk across that)
     enter();
 #pragma unroll
     for (int j = 0; j < NJ; ++j) k[j] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -171,26 +172,28 @@ __global__ __launch_bounds__(64, D == 256 ? 1 : 2) void attn_paged_f32_kernel(co
         if (ends || !more) {
             // ---- the segment [seg0, h] of the item is done.  Lane (n, g) holds channels 64 * t + 16 * g + 4 * r + c of row n.
             PagedArgs &p = paged_args();
-            const PagedPlace to = paged_place<TR>(p, cur, seg0, h, pos, walk.run, lane);
+            const PagedPlace to = paged_place<TR>(p, cur, seg0, h, pos, walk.run, wave, lane);
             lsum = query_sum(lsum);
             float zero = lsum * 0.f;
 #pragma unroll
             for (int i = 0; i < 16 * NT; ++i) zero = fmaf(o[i / 16][i / 4 % 4][i % 4], 0.f, zero);
             if (__builtin_expect(__builtin_amdgcn_ballot_w64(no_page || state_is_odd(zero, m, lsum)) != 0, 0)) {
                 paged_exact_segment<float, D, TR>(p, cur, to, seg0, h, lane);
-            } else {
-                const PagedRow row = paged_row(p, cur, to, TR, n);
-                f32x4 pieces[D / 16];
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) pieces[i] = f32x4{o[i / 4][0][i % 4], o[i / 4][1][i % 4], o[i / 4][2][i % 4], o[i / 4][3][i % 4]};
-                if (row.valid) paged_finish_row<float, D>(p, to, row, g, m, lsum, pieces, [&](int i) { return 64 * (i / 4) + 16 * g + 4 * (i % 4); });
+                if (!more) return;
+                break;
             }
+            const PagedRow row = paged_row(p, cur, to, TR, n);
+            f32x4 pieces[D / 16];
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) pieces[i] = f32x4{o[i / 4][0][i % 4], o[i / 4][1][i % 4], o[i / 4][2][i % 4], o[i / 4][3][i % 4]};
+            if (row.valid) paged_finish_row<float, D>(p, to, row, g, m, lsum, pieces, [&](int i) { return 64 * (i / 4) + 16 * g + 4 * (i % 4); });
             if (!more) return;
             rows(nh);
         }
         x = nx;
         h = nh;
         part = npart;
+    }
     }
 }
 
@@ -200,7 +203,7 @@ namespace kvc {
 
 int launch_paged_f32(const PagedAttnParams &p, hipStream_t s)
 {
-    const dim3 grid((unsigned)p.n_waves), block(64);
+    const dim3 grid((unsigned)(p.n_waves / kPagedBlockWaves)), block(64 * kPagedBlockWaves);
     switch (p.D) {
         case 64: return launch(attn_paged_f32_kernel<64>, grid, block, 0, s, p);
         case 128: return launch(attn_paged_f32_kernel<128>, grid, block, 0, s, p);

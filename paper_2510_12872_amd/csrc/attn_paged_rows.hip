@@ -18,7 +18,7 @@ __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)"
 // their number per compute unit is what fits LDS.
 // What bounds it is HBM.  A half lies in one page or in two, whose entries are read, through the scalar cache, a half ahead.
 template <int D, int RH>
-__global__ __launch_bounds__(64, RH == 2 || D >= 128 ? 2 : 4) void attn_paged_rows_kernel(const PagedAttnParams)
+__global__ __launch_bounds__(64 * kPagedBlockWaves, RH == 2 || D >= 128 ? 2 : 4) void attn_paged_rows_kernel(const PagedAttnParams)
 {
     PagedArgs &p = paged_args();
     await_paged_args(p);
@@ -26,23 +26,20 @@ __global__ __launch_bounds__(64, RH == 2 || D >= 128 ? 2 : 4) void attn_paged_ro
     constexpr int NF = D / 16, KCH = D / 8, ROWB = D * 2, HALFB = 32 * ROWB;
     constexpr int RPL = 64 / KCH, LPT = 32 / RPL;              // key rows filled by one wavefront-wide direct load, loads of a half
     constexpr int KD = 16 / RPL, VD = RPL < 8 ? 8 / RPL : 1;   // loads after which the swizzle pattern of the rows repeats
-#ifdef KNT
-    constexpr bool NT = false;
-#else
-    constexpr bool NT = true;
-#endif
+    constexpr bool NT = true;   // non-temporal: nobody reads a half again in this launch
     auto k_swz = [](int key) __attribute__((always_inline)) -> int { return D == 64 ? (key >> 1) & 7 : key & 15; };
     auto v_swz = [](int key) __attribute__((always_inline)) -> int {
         return D == 64 ? (2 * (key & 2)) | ((key >> 1) & 2) : 4 * (key & 3) | ((key >> 1) & 2);
     };
-    __shared__ __align__(16) unsigned char smem[2 * HALFB];
-    const int lane = threadIdx.x, n = lane & 15, g = lane >> 4, lq = lane / KCH;
-    lds_byte *kbuf = (lds_byte *)smem, *vbuf = kbuf + HALFB;
+    constexpr int NW = kPagedBlockWaves;   // of a block, which share nothing but their arguments' way to the caches
+    __shared__ __align__(16) unsigned char smem[NW * 2 * HALFB];
+    const int wave = __builtin_amdgcn_readfirstlane((int)blockIdx.x * NW + (int)(threadIdx.x >> 6));
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, lq = lane / KCH;
+    lds_byte *kbuf = (lds_byte *)smem + (wave % NW) * 2 * HALFB, *vbuf = kbuf + HALFB;
 
     PagedWalk<TR> walk(lane);
-    int64_t pos, end;
+    int64_t pos = -1, end;
     int h;
-    if (!walk.begin(blockIdx.x, pos, end, h)) return;
 
     // ---- where the halves of an item lie
     const unsigned char *kp, *vp, *kf, *vf;   // (layer, head) of the pools and of the prefix
@@ -61,7 +58,7 @@ __global__ __launch_bounds__(64, RH == 2 || D >= 128 ? 2 : 4) void attn_paged_ro
     };
     struct Half {       // of an item, to be loaded
         int at, limit;  // first key of the prefix or token of the pages, and how many there are: 0: an item without tokens, nothing is read
-        bool prefix;
+        int prefix;     // truth value (as bool it left bytes between, which were copied through memory)
         int page[2];    // of the tokens at ... and at + 16 ...
     };
     auto half_at = [&](int h_) __attribute__((always_inline)) -> Half {
@@ -141,12 +138,6 @@ __global__ __launch_bounds__(64, RH == 2 || D >= 128 ? 2 : 4) void attn_paged_ro
         __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0), seen by the compiler: it puts no wait for the queries into the loop
     };
 
-    enter();
-    Half x = half_at(h);
-    load_k(x);
-    load_v(x);
-    rows(h);
-
     // Operand addresses: K chunk 4 * ks + g of key n (and 16 + n); V^T is transposed on the way out of LDS.
     int k_off[NF / 2], v_off[NF];
 #pragma unroll
@@ -160,6 +151,12 @@ __global__ __launch_bounds__(64, RH == 2 || D >= 128 ? 2 : 4) void attn_paged_ro
         }
     }
 
+    while (walk.begin(wave, pos, end, h)) {   // (again where a segment has been computed by the formula: nothing is kept for the walk across that)
+    enter();
+    Half x = half_at(h);
+    load_k(x);
+    load_v(x);
+    rows(h);
     while (true) {
         const bool ends = h + 1 == cur.count;   // the item
         ++pos;
@@ -251,7 +248,7 @@ __global__ __launch_bounds__(64, RH == 2 || D >= 128 ? 2 : 4) void attn_paged_ro
         if (ends || !more) {
             // ---- the segment [seg0, h] of the item is done
             PagedArgs &p = paged_args();
-            const PagedPlace to = paged_place<TR>(p, cur, seg0, h, pos, walk.run, lane);
+            const PagedPlace to = paged_place<TR>(p, cur, seg0, h, pos, walk.run, wave, lane);
             bool odd = no_page;
 #pragma unroll
             for (int r = 0; r < RH; ++r) {
@@ -263,18 +260,21 @@ __global__ __launch_bounds__(64, RH == 2 || D >= 128 ? 2 : 4) void attn_paged_ro
             }
             if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, 0)) {
                 paged_exact_segment<bf16_t, D, TR>(p, cur, to, seg0, h, lane);
-            } else {
+                if (!more) return;
+                wait_loads<0>();   // (the next half's, which is requested again)
+                break;
+            }
 #pragma unroll
-                for (int r = 0; r < RH; ++r) {
-                    const PagedRow row = paged_row(p, cur, to, TR, 16 * r + n);
-                    if (row.valid) paged_finish_row<bf16_t, D>(p, to, row, g, m[r], lsum[r], o[r], [&](int i) { return 16 * i + 4 * g; });
-                }
+            for (int r = 0; r < RH; ++r) {
+                const PagedRow row = paged_row(p, cur, to, TR, 16 * r + n);
+                if (row.valid) paged_finish_row<bf16_t, D>(p, to, row, g, m[r], lsum[r], o[r], [&](int i) { return 16 * i + 4 * g; });
             }
             if (!more) return;
             rows(nh);
         }
         x = nx;
         h = nh;
+    }
     }
 }
 
@@ -284,7 +284,7 @@ namespace kvc {
 
 int launch_paged_rows(const PagedAttnParams &p, int tile_rows, hipStream_t s)
 {
-    const dim3 grid((unsigned)p.n_waves), block(64);
+    const dim3 grid((unsigned)(p.n_waves / kPagedBlockWaves)), block(64 * kPagedBlockWaves);
     const bool one = tile_rows == 16;
     switch (p.D) {
         case 64: return launch(one ? attn_paged_rows_kernel<64, 1> : attn_paged_rows_kernel<64, 2>, grid, block, 0, s, p);
