@@ -1,5 +1,5 @@
-"""Host-side sequencing of the reuse step: three library calls per segment/agent; and of the suffix that follows it, over a cache of the
-model's type or in 4 bits.
+"""Host-side sequencing of the reuse step: three library calls per segment/agent; of the suffix that follows it, over a cache of the
+model's type or in 4 bits; and of the batch of answers that continue an agent's cache, in pages.
 
 Nothing is computed here; the functions only issue the calls of include/kvcomm.h in the
 order of the reuse branch of Algorithm 1 (weights -> offset approximation per placeholder,
@@ -357,6 +357,75 @@ def suffix_step(model, q, k, v, cache, n_ctx, window=None, n_sinks=0, q_weight=N
         if window is None:
             return kv.kvcomm_suffix_attn(model, placed_q, cache_k, cache_v, n_ctx, out=out, stream=stream)
         return kv.kvcomm_suffix_attn_window(model, placed_q, cache_k, cache_v, n_ctx, window, n_sinks, out=out, stream=stream)
+
+
+class PagedCache:
+    """Keys and values of sequences of any lengths in the pages of one pool: answers that continue an agent's assembled cache, or agents decoded together.
+    A page holds page_size tokens of all layers and heads; which pages a sequence has is kept here, on the host."""
+
+    def __init__(self, model, n_pages, page_size, device):
+        self.model, self.n_pages, self.page_size, self.device = model, n_pages, page_size, device
+        # the slots of a head lie behind each other: [layer, page, head, slot, channel]
+        new = lambda: torch.zeros((model.n_layers, n_pages, model.n_kv_heads, page_size, model.head_dim), dtype=model.dtype, device=device).transpose(1, 2)
+        self.k, self.v = new(), new()
+        self.pages, self.lens, self._free, self._next = {}, {}, list(range(n_pages - 1, -1, -1)), 0
+
+    def open(self):
+        """A new sequence without tokens."""
+        seq, self._next = self._next, self._next + 1
+        self.pages[seq], self.lens[seq] = [], 0
+        return seq
+
+    def close(self, seq):
+        """Its pages are free again (for kernels behind those that read them, on the same stream)."""
+        self._free += reversed(self.pages.pop(seq))
+        del self.lens[seq]
+
+    def extend(self, seqs, rows, stream=None):
+        """The batch of these sequences, each with rows[i] more tokens, which are still to be placed."""
+        seqs, rows = list(seqs), list(rows)
+        if len(seqs) != len(rows) or not seqs or len(set(seqs)) != len(seqs) or min(rows) < 0 or any(s not in self.pages for s in seqs):
+            raise kv.KVCommError(kv.EINVAL, "extend: expected open sequences, each once, and a number of rows for each")
+        more = [-(-(self.lens[s] + n) // self.page_size) - len(self.pages[s]) for s, n in zip(seqs, rows)]
+        if sum(more) > len(self._free):
+            raise kv.KVCommError(kv.EINVAL, f"a paged cache with {len(self._free)} free pages has no room for {sum(more)}")
+        for s, n, m in zip(seqs, rows, more):
+            self.pages[s] += [self._free.pop() for _ in range(m)]
+            self.lens[s] += n
+        width = max(1, max(len(self.pages[s]) for s in seqs))
+        table = torch.tensor([self.pages[s] + [-1] * (width - len(self.pages[s])) for s in seqs], dtype=torch.int32)
+        lens = torch.tensor([self.lens[s] for s in seqs], dtype=torch.int32)
+        starts = None if all(n == 1 for n in rows) else torch.tensor([0] + rows, dtype=torch.int32).cumsum(0, dtype=torch.int32)
+        with kv.on_stream(stream):
+            return kv.Batch(table.to(self.device), lens.to(self.device), None if starts is None else starts.to(self.device), max_rows=max(rows))
+
+    def retract(self, seqs, rows):
+        """Takes back the last rows[i] tokens of each sequence."""
+        for s, n in zip(seqs, rows):
+            self.lens[s] -= n
+            keep = -(-self.lens[s] // self.page_size)
+            self._free += reversed(self.pages[s][keep:])
+            del self.pages[s][keep:]
+
+
+def batch_step(model, q, k, v, cache, seqs, rows, prefix=None, q_weight=None, k_weight=None, norm_eps=0.0, out=None, stream=None):
+    """New tokens of several sequences of a PagedCache, rows[i] of seqs[i] behind each other, from their projections q [L,Hq,n,D], k, v [L,Hkv,n,D] to
+    their attention output: norms, rotation and pages (kvcomm_place_qkv_paged), then attention over each sequence's own tokens and the prefix that all of
+    them continue, (cache_k, cache_v) of an agent's assembled cache, whose length is where their positions begin; None: at 0."""
+    seqs, rows = list(seqs), list(rows)
+    if sum(rows) != q.shape[2]:
+        raise kv.KVCommError(kv.EINVAL, f"batch_step: {sum(rows)} rows, but {q.shape[2]} queries")
+    batch = cache.extend(seqs, rows, stream)
+    try:
+        with kv.on_stream(stream):   # what only this step's kernels read belongs to their stream
+            first = 0 if prefix is None else prefix[0].shape[2]
+            placed = kv.kvcomm_place_qkv_paged(model, q, k, v, batch, cache.k, cache.v, first, q_weight=q_weight, k_weight=k_weight, norm_eps=norm_eps, stream=stream)
+            if prefix is None:
+                return kv.kvcomm_paged_attn(model, placed, cache.k, cache.v, batch, out=out, stream=stream)
+            return kv.kvcomm_paged_attn_prefix(model, placed, *prefix, cache.k, cache.v, batch, out=out, stream=stream)
+    except BaseException:   # the step has not been made: one made again finds the cache as it was
+        cache.retract(seqs, rows)
+        raise
 
 
 class TwoStreamPipeline:

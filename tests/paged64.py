@@ -67,6 +67,11 @@ class Case:
             return kv.kvcomm_paged_attn_prefix(self.model, self.q, self.prefix_k, self.prefix_v, self.pages_k, self.pages_v, self.batch, **kw)
         return kv.kvcomm_paged_attn(self.model, self.q, self.pages_k, self.pages_v, self.batch, **kw)
 
+    def workspace(self):
+        if self.prefix:
+            return kv.kvcomm_paged_attn_prefix_workspace(self.model, self.prefix, self.n, self.page, self.n_pages, self.batch)
+        return kv.kvcomm_paged_attn_workspace(self.model, self.n, self.page, self.n_pages, self.batch)
+
     def token(self, b, t):
         """(page, slot) of a token, None: it is not there."""
         if t < 0 or t >= max(self.lens[b], 0) or t // self.page >= self.table.shape[1]:
