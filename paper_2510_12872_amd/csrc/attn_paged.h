@@ -244,7 +244,9 @@ struct PagedWalk {
         }
         int64_t total = (int64_t)width * a.heads;
         // (a little more than its share each, so that rounding leaves nothing)
-        run = __builtin_amdgcn_readfirstlane((int)((float)total * a.per_wave)) + 1;
+        // (bounded whatever `starts` claims: sequences that overlap may have more rows, and halves, than a launch is planned for, and are then not all taken)
+        if (width <= 0) return false;
+        run = min(__builtin_amdgcn_readfirstlane((int)fminf((float)total * a.per_wave, 1e9f)), 1 << 30) + 1;
         // Short runs are cut within items: a wavefront that ends one item and begins another takes as long as two.  The items' last runs may be short then, so there have
         // to be wavefronts enough for one more of each.
         if (run <= kPagedShortRun && a.slots && 2 * (int64_t)items * a.heads <= a.n_waves) {
@@ -272,6 +274,7 @@ struct PagedWalk {
             at -= ahead;
             int index = a.prefix_tiles;
             for (int c = 0;; c += 64) {
+                if (c >= a.n_seqs) return false;   // (as above)
                 if (chunk != c) load(a, c);
                 if (c) upto = wave_scan(tiles(a) * padded(count(a, len))), before = wave_scan(tiles(a));
                 const int sum = __builtin_amdgcn_readlane(upto, 63);
@@ -438,7 +441,7 @@ __device__ __forceinline__ PagedPlace paged_place(const P &p, const PagedItem &i
         to.ml = p.slot_ml + slot * 2;
     }
     if (ends) {
-        if (lane < 2 && it.index < p.max_items) {
+        if (lane < 2 && (uint32_t)it.index < (uint32_t)p.max_items) {
             const int64_t begin = pos - it.count;   // of the item, on the axis
             const int first = to.kind ? to.kind : quotient(begin, run);
             p.items[((int64_t)it.lh * p.max_items + it.index) * 2 + lane] = lane ? (int)wave : first;

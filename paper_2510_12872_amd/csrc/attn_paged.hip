@@ -26,10 +26,10 @@ __global__ __launch_bounds__(256) void attn_paged_combine_kernel(const CombinePa
     const int item = known ? p.prefix_tiles + row : p.item_of[2 * row], number = known ? 0 : p.item_of[2 * row + 1];
     int first, n;
     all_rows(p, first, n);
-    if (row < first || row >= first + n || item == kDirect) return;
+    if (row < first || row >= first + n || (item < 0 && (item != kWhole || p.prefix_part < p.tile_runs))) return;   // kDirect
     const bool apart = p.n_prefix > 0 && p.walked_prefix == 0;
-    // What the walks left of an item: `count` slots from wavefront `wave` on, the last of them an item's end; or parts by rows.  (Clamped: item_of is not
-    // written for every row where starts decreases.)
+    // What the walks left of an item: `count` slots from wavefront `wave` on, the last of them an item's end; or parts by rows.  (Clamped, and only
+    // parts that there is room for: where starts decreases, items and item_of are not written for every row.)
     struct Parts {
         int wave, count, row;
         bool whole;
@@ -41,7 +41,7 @@ __global__ __launch_bounds__(256) void attn_paged_combine_kernel(const CombinePa
     auto parts_of = [&](int hkv, int index, int packed) -> Parts {
         const int32_t *e = p.items + ((int64_t)(l * p.Hkv + hkv) * p.max_items + max(0, min(index, p.max_items - 1))) * 2;
         const int w0 = e[0], w1 = e[1];
-        if (w0 < 0) return Parts{w0, 1, 0, true};
+        if (w0 < 0) return Parts{w0 == kWhole && p.prefix_part > 0 ? kWhole : kDirect, 1, 0, true};
         const int last = max(0, min(w1, p.n_waves - 1)), from = min(w0, last);
         return Parts{from, last - from + 1, packed & (p.tile_rows - 1), false};
     };
@@ -151,8 +151,8 @@ int launch_combine(const PagedAttnParams &a, hipStream_t s)
     static_cast<PagedAttnParams &>(p) = a;
     const int Hq = a.Hkv * a.G;
     const int64_t rows = (int64_t)a.L * a.batch.n_rows;
-    // Few rows: a block per head.  us, 8 sequences of 600 to 3100 tokens, one layer COMB_FEW; many: as many heads of a wavefront as leave 16384 of them (64 sequences behind a prefix,
-    // 32 layers: COMB_MANY).
+    // Few rows: a block per head.  us, 8 sequences of 600 to 3100 tokens, one layer: 8.7 as a wavefront per head, 4.9 so.  Many: as many heads of a wavefront as
+    // leave 16384 of them (64 sequences behind a prefix, 32 layers: 22; with 4096 of them 45).
     const bool few = rows * Hq <= 4096;
     p.heads = few ? 1 : (int)std::min<int64_t>(std::min(Hq, 64), std::max<int64_t>(1, rows * Hq / 16384));
     p.chunks = (Hq + p.heads - 1) / p.heads;
@@ -223,7 +223,7 @@ Plan plan_of(const kvcomm_model &m, const kvcomm_batch &b, int n_prefix)
 bool countable(const kvcomm_model &m, const kvcomm_batch &b)
 {
     const double G = m.n_q_heads / m.n_kv_heads;
-    return (double)b.n_rows * G <= (double)kMaxRows && (double)b.n_rows * m.n_q_heads * m.n_layers < 67108864.0 && (double)m.n_layers * m.n_kv_heads <= INT32_MAX;
+    return (double)b.n_rows * G <= (double)kMaxRows && (double)b.n_rows * m.n_q_heads * m.n_layers < 67000000.0 && (double)m.n_layers * m.n_kv_heads <= INT32_MAX;
 }
 
 // The direct loads' 32-bit offsets: see direct_loads_reach().

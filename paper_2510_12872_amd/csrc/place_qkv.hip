@@ -338,6 +338,7 @@ extern "C" int kvcomm_place_qkv_paged(const kvcomm_model *model, kvcomm_tensor q
     const int dt = model->dtype, es = elem_size(dt), D = model->head_dim, L = model->n_layers, n = batch->n_rows;
     if ((int64_t)first_pos + p.batch.cap > INT32_MAX) return KVCOMM_EINVAL;
     if (!(norm_eps >= 0.f) || norm_eps > FLT_MAX) return KVCOMM_EINVAL;
+    if ((double)L * ((double)model->n_q_heads + 2.0 * model->n_kv_heads) * n * D >= 34359738368.0) return KVCOMM_EUNSUPPORTED;   // 2^35 values: see launch_place()
     const bool pages = p.batch.cap > 0;   // else there is nothing to store into: keys and values are not looked at
     const kvcomm_tensor in[3] = {q, k, v};
     const kvcomm_pages *pool[2] = {&pages_k, &pages_v};

@@ -245,3 +245,26 @@ def test_no_pages_at_all():
             placed = kv.kvcomm_place_qkv_paged(m, q, k[:, :, :3], k[:, :, 3:6], batch, pool, pool.clone(), 3)
             assert torch.equal(placed[:, :, 2], kv.kvcomm_place_qkv(m, q[:, :, 2:], None, None, 3)[0][:, :, 0])
             assert torch.equal(placed[:, :, 0], kv.kvcomm_place_qkv(m, q[:, :, :1], None, None, 7)[0][:, :, 0])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("prefix", [0, 40, 300])
+def test_sequences_that_claim_the_same_rows(dtype, prefix):
+    """starts that goes up and down between 130 sequences, each with up to all rows: which rows are written, and with what, is not defined, but nothing else is."""
+    n = 60
+    c = Case(1, 2, 4, 64, dtype, rows=[n] + [0] * 129, lens=[3 * i % 50 for i in range(130)], page=16, prefix=prefix, fill=0.0)
+    need = c.workspace()
+    for starts in ([n * (i % 2) for i in range(131)], [(37 * i) % (n + 5) - 2 for i in range(131)], [-(2 ** 31) if i % 3 else 2 ** 31 - 1 for i in range(131)]):
+        c.batch.starts.copy_(torch.tensor(starts, dtype=torch.int32))
+        for most in (0, 1):
+            c.batch = kv.Batch(c.batch.table, c.batch.lens, c.batch.starts, max_rows=most)
+            ws = torch.full((max(need, c.workspace()) + 4096,), 9, dtype=torch.uint8, device="cuda")
+            guard = torch.full((1, 8, n + 16, 64), 5.0, dtype=dtype, device="cuda")
+            lse = torch.full((8 * n + 64,), 5.0, device="cuda")
+            use = c.workspace()
+            for w in (ws[:use], None):
+                c.attend(out=guard[:, :, 8:8 + n], lse_out=lse[32:32 + 8 * n].view(1, 8, n), want_lse=True, workspace=w)
+            kv.kvcomm_place_qkv_paged(c.model, c.q, c.q[:, :2], c.q[:, 2:4], c.batch, c.pages_k, c.pages_v, q_out=guard[:, :, 8:8 + n])
+            torch.cuda.synchronize()
+            assert bool((guard[:, :, :8] == 5).all()) and bool((guard[:, :, 8 + n:] == 5).all()) and bool((ws[use:] == 9).all())
+            assert bool((lse[:32] == 5).all()) and bool((lse[32 + 8 * n:] == 5).all())
