@@ -76,19 +76,29 @@ __global__ __launch_bounds__(256) void attn_paged_combine_kernel(const CombinePa
                 ml = p.slot_ml + at * 2;
             }
         };
-        // Parts k0 ... of this group, whose loads are all in flight at once, against the largest reference so far.
+        // Parts k0 ... of this group, whose loads are all in flight at once, against the largest reference so far.  (Those behind the last one are not read: 2048 rows of 3 parts
+        // each 25.1 -> 23.6 us with the kernel before.)
         float M = -INFINITY, sum = 0.f;
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
         for (int k0 = W == 4 ? sub * NG + group : group; k0 < count; k0 += W * NG * U) {
             f32x4 os[U];
             float ms[U], ls[U], top = M;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
+            for (int u = 0; u < U; ++u) ms[u] = -INFINITY, ls[u] = 0.f, os[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+            auto get = [&](int u) __attribute__((always_inline)) {
                 const float *o, *ml;
-                place(min(k0 + u * W * NG, count - 1), o, ml);
+                place(k0 + u * W * NG, o, ml);
                 ms[u] = ml[0];
                 ls[u] = ml[1];
                 os[u] = *reinterpret_cast<const f32x4 *>(o + c);
+            };
+            if (k0 + (U - 1) * W * NG < count) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) get(u);
+            } else {
+#pragma unroll
+                for (int u = 0; u < U - 1; ++u)
+                    if (k0 + u * W * NG < count) get(u);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) top = fmaxf(top, ms[u]);
@@ -98,7 +108,6 @@ __global__ __launch_bounds__(256) void attn_paged_combine_kernel(const CombinePa
             M = top;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                if (k0 + u * W * NG >= count) continue;
                 if (ms[u] != -INFINITY) {
                     const float f = __builtin_amdgcn_exp2f((ms[u] - M) * p.scale_log2);
                     sum = fmaf(f, ls[u], sum);
@@ -170,6 +179,12 @@ int launch_combine(const PagedAttnParams &a, hipStream_t s)
 //   Sequences of up to kFewRows packed rows go to the wavefront kernel, longer ones, if there may be any, to the tiles kernel; the prefix, for the rows of all of them, to one
 //   or the other.
 constexpr int kFewRows = 32;
+// A prefix for more rows than that, one of each of many sequences, goes to the wavefront kernel where that has up to so many halves of it for each wavefront.  us for the whole call
+// by that kernel / by the tiles kernel, D = 128, 8 kv heads, G = 4; halves of a wavefront: one layer, 16 sequences, prefix 8192 (2) 32 / 51, 32 sequences (4) 44 / 52,
+// 64 (8) 70 / 69, 128 (16) 113 / 81; 4 layers, 10 sequences, prefix 1000 (1) 27 / 35, 64 (4) 66 / 65; 16 layers, 16, prefix 8192 (32) 241 / 150.
+constexpr int kPrefixHalves = 4;
+// Runs of the keys of a sequence's row tile, at most.
+constexpr int kSeqMaxRuns = 16;
 
 struct Plan {
     int tile_rows, n_waves, prefix_tiles;   // of the wavefront kernel
@@ -188,18 +203,25 @@ Plan plan_of(const kvcomm_model &m, const kvcomm_batch &b, int n_prefix)
     const int64_t most = b.starts ? (b.max_rows ? std::min<int64_t>(b.max_rows, b.n_rows) : b.n_rows) * G : G;
     const bool f32 = m.dtype == KVCOMM_F32;   // the wavefront kernel takes it all
     pl.tiles = !f32 && most > kFewRows;
-    pl.tile_rows = f32 ? 16 : D < 256 && (most > 16 || (n_prefix && rows > 16 && rows <= kFewRows)) ? 32 : 16;
+    bool few_prefix = n_prefix && (f32 || rows <= kFewRows);
+    if (n_prefix && !few_prefix && !pl.tiles) {
+        const int tr = D < 256 ? 32 : 16;
+        few_prefix = (double)LH * ((rows + tr - 1) / tr) * ((n_prefix + 31) / 32) <= (double)kPrefixHalves * kChipCUs * paged_rows_waves(D, tr);
+    }
+    pl.tile_rows = f32 ? 16 : D < 256 && (most > 16 || (few_prefix && rows > 16)) ? 32 : 16;
     pl.n_waves = kChipCUs * (f32 ? paged_f32_waves(D) : paged_rows_waves(D, pl.tile_rows));
     pl.max_items = b.starts ? (pl.tiles ? (int64_t)b.n_seqs * (kFewRows / pl.tile_rows) : rows / pl.tile_rows + b.n_seqs) : (int64_t)b.n_seqs * ((G + pl.tile_rows - 1) / pl.tile_rows);
     pl.seq_runs = 1;
     if (pl.tiles) {
         pl.seq_rows = D == 256 || rows < 512 * (int64_t)b.n_seqs ? 128 : 256;
         const int64_t tiles = rows / pl.seq_rows + std::min<int64_t>(b.n_seqs, rows / (kFewRows + 1) + 1), reach = (int64_t)b.table_width * b.page_size;
-        // Keys are cut where the row tiles are few.  (The lengths lie on the device: by what the table reaches, and into runs of 512 at least.)
-        while (pl.seq_runs < kTileMaxSplits && tiles * LH * pl.seq_runs * 2 <= kChipCUs && reach >= 1024 * pl.seq_runs) pl.seq_runs *= 2;
+        // Keys are cut where the row tiles are few, up to two blocks per compute unit (of the tiles that there may be, many are not there).  The lengths lie on the
+        // device: by what the table reaches, and into runs of 512 at least.  Up to two blocks / one, one layer, 8 kv heads, G = 4, us: 4 sequences, 64 rows behind
+        // 1000 to 4000 tokens 38 / 51 (D = 256 63 / 88), 512 rows behind 3100 55 / 71, 128 behind 9000 44 / 53; up to four 40 (D = 256 76), 54, 44.
+        while (pl.seq_runs < kSeqMaxRuns && tiles * LH * pl.seq_runs * 2 <= 2 * kChipCUs && reach >= 1024 * pl.seq_runs) pl.seq_runs *= 2;
         pl.seq_units = tiles * pl.seq_runs;
     }
-    if (n_prefix && (f32 || rows <= kFewRows)) {
+    if (few_prefix) {
         pl.prefix_tiles = (int)((rows + pl.tile_rows - 1) / pl.tile_rows);
         pl.max_items += pl.prefix_tiles;
     } else if (n_prefix) {

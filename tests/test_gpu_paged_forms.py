@@ -53,6 +53,21 @@ def test_kernels_against_float64(case, prefix):
     _close(c, c.attend(want_lse=True))
 
 
+@pytest.mark.parametrize("case", [
+    # a prefix for some tiles of rows, on the wavefronts' axis: with and without starts, a last tile that is not full, sequences that end within one
+    dict(L=1, H=2, G=4, D=128, dtype=BF16, rows=[1] * 21, lens=[11 * i % 90 + 1 for i in range(21)], page=16, prefix=500, one=True),
+    dict(L=2, H=1, G=3, D=64, dtype=BF16, rows=[i % 4 for i in range(30)], lens=[i % 4 + 3 * i % 40 for i in range(30)], page=16, pad=2, before=1, prefix=257),
+    dict(L=1, H=1, G=8, D=256, dtype=BF16, rows=[1] * 9, lens=[40, 1, 0, 70, 33, 32, 31, 64, 5], page=32, prefix=300, one=True),
+    # so many that its tiles are of 128 and 256 rows, and so few of them that keys are cut
+    dict(L=4, H=8, G=8, D=64, dtype=BF16, rows=[1] * 64, lens=[7 * i % 60 + 1 for i in range(64)], page=16, prefix=700, one=True),
+    dict(L=4, H=8, G=4, D=128, dtype=BF16, rows=[1] * 30, lens=[7 * i % 60 + 1 for i in range(30)], page=16, prefix=2100, one=True),
+    dict(L=4, H=4, G=4, D=256, dtype=BF16, rows=[1] * 40, lens=[7 * i % 60 + 1 for i in range(40)], page=16, prefix=1100, one=True),
+], ids=_id)
+def test_tokens_of_many_sequences_behind_a_prefix(case):
+    c = Case(**case)
+    _close(c, c.attend(want_lse=True))
+
+
 @pytest.mark.parametrize("prefix", [0, 70])
 @pytest.mark.parametrize("case", [CASES[1], CASES[2], CASES[4], CASES[6], CASES[7]], ids=_id)
 def test_without_a_workspace(case, prefix):
