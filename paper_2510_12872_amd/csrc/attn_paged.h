@@ -178,7 +178,9 @@ __device__ __forceinline__ void paged_store_row(const P &p, int l, int hq, int r
 }
 
 // ------------------------------------------------------------------------------------------ the walk
-constexpr int kPagedShortRun = 8;   // halves of runs that are cut within items, at most
+// Halves of runs that are cut within items, at most.  (The shortest run in any case: one half.  One layer, prefix 2560 and 8 tokens, with runs of 1 / 2 / 4 / 8 halves
+// at least: 12.4 / 15.5 / 21.9 / 37.3 us.)
+constexpr int kPagedShortRun = 8;
 typedef const __attribute__((address_space(4))) int32_t const_int;   // read through the scalar cache (whole-wavefront values)
 __device__ __forceinline__ const_int *scalar(const int32_t *x) { return (const_int *)(uintptr_t)x; }
 
@@ -411,7 +413,8 @@ private:
 };
 
 constexpr int kPagedBlockWaves = 4;   // of a wavefront kernel's block, which share nothing
-// Wavefronts of attn_paged_rows_kernel that a compute unit holds: by LDS, and by registers.
+// Wavefronts of attn_paged_rows_kernel on a compute unit: LDS has room for 10 of 16 KB at D = 128 (8 are faster, see there), 5 at D = 256 and 20 at D = 64, registers for 8 with
+// tiles of 32 rows.
 constexpr int paged_rows_waves(int D, int rows) { return D == 256 ? 4 : D == 128 || rows == 32 ? 8 : 16; }
 
 constexpr int paged_f32_waves(int D) { return D == 256 ? 4 : 8; }
@@ -557,6 +560,10 @@ __device__ __forceinline__ void paged_exact_segment(const P &p0, const PagedItem
 
 // ------------------------------------------------------------------------------------------ tiles of many rows
 // attn_mfma_kernel (suffix_attn.hip) with Keys::kPaged: a block is a tile of rows and a run of 64-key tiles of one sequence's pages, or of the prefix.
+// What bounds it: the matrix cores with their vector work, as over a whole cache.  4 layers, 6 sequences of 100 to 2000 rows behind up to 6000 tokens (1258 GFLOP)
+// 1.19 ms = 1.05 PFLOP/s, matrix pipes busy in 51 % of the cycles; 32 layers, a prefix of 8192 for 64 rows of each (layer, head) 0.25 ms (54 %).
+// Where a call has both, a sequence's block joins the prefix's parts to its rows at its end: 8 layers, 16 suffixes behind a prefix of 4096, 0.45 ms; with all of
+// them joined by the combine kernel 0.51 (110 us of it there).
 struct PagedTileParams : PagedAttnParams {   // row_o null: rows go to `out`.  Over the prefix: k, v and their strides are the prefix's, one page
     int32_t over_prefix;
     int32_t n_items;

@@ -14,9 +14,13 @@ __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)"
 
 // attn_paged_rows_kernel: 16 * RH packed rows on 16x16x32 MFMAs, products, operand layout and LDS swizzles as in attn_rows_kernel16, but a wavefront is alone: it
 // walks 32 keys after the other of its run, K and V of a half go global -> LDS into its own 64 * D bytes, and those of the next half, of whatever item, are
-// requested as soon as the operands of this one are in registers.  Nothing is joined inside the launch, so that no wavefront waits for another one;
-// their number per compute unit is what fits LDS.
-// What bounds it is HBM.  A half lies in one page or in two, whose entries are read, through the scalar cache, a half ahead.
+// requested as soon as the operands of this one are in registers.  Nothing is joined inside the launch, so that no wavefront waits for another one.
+// A half lies in one page or in two, whose entries are read, through the scalar cache, a half ahead.
+// What bounds it: HBM in large launches.  32 layers, 16 sequences of 500 to 16 000 tokens (13.5 GB) 2.01 ms = 6.7 TB/s, every byte read once; a
+// prefix of 32 768 for four sequences (4.3 GB) 0.69 ms.  In small ones the chain of a wavefront: one layer, 8 sequences (55 MB) 13 us, of which the first
+// rows arrive after 4.5 and the halves after that take 1.1 each.
+// Wavefronts of a compute unit, the large launch, ms with cached / non-temporal loads: 10 (what fits LDS) 2.38 / 2.18, 8 2.20 / 2.01, 6 - / 2.07, 4 - / 1.99
+// (4 leave the small launches' chains longer).  Wavefronts of a block, large launch / fp32 kernel of the tiny one: 1 2.08 ms / 9.2 us, 2 2.08 / 9.2, 4 2.00 / 8.2, 8 2.01 / 10.0.
 template <int D, int RH>
 __global__ __launch_bounds__(64 * kPagedBlockWaves, RH == 2 || D >= 128 ? 2 : 4) void attn_paged_rows_kernel(const PagedAttnParams)
 {

@@ -7,7 +7,8 @@
 // which the last-level cache then holds); with a token or two the launch is one chain of load, trigonometry, reduction and store (2.6 us; 3.6 us from launch to launch).
 // A thread owns the 16 bytes of channels c ... and the 16 bytes of c + D/2 ..., both members of its pairs, and keeps its (token, channels)
 // from head to head: the cosines and sines, in double up to their rounding, are formed once per thread and stay in registers.
-// kvcomm_place_qkv_paged: the same kernel for the rows of a batch; a row's sequence, position and slot are found while its values travel.
+// kvcomm_place_qkv_paged: the same kernel for the rows of a batch; a row's sequence, position and slot are found while its values travel.  What bounds it is the same:
+// 32 layers, six prompts of 100 to 1200 tokens with norms (2.55 GB) 494 us = 5.2 TB/s, half read and half written (a copy of 2 GiB: 4.9); a token of 8 sequences, one layer, 3.6 us.
 #include <float.h>
 
 #include <type_traits>
