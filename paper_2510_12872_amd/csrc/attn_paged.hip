@@ -264,6 +264,12 @@ int paged_attn(const kvcomm_model *model, const kvcomm_tensor &q, const kvcomm_t
     if (n_prefix && ((st = check_tensor(prefix_k, dt, true)) || (st = check_tensor(prefix_v, dt, true)))) return st;
     if (p.batch.cap && ((st = check_pages(pages_k, dt)) || (st = check_pages(pages_v, dt)))) return st;
     if (!aligned4(lse_out)) return KVCOMM_EINVAL;
+    {   // queries are read again after outputs of the same rows have been written
+        const int L = model->n_layers, Hq = model->n_q_heads, es = elem_size(dt);
+        if (extents_overlap(extent_of(out, L, Hq, batch->n_rows, D, es), extent_of(q, L, Hq, batch->n_rows, D, es)) &&
+            !beside_each_other(out, Hq, D * es, es, q, Hq, D * es, es, L))
+            return KVCOMM_EINVAL;
+    }
     if ((int64_t)n_prefix + p.batch.cap > kMaxPagedTokens || !countable(*model, *batch)) return KVCOMM_EUNSUPPORTED;
     if (dt == KVCOMM_BF16 && ((p.batch.cap && (!reaches(pages_k.stride_token, D) || !reaches(pages_v.stride_token, D))) ||
                               (n_prefix && (!reaches(prefix_k.stride_token, D) || !reaches(prefix_v.stride_token, D)))))

@@ -187,6 +187,8 @@ def test_refusals_of_the_library():
                    dict(q=T(0x10000, st=4)), dict(pk=none), dict(pk=T(0xb000000), pv=none), dict(pk=T(0xb000000), n_prefix=0), dict(pk=T(0xb000000), n_prefix=-1),
                    dict(m=model(0))):
         assert attend(**change) == -1, change
+    for q in (T(0x10000), T(0x10000 + 256), T(0x10000 + 16)):   # the outputs are the queries, or share some of them
+        assert attend(q=q, out=T(0x10000)) == -1 and attend(q=q, out=T(0x10000), pk=T(0xb000000)) == -1
     assert attend(m=model(96)) == -2 and attend(pk=T(0xb000000), n_prefix=2 ** 30 + 1) == -2
     for change in (dict(q=none), dict(out=none), dict(k=none), dict(pv=P(None)), dict(pk=P(0x20000008)), dict(first=2 ** 31 - 100), dict(eps=-1.0), dict(eps=float("nan")),
                    dict(wq=0x1000), dict(wq=0x1004, eps=1e-5), dict(q=none, out=none, wq=0x1000, eps=1e-5), dict(pk=P(0x10000)), dict(pk=P(0x40000000)), dict(out=T(0x800000)),
