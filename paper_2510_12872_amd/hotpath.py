@@ -392,15 +392,22 @@ class PagedCache:
         for s, n, m in zip(seqs, rows, more):
             self.pages[s] += [self._free.pop() for _ in range(m)]
             self.lens[s] += n
-        width = max(1, max(len(self.pages[s]) for s in seqs))
-        table = torch.tensor([self.pages[s] + [-1] * (width - len(self.pages[s])) for s in seqs], dtype=torch.int32)
-        lens = torch.tensor([self.lens[s] for s in seqs], dtype=torch.int32)
-        starts = None if all(n == 1 for n in rows) else torch.tensor([0] + rows, dtype=torch.int32).cumsum(0, dtype=torch.int32)
-        with kv.on_stream(stream):
-            return kv.Batch(table.to(self.device), lens.to(self.device), None if starts is None else starts.to(self.device), max_rows=max(rows))
+        try:
+            width = max(1, max(len(self.pages[s]) for s in seqs))
+            table = torch.tensor([self.pages[s] + [-1] * (width - len(self.pages[s])) for s in seqs], dtype=torch.int32)
+            lens = torch.tensor([self.lens[s] for s in seqs], dtype=torch.int32)
+            starts = None if all(n == 1 for n in rows) else torch.tensor([0] + rows, dtype=torch.int32).cumsum(0, dtype=torch.int32)
+            with kv.on_stream(stream):
+                return kv.Batch(table.to(self.device), lens.to(self.device), None if starts is None else starts.to(self.device), max_rows=max(rows))
+        except BaseException:   # (no memory for the batch)
+            self.retract(seqs, rows)
+            raise
 
     def retract(self, seqs, rows):
         """Takes back the last rows[i] tokens of each sequence."""
+        seqs, rows = list(seqs), list(rows)
+        if len(seqs) != len(rows) or len(set(seqs)) != len(seqs) or any(s not in self.pages or not 0 <= n <= self.lens[s] for s, n in zip(seqs, rows)):
+            raise kv.KVCommError(kv.EINVAL, "retract: expected open sequences, each once, and a number of rows that each has")
         for s, n in zip(seqs, rows):
             self.lens[s] -= n
             keep = -(-self.lens[s] // self.page_size)

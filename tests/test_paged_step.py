@@ -36,6 +36,24 @@ def test_pages_are_handed_out_and_taken_back():
     assert c.extend([b], [0]).starts.tolist() == [0, 0]
 
 
+def test_a_batch_that_cannot_be_made_takes_no_pages(monkeypatch):
+    c = _cpu()
+    a = c.open()
+    c.extend([a], [20])
+
+    def no_memory(*args, **kw):
+        raise MemoryError
+    with monkeypatch.context() as m:
+        m.setattr(hotpath.kv, "Batch", no_memory)
+        with pytest.raises(MemoryError):
+            c.extend([a], [40])
+    assert c.lens[a] == 20 and len(c.pages[a]) == 2 and len(c._free) == 4
+    for seqs, rows in (([a], [21]), ([a], [-1]), ([a, a], [1, 1]), ([9], [0]), ([a], [])):
+        with pytest.raises(kv.KVCommError):
+            c.retract(seqs, rows)
+        assert c.lens[a] == 20 and len(c.pages[a]) == 2 and len(c._free) == 4
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("n_prefix", [0, 100])
