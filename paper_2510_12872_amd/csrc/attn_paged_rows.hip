@@ -175,6 +175,8 @@ __global__ __launch_bounds__(64 * kPagedBlockWaves, RH == 2 || D >= 128 ? 2 : 4)
         Half nx = x;
         if (more) nx = half_at(nh);
 
+        // Every counted wait below stands behind loads that are certain to have been issued: a half has LPT loads of K and LPT of V, or, where its
+        // item has no tokens (limit 0), none of either.
         wait_loads<LPT>();               // K has landed (V may be outstanding)
         bf16x8 ka[NF];                   // all operand reads in flight at once: ks = i / 2, keys 16 * (i & 1) ...
 #pragma unroll
@@ -235,10 +237,10 @@ __global__ __launch_bounds__(64 * kPagedBlockWaves, RH == 2 || D >= 128 ? 2 : 4)
             pf[r] = as_bf16x8(pk);
             lsum[r] += rs0 + rs1;
         }
-        if (more)
+        if (more && nx.limit > 0)
             wait_loads<LPT>();   // V has landed (K of the next half may be outstanding)
         else
-            wait_loads<0>();
+            wait_loads<0>();     // (no K behind it)
         bf16x8 va[NF];
 #pragma unroll
         for (int db = 0; db < NF; ++db) va[db] = lds_read_tr_pair(vbuf + v_off[db], vbuf + v_off[db] + 16 * ROWB);
