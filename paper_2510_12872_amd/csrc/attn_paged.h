@@ -234,20 +234,21 @@ struct PagedWalk {
     {
         const Args a;
         pad = 1;
-        load(a, 0);
+        bool falls = load(a, 0);
         const int before0 = a.prefix_tiles * a.prefix_count();
         int upto = wave_scan(tiles(a) * count(a, len)), before = wave_scan(tiles(a));   // (kept: most batches have no more)
         int ahead = before0, items = a.prefix_tiles + __builtin_amdgcn_readlane(before, 63);
         width = ahead + __builtin_amdgcn_readlane(upto, 63);
         for (int c = 64; c < a.n_seqs; c += 64) {
-            load(a, c);
+            falls |= load(a, c);
             width += __builtin_amdgcn_readlane(wave_scan(tiles(a) * count(a, len)), 63);
             items += __builtin_amdgcn_readlane(wave_scan(tiles(a)), 63);
         }
         int64_t total = (int64_t)width * a.heads;
         // (a little more than its share each, so that rounding leaves nothing)
-        // (bounded whatever `starts` claims: sequences that overlap may have more rows, and halves, than a launch is planned for, and are then not all taken)
-        if (width <= 0) return false;
+        // Where `starts` falls, sequences may share rows, and have more of them together than the batch: sums that 31 bits do not hold.  Nothing is walked then.
+        // (Where it does not, the sequences' rows are those of the batch at most, whose halves the host has counted.)
+        if (falls || width <= 0) return false;
         run = min(__builtin_amdgcn_readfirstlane((int)fminf((float)total * a.per_wave, 1e9f)), 1 << 30) + 1;
         // Short runs are cut within items: a wavefront that ends one item and begins another takes as long as two.  The items' last runs may be short then, so there have
         // to be wavefronts enough for one more of each.
@@ -276,7 +277,7 @@ struct PagedWalk {
             at -= ahead;
             int index = a.prefix_tiles;
             for (int c = 0;; c += 64) {
-                if (c >= a.n_seqs) return false;   // (as above)
+                if (c >= a.n_seqs) return false;
                 if (chunk != c) load(a, c);
                 if (c) upto = wave_scan(tiles(a) * padded(count(a, len))), before = wave_scan(tiles(a));
                 const int sum = __builtin_amdgcn_readlane(upto, 63);
@@ -356,7 +357,7 @@ private:
         __device__ __forceinline__ int prefix_count() const { return (n_prefix + 31) / 32; }
     };
 
-    __device__ __forceinline__ void load(const Args &a, int c)
+    __device__ __forceinline__ bool load(const Args &a, int c)   // does `starts` fall there?
     {
         chunk = c;
         const int b = min(c + lane, a.n_seqs - 1);
@@ -366,10 +367,12 @@ private:
         if (a.starts) {
             const int s0 = a.starts[b], s1 = a.starts[b + 1];
             first = max(0, min(s0, a.n_rows));
-            n = max(0, min(s1, a.n_rows) - first);
+            n = max(0, min(s1, a.n_rows)) - first;
         }
-        n = c + lane < a.n_seqs ? n : 0;
+        const bool falls = __builtin_amdgcn_ballot_w64(n < 0) != 0;
+        n = c + lane < a.n_seqs ? max(0, n) : 0;
         len = max(0, l);
+        return falls;
     }
     __device__ __forceinline__ void enter(const Args &a, int c)
     {

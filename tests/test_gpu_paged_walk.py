@@ -62,3 +62,27 @@ def test_a_prefix_and_no_pages(G, D, n_pages, width):
     for kw in (dict(), dict(workspace=torch.empty((0,), dtype=torch.uint8, device="cuda"))):
         got = kv.kvcomm_paged_attn_prefix(m, q, k, v, pool, pool.clone(), batch, **kw)
         assert bool(((got.double() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n_seqs,n_rows,entries", [(123, 54728, 11), (266, 59538, 14), (128, 46555, 13)])
+def test_more_rows_together_than_the_batch_has(dtype, n_seqs, n_rows, entries):
+    """starts that falls from sequence to sequence: every other one claims all rows, and their halves together leave 31 bits.  Which rows are written is not defined,
+    but nothing else is, and the call ends."""
+    D, page = 64, 65536
+    m = kv.Model(1, 1, 1, D, dtype, 1e4)
+    pool = torch.zeros((1, 1, 1, page, D), dtype=dtype, device="cuda")
+    table = torch.zeros((n_seqs, entries), dtype=torch.int32, device="cuda")   # every token in the one page
+    lens = torch.full((n_seqs,), entries * page, dtype=torch.int32, device="cuda")
+    starts = torch.tensor([n_rows * (b % 2) for b in range(n_seqs + 1)], dtype=torch.int32, device="cuda")
+    batch = kv.Batch(table, lens, starts, max_rows=1)   # (a hint: the wavefront kernels take them)
+    q = torch.zeros((1, 1, n_rows, D), dtype=dtype, device="cuda")
+    guard = torch.full((1, 1, n_rows + 128, D), 5.0, dtype=dtype, device="cuda")
+    lse = torch.full((n_rows + 128,), 5.0, device="cuda")
+    need = kv.kvcomm_paged_attn_workspace(m, n_rows, page, 1, batch)
+    ws = torch.full((need + 4096,), 9, dtype=torch.uint8, device="cuda")
+    for w in (ws[:need], ws[:0]):
+        kv.kvcomm_paged_attn(m, q, pool, pool, batch, out=guard[:, :, 64:64 + n_rows], lse_out=lse[64:64 + n_rows].view(1, 1, n_rows), want_lse=True, workspace=w)
+    torch.cuda.synchronize()
+    assert bool((guard[:, :, :64] == 5).all()) and bool((guard[:, :, 64 + n_rows:] == 5).all()) and bool((ws[need:] == 9).all())
+    assert bool((lse[:64] == 5).all()) and bool((lse[64 + n_rows:] == 5).all())
