@@ -573,7 +573,8 @@ int kvcomm_place_qkv_paged(const kvcomm_model *model, kvcomm_tensor q, kvcomm_te
  * or an entry that is no page are computed again key by key, as in kvcomm_suffix_attn_kv4).  Reproducible: no atomics; a row's sums depend on lens and starts
  * of the whole batch, by the cut of the keys.
  * Errors: KVCOMM_EINVAL / KVCOMM_EUNSUPPORTED as above; KVCOMM_EUNSUPPORTED for token strides as in kvcomm_suffix_attn and where the rows or the
- * launch's threads do not fit 31 or 32 bits: from n_rows * Hq * L = 67 000 000 on, or where the halves (32 keys) of all row tiles of one (layer, kv head) may be 2^31.
+ * launch's threads do not fit 31 or 32 bits: from n_rows * Hq * L = 67 000 000 on, or where the halves (32 keys) of all row tiles of one (layer, kv head) may be 2^31, or
+ * those of all of them 990 000 000 for each of the launch's wavefronts (1024 to 4096).
  * A NaN that rows see costs much: prompts of 100 to 2000 tokens, 4 layers, with one in every head 1.2 -> 770 ms, a token of 8 sequences, one layer, 20 -> 176 us. */
 size_t kvcomm_paged_attn_workspace(const kvcomm_model *model, const kvcomm_batch *batch);
 

@@ -181,6 +181,8 @@ __device__ __forceinline__ void paged_store_row(const P &p, int l, int hq, int r
 // Halves of runs that are cut within items, at most.  (The shortest run in any case: one half.  One layer, prefix 2560 and 8 tokens, with runs of 1 / 2 / 4 / 8 halves
 // at least: 12.4 / 15.5 / 21.9 / 37.3 us.)
 constexpr int kPagedShortRun = 8;
+// Halves of a run, at most: longer ones are refused before the launch.
+constexpr int kPagedMostRun = 1000000000;
 typedef const __attribute__((address_space(4))) int32_t const_int;   // read through the scalar cache (whole-wavefront values)
 __device__ __forceinline__ const_int *scalar(const int32_t *x) { return (const_int *)(uintptr_t)x; }
 
@@ -249,7 +251,7 @@ struct PagedWalk {
         // Where `starts` falls, sequences may share rows, and have more of them together than the batch: sums that 31 bits do not hold.  Nothing is walked then.
         // (Where it does not, the sequences' rows are those of the batch at most, whose halves the host has counted.)
         if (falls || width <= 0) return false;
-        run = min(__builtin_amdgcn_readfirstlane((int)fminf((float)total * a.per_wave, 1e9f)), 1 << 30) + 1;
+        run = __builtin_amdgcn_readfirstlane((int)fminf((float)total * a.per_wave, (float)kPagedMostRun)) + 1;
         // Short runs are cut within items: a wavefront that ends one item and begins another takes as long as two.  The items' last runs may be short then, so there have
         // to be wavefronts enough for one more of each.
         if (run <= kPagedShortRun && a.slots && 2 * (int64_t)items * a.heads <= a.n_waves) {

@@ -306,10 +306,10 @@ int paged_attn(const kvcomm_model *model, const kvcomm_tensor &q, const kvcomm_t
     const int64_t LH = (int64_t)p.L * p.Hkv;
     const double most_blocks = 4294967296.0 / 512;   // a launch holds fewer than 2^32 threads
     if ((double)pl.seq_units * LH >= most_blocks || (double)pl.prefix_units * LH >= most_blocks || pl.max_items > INT32_MAX / 2) return KVCOMM_EUNSUPPORTED;
-    // The axis: halves of a (layer, kv head) in 31 bits, and of a run.
+    // The axis: halves of a (layer, kv head) in 31 bits, and of a run up to kPagedMostRun (less what the wavefronts add to their share against rounding).
     const int64_t most_tiles = batch->starts ? rows / ((int64_t)p.L * p.Hkv * pl.tile_rows) + batch->n_seqs : (int64_t)batch->n_seqs * ((p.G + pl.tile_rows - 1) / pl.tile_rows);
     const double axis = (double)most_tiles * ((double)(p.batch.cap + 31) / 32 + (scratch ? 0.0 : (double)(n_prefix + 31) / 32) + 1) + (double)pl.prefix_tiles * ((n_prefix + 31) / 32);
-    if (axis >= 2147483647.0 || axis * LH / pl.n_waves >= 2147483000.0) return KVCOMM_EUNSUPPORTED;
+    if (axis >= 2147483647.0 || axis * LH / pl.n_waves >= 0.99 * kPagedMostRun) return KVCOMM_EUNSUPPORTED;
     p.tile_rows = pl.tile_rows;
     p.n_waves = pl.n_waves;
     p.per_wave = 1.000001f / (float)pl.n_waves;
