@@ -565,7 +565,8 @@ int kvcomm_place_qkv_paged(const kvcomm_model *model, kvcomm_tensor q, kvcomm_te
 
 /* Causal attention of a batch over its pages: row i of sequence b sees the tokens 0 ... lens[b] - n_b + i that are there.
  *   q, out       [L, Hq, n_rows, D], sharing no bytes (KVCOMM_EINVAL; nor may out, lse_out or workspace share any with what else the call reads or writes, which
- *                is not looked at);  lse_out  DEVICE [L, Hq, n_rows] fp32 or NULL.  A row that sees nothing: output 0, log-sum-exp -infinity.
+ *                is not looked at);  lse_out  DEVICE [L, Hq, n_rows] fp32 or NULL.  A row that sees no key: output 0, log-sum-exp -infinity; one that
+ *                sees keys, but none with a score above -infinity: NaN, log-sum-exp -infinity, as kvcomm_suffix_attn.
  *   workspace    DEVICE scratch of kvcomm_paged_attn_workspace() bytes, 16-byte aligned, or NULL: with it the keys of a sequence are shared out over
  *                several thread blocks where there are few rows.  Without it (NULL, too small or misaligned) the same result up to rounding, only slower.
  *                Its contents do not matter before the call and are undefined afterwards.

@@ -9,6 +9,8 @@
 // row, in the second of its two slots, or, if it holds the item's last half, in the first.  attn_paged_combine_kernel joins them.
 #pragma once
 
+#include <float.h>
+
 #include "attn_common.h"
 #include "paged.h"
 
@@ -78,6 +80,11 @@ __device__ __forceinline__ P &again(P &p)
     return *q;
 }
 
+// The reference that a row, or a part of one, begins with if it sees a key: if none of its scores is above -infinity, it ends with that and sum 0, which beside
+// another part's score weighs nothing and alone is the formula's 0 / 0.  A row that sees no key has -infinity all along, and becomes 0.
+constexpr float kNoScore = -FLT_MAX;
+__device__ __forceinline__ bool paged_state_is_odd(float zero, float m, float sum) { return state_is_odd(zero, m <= kNoScore ? -INFINITY : m, sum); }
+
 // One row (sequence b, row `row` of the queries, query head hq) over the halves [h0, h1) by the formula, key by key, in fp32; what the row does not
 // see (`last`: the last token of its pages that it sees) is not looked at.  Whole rows: halves 0 ... of the prefix, then of the pages.
 // Returns reference and sum; lanes 0 ... D / 8 - 1 hold channels 8 * lane ... of the unnormalised output.
@@ -132,7 +139,7 @@ __device__ __forceinline__ void paged_exact_row(const P &p0, int l, int hkv, int
                 for (int j = 0; j < 8; ++j) s = fmaf(qq[j], kk[j], s);
             }
         }
-        float mx = s;
+        float mx = seen ? fmaxf(s, kNoScore) : -INFINITY;
 #pragma unroll
         for (int off = 32; off >= 1; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
         const float m_new = fmaxf(m, mx);
@@ -466,7 +473,7 @@ __device__ __forceinline__ PagedPlace paged_place(const P &p, const PagedItem &i
 }
 
 // Another part of a row, (m2, l2), joined to (m, l): its outputs are to be multiplied by f2 (and left out where that is 0: they may never have been written), the
-// row's own by f.  A reference of -infinity has seen no key and has sum 0, or nothing but NaN scores and a sum that says so.
+// row's own by f.  A reference of -infinity has seen no key and has sum 0.
 __device__ __forceinline__ void join_part(float &m, float &l, float m2, float l2, float scale_log2, float &f, float &f2)
 {
     const float M = fmaxf(m, m2);
@@ -474,6 +481,12 @@ __device__ __forceinline__ void join_part(float &m, float &l, float m2, float l2
     f2 = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m2 - M) * scale_log2);
     l = (m == -INFINITY ? l : l * f) + (m2 == -INFINITY ? l2 : l2 * f2);
     m = M;
+}
+
+// What the reference of a row whose last token is `last` begins with, over a segment from half seg0 of the item on.
+__device__ __forceinline__ float first_reference(const PagedItem &it, int seg0, int last)
+{
+    return seg0 < it.walk || last >= 32 * (seg0 - it.walk) ? kNoScore : -INFINITY;
 }
 
 // Row r of an item's tile, in that place.

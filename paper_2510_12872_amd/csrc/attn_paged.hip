@@ -106,7 +106,7 @@ __global__ __launch_bounds__(256) void attn_paged_combine_kernel(const CombinePa
 #pragma unroll
             for (int u = 0; u < U; ++u) top = fmaxf(top, ms[u]);
             const float f0 = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - top) * p.scale_log2);
-            sum = M == -INFINITY ? sum : sum * f0;   // (nothing seen: 0; nothing but NaN scores: NaN)
+            sum = M == -INFINITY ? sum : sum * f0;   // (nothing seen: 0)
             acc *= f0;
             M = top;
 #pragma unroll

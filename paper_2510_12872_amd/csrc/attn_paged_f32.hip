@@ -102,7 +102,7 @@ __global__ __launch_bounds__(64 * kPagedBlockWaves, D == 256 ? 1 : 2) void attn_
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int c = 0; c < 4; ++c) o[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-        m = -INFINITY;
+        m = first_reference(cur, seg0, last);
         lsum = 0.f;
     };
 
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(64 * kPagedBlockWaves, D == 256 ? 1 : 2) void attn_
                 for (int c = 0; c < 4; ++c) o[t][c] *= corr;
             m = m_new;
         }
-        const float ref = m == -INFINITY ? 0.f : m;   // a row that has seen no key yet: exponentials 0
+        const float ref = m == -INFINITY ? 0.f : m;   // a row that sees no key: exponentials 0
 #pragma unroll
         for (int r = 0; r < 4; ++r) s[r] = __builtin_amdgcn_exp2f((s[r] - ref) * p.scale_log2);
         lsum += (s[0] + s[1]) + (s[2] + s[3]);
@@ -178,7 +178,7 @@ __global__ __launch_bounds__(64 * kPagedBlockWaves, D == 256 ? 1 : 2) void attn_
             float zero = lsum * 0.f;
 #pragma unroll
             for (int i = 0; i < 16 * NT; ++i) zero = fmaf(o[i / 16][i / 4 % 4][i % 4], 0.f, zero);
-            if (__builtin_expect(__builtin_amdgcn_ballot_w64(no_page || state_is_odd(zero, m, lsum)) != 0, 0)) {
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(no_page || paged_state_is_odd(zero, m, lsum)) != 0, 0)) {
                 paged_exact_segment<float, D, TR>(p, cur, to, seg0, h, lane);
                 if (!more) return;
                 break;

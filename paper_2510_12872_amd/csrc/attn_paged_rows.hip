@@ -137,7 +137,7 @@ __global__ __launch_bounds__(64 * kPagedBlockWaves, RH == 2 || D >= 128 ? 2 : 4)
             for (int ks = 0; ks < NF / 2; ++ks) qf[x][ks] = as_bf16x8(load16(q + ks * 32 + g * 8));
 #pragma unroll
             for (int db = 0; db < NF; ++db) o[x][db] = f32x4{0.f, 0.f, 0.f, 0.f};
-            m[x] = -INFINITY, mc[x] = 0.f, lsum[x] = 0.f;
+            m[x] = first_reference(cur, seg0, last[x]), mc[x] = 0.f, lsum[x] = 0.f;
         }
         __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0), seen by the compiler: it puts no wait for the queries into the loop
     };
@@ -217,7 +217,7 @@ __global__ __launch_bounds__(64 * kPagedBlockWaves, RH == 2 || D >= 128 ? 2 : 4)
 #pragma unroll
                 for (int db = 0; db < NF; ++db) o[r][db] *= corr;
                 m[r] = m_new;
-                mc[r] = m[r] == -INFINITY ? 0.f : m[r] * p.scale_log2;   // a row that has seen no key yet: exponentials 0
+                mc[r] = m[r] == -INFINITY ? 0.f : m[r] * p.scale_log2;   // a row that sees no key: exponentials 0
             }
         }
         // Probabilities are rounded to bf16 for the second product, as in the other attention kernels; their sums take them unrounded.
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(64 * kPagedBlockWaves, RH == 2 || D >= 128 ? 2 : 4)
                 float zero = lsum[r] * 0.f;
 #pragma unroll
                 for (int i = 0; i < 4 * NF; ++i) zero = fmaf(o[r][i / 4][i % 4], 0.f, zero);
-                odd |= state_is_odd(zero, m[r], lsum[r]);
+                odd |= paged_state_is_odd(zero, m[r], lsum[r]);
             }
             if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, 0)) {
                 paged_exact_segment<bf16_t, D, TR>(p, cur, to, seg0, h, lane);

@@ -671,6 +671,10 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Par
                     sbuf[h][i & 1][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qf[c][i >> 1], i < 2 ? f32x4{0.f, 0.f, 0.f, 0.f} : sbuf[h][i & 1][c], 0, 0, 0);
             }
         }
+        if constexpr (kPaged) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) m[h] = qi[h] >= origin ? kNoScore : -INFINITY;
+        }
         ExpState st;
         rereference(sbuf[0], pbuf[0], st, limit_of(0), true);
         lsum[0] = st.rs[0];
@@ -755,7 +759,7 @@ __global__ __launch_bounds__(64 * NW, FORM % 16) void attn_mfma_kernel(const Par
             float zero = lsum[h] * 0.f;
 #pragma unroll
             for (int i = 0; i < 4 * NF; ++i) zero = fmaf(o[h][i / 4][i % 4], 0.f, zero);
-            odd |= state_is_odd(zero, m[h], query_sum(lsum[h]));
+            odd |= kPaged ? paged_state_is_odd(zero, m[h], query_sum(lsum[h])) : state_is_odd(zero, m[h], query_sum(lsum[h]));
         }
         if (__syncthreads_or(odd || no_page)) {
             if constexpr (kPaged)
