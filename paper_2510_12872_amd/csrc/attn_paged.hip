@@ -163,9 +163,11 @@ int launch_combine(const PagedAttnParams &a, hipStream_t s)
     static_cast<PagedAttnParams &>(p) = a;
     const int Hq = a.Hkv * a.G;
     const int64_t rows = (int64_t)a.L * a.batch.n_rows;
-    // Few rows: a block per head.  us, 8 sequences of 600 to 3100 tokens, one layer: 8.7 as a wavefront per head, 4.9 so.  Many: as many heads of a wavefront as
+    // Few rows: a block per head.  us, the kernel alone, 8 sequences of 600 to 3100 tokens, one layer: 8.7 as a wavefront per head, 4.9 so.  Many: as many heads of a wavefront as
     // leave 16384 of them (64 sequences behind a prefix, 32 layers: 22; with 4096 of them 45).
-    const bool few = rows * Hq <= 4096;
+    // The line, us for the whole call with a block / a wavefront per head, D = 128, 32 heads but for the f32 ones (D = 64, 8): (layer, head, row) triples 256 11.5 / 13.0, 512 f32 13.1 / 13.5,
+    // 1024 17.5 / 17.5, 121.4 / 120.9 and f32 20.8 / 20.6, 2048 27.6 / 26.1, 107.8 / 106.2 and f32 32.3 / 31.7, 4096 45.5 / 43.6, 119.1 / 115.9 and f32 40.5 / 37.7, 8192 84.3 / 79.4.
+    const bool few = rows * Hq <= 1024;
     p.heads = few ? 1 : (int)std::min<int64_t>(std::min(Hq, 64), std::max<int64_t>(1, rows * Hq / 16384));
     p.chunks = (Hq + p.heads - 1) / p.heads;
     p.by_chunks = make_divisor((uint32_t)p.chunks);
