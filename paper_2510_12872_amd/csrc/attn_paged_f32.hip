@@ -174,6 +174,10 @@ __global__ __launch_bounds__(64 * kPagedBlockWaves, D == 256 ? 1 : 2) void attn_
             // ---- the segment [seg0, h] of the item is done.  Lane (n, g) holds channels 64 * t + 16 * g + 4 * r + c of row n.
             PagedArgs &p = paged_args();
             const PagedPlace to = paged_place<TR>(p, cur, seg0, h, pos, walk.run, wave, lane);
+            if (x.limit == 0) {   // an item without tokens: nothing was loaded, and what an earlier item has left in the registers does not count
+#pragma unroll
+                for (int i = 0; i < 4 * NT; ++i) o[i / 4][i % 4] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
             lsum = query_sum(lsum);
             float zero = lsum * 0.f;
 #pragma unroll

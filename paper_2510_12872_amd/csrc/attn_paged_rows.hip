@@ -256,6 +256,10 @@ __global__ __launch_bounds__(64 * kPagedBlockWaves, RH == 2 || D >= 128 ? 2 : 4)
             PagedArgs &p = paged_args();
             const PagedPlace to = paged_place<TR>(p, cur, seg0, h, pos, walk.run, wave, lane);
             bool odd = no_page;
+            if (x.limit == 0) {   // an item without tokens: nothing was loaded, and what earlier work has left in LDS, NaN perhaps, does not count
+#pragma unroll
+                for (int i = 0; i < RH * NF; ++i) o[i / NF][i % NF] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
 #pragma unroll
             for (int r = 0; r < RH; ++r) {
                 lsum[r] = query_sum(lsum[r]);

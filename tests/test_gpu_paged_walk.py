@@ -86,3 +86,29 @@ def test_more_rows_together_than_the_batch_has(dtype, n_seqs, n_rows, entries):
     torch.cuda.synchronize()
     assert bool((guard[:, :, :64] == 5).all()) and bool((guard[:, :, 64 + n_rows:] == 5).all()) and bool((ws[need:] == 9).all())
     assert bool((lse[:64] == 5).all()) and bool((lse[64 + n_rows:] == 5).all())
+
+
+@pytest.mark.parametrize("case", [
+    dict(L=4, H=8, G=8, D=128, dtype=BF16, rows=[1] * 40, lens=_idle(40, 100), page=16, prefix=1100, one=True),
+    dict(L=4, H=8, G=8, D=64, dtype=BF16, rows=[1] * 40, lens=_idle(40, 100), page=16, prefix=1100, one=True),
+    dict(L=4, H=8, G=16, D=256, dtype=BF16, rows=[1] * 30, lens=_idle(30, 100), page=32, prefix=1100, one=True),
+    dict(L=4, H=8, G=3, D=128, dtype=BF16, rows=[1, 2, 9] * 10, lens=_idle(30, 100), page=32, prefix=1100),
+    dict(L=4, H=8, G=8, D=128, dtype=F32, rows=[1] * 20, lens=_idle(20, 60), page=16, prefix=200, one=True),
+], ids=lambda c: f"D{c['D']}-{str(c['dtype'])[6:]}-rows{max(c['rows'])}")
+def test_the_same_bits_after_anything(case):
+    """Sequences without tokens behind a prefix: what an earlier launch has left on the chip does not show, not in the last bit either."""
+    c = Case(**case)
+    n = len(c.rows)
+    bad = Case(**{**case, "rows": [1] * n, "lens": [64] * n, "prefix": 0, "one": True})   # fills what the kernels keep there with NaN
+    bad.pages_k.fill_(float("nan")), bad.pages_v.fill_(float("nan"))
+    outs = []
+    for i in range(6):
+        if i % 2:
+            bad.attend()
+        else:
+            torch.zeros((1 << 26,), device="cuda").add_(1)
+            kv.kvcomm_paged_attn(c.model, c.q, torch.zeros_like(c.pages_k), torch.zeros_like(c.pages_v), c.batch)
+        outs.append(c.attend(want_lse=True))
+    for got in outs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got, outs[0]))
+    _close(c, outs[0])
