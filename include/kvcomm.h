@@ -554,7 +554,7 @@ typedef struct {
  *                        are NULL is left out; weights, norm and arithmetic as there, results bit for bit.
  *   first_pos            position of a sequence's token 0: the length of the cache that the sequences continue, or 0.
  * A token that has no page (or lies before its sequence's first, lens[b] < n_b) is not stored; its query is placed.  Slots that no new token has stay as
- * they were.  A slot that two new tokens share holds one of them.
+ * they were.  A slot that two new tokens share (sequences that have a page in common and both write to it) holds, 16 bytes by 16 bytes, either.
  * q_out may be exactly q; any other sharing of bytes between an output and another tensor of the call returns KVCOMM_EINVAL (pools of one shape may lie
  * interleaved in any order, other tensors are compared by whole ranges).  Other errors as for kvcomm_place_qkv; KVCOMM_EINVAL for a batch whose pointers are missing
  * or not 4-byte aligned, whose sizes are not positive or whose positions leave 32 bits.                                                                     */
@@ -571,12 +571,14 @@ int kvcomm_place_qkv_paged(const kvcomm_model *model, kvcomm_tensor q, kvcomm_te
  *                several thread blocks where there are few rows.  Without it (NULL, too small or misaligned) the same result up to rounding, only slower.
  *                Its contents do not matter before the call and are undefined afterwards.
  * Types, arithmetic and softmax_scale as for kvcomm_suffix_attn; a key that a row does not see has no influence on it, whatever it holds (blocks that meet a NaN, an infinity
- * or an entry that is no page are computed again key by key, as in kvcomm_suffix_attn_kv4).  Reproducible: no atomics; a row's sums depend on lens and starts
- * of the whole batch, by the cut of the keys.
+ * or an entry that is no page are computed again key by key, as in kvcomm_suffix_attn_kv4).  Reproducible: no atomics, the same bits from the same call; a row's sums depend,
+ * by the choice of the kernels and the cut of the keys, on lens and starts of the whole batch, the sizes in the structure (table_width, page_size and max_rows among them), n_prefix and whether there
+ * is a workspace.
  * Errors: KVCOMM_EINVAL / KVCOMM_EUNSUPPORTED as above; KVCOMM_EUNSUPPORTED for token strides as in kvcomm_suffix_attn and where the rows or the
  * launch's threads do not fit 31 or 32 bits: from n_rows * Hq * L = 67 000 000 on, or where the halves (32 keys) of all row tiles of one (layer, kv head) may be 2^31, or
  * those of all of them 990 000 000 for each of the launch's wavefronts (1024 to 4096).
- * A NaN that rows see costs much: prompts of 100 to 2000 tokens, 4 layers, with one in every head 1.2 -> 770 ms, a token of 8 sequences, one layer, 20 -> 176 us. */
+ * A NaN that rows see, or an entry below a sequence's length that is no page, costs much: prompts of 100 to 2000 tokens, 4 layers, with a NaN in every head 1.2 -> 770 ms, with the first
+ * entry of every sequence missing 1.4 -> 970 ms; a token of 8 sequences, one layer, 20 -> 176 us and 21 -> 131 us.                                            */
 size_t kvcomm_paged_attn_workspace(const kvcomm_model *model, const kvcomm_batch *batch);
 
 int kvcomm_paged_attn(const kvcomm_model *model, kvcomm_tensor q, kvcomm_pages pages_k, kvcomm_pages pages_v,

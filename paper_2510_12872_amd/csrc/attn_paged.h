@@ -43,7 +43,8 @@ struct PagedAttnParams {
     int32_t *items;            // [layer, kv head][max_items][2]: first and last wavefront of an item; kDirect, kWhole
     int32_t *item_of;          // [n_rows][2]: item of its sequence's first tile, its number in the sequence; kDirect, kWhole: the tiles kernel's
 };
-// A wavefront kernel's parameters, where they are used: what is read once per item is loaded there and not kept in (or spilled from) scalar registers all along.
+// A wavefront kernel's parameters, where they are used: what is read once per item is loaded there and not kept in scalar registers all along.  (There are too few of them all the same: 91 to
+// 121 are spilled, to lanes of vector registers and not to memory, and some read back in the loop over the halves.)
 typedef const __attribute__((address_space(4))) PagedAttnParams PagedArgs;
 __device__ __forceinline__ PagedArgs &paged_args()
 {
@@ -71,7 +72,7 @@ __device__ __forceinline__ void all_rows(const P &p, int &first, int &n)
 // A sequence's tokens from row i of n on: the last one that it sees, -1 or less: none.
 __device__ __forceinline__ int last_seen(int len, int n, int i, int cap) { return min(len - n + i, min(len, cap) - 1); }
 
-// The same parameters, loaded again where they are used from here on: nothing of them is kept in (or spilled from) scalar registers across this.
+// The same parameters, loaded again where they are used from here on: nothing that was read of them before is kept across this.
 template <class P>
 __device__ __forceinline__ P &again(P &p)
 {
@@ -185,8 +186,10 @@ __device__ __forceinline__ void paged_store_row(const P &p, int l, int hq, int r
 }
 
 // ------------------------------------------------------------------------------------------ the walk
-// Halves of runs that are cut within items, at most.  (The shortest run in any case: one half.  One layer, prefix 2560 and 8 tokens, with runs of 1 / 2 / 4 / 8 halves
-// at least: 12.4 / 15.5 / 21.9 / 37.3 us.)
+// Runs of up to so many halves are cut within items.  (What is cut so has up to twice as many: half of the wavefronts may be the items' last ones.)  us for the whole call, D = 128, 8 kv heads, G = 4,
+// cut within items / across them, halves of a run: 8 sequences, one layer, 1.1 16.2 / 16.8, 2.8 22.6 / 23.5, 4.8 34.2 / 34.9, 7.3 45.4 / 46.6, 10.4 61.3 / 61.4, 19 106.8 / 106.9; 32 sequences 1.2 16.5 / 17.3,
+// 4.5 32.4 / 33.5, 8.5 52.4 / 52.9, 18 101.6 / 103.3; fp32 1.9 29.4 / 29.1, 5.5 75.9 / 75.3, 10.3 133.3 / 130.8: longer ones gain 1 % or lose 2.
+// The shortest run in any case is one half: one layer, prefix 2560 and 8 tokens, with runs of 1 / 2 / 4 / 8 halves at least: 12.4 / 15.5 / 21.9 / 37.3 us.
 constexpr int kPagedShortRun = 8;
 // Halves of a run, at most: longer ones are refused before the launch.
 constexpr int kPagedMostRun = 1000000000;
@@ -580,6 +583,8 @@ __device__ __forceinline__ void paged_exact_segment(const P &p0, const PagedItem
 // attn_mfma_kernel (suffix_attn.hip) with Keys::kPaged: a block is a tile of rows and a run of 64-key tiles of one sequence's pages, or of the prefix.
 // What bounds it: the matrix cores with their vector work, as over a whole cache.  4 layers, 6 sequences of 100 to 2000 rows behind up to 6000 tokens (1258 GFLOP)
 // 1.19 ms = 1.05 PFLOP/s, matrix pipes busy in 51 % of the cycles; 32 layers, a prefix of 8192 for 64 rows of each (layer, head) 0.25 ms (54 %).
+// Blocks of 128 rows at D = 128 and those at D = 256 have more values than vector registers: 28 and 48 bytes of scratch memory a lane, of which D = 256 reads some again inside
+// the loop over the tiles.
 // Where a call has both, a sequence's block joins the prefix's parts to its rows at its end: 8 layers, 16 suffixes behind a prefix of 4096, 0.45 ms; with all of
 // them joined by the combine kernel 0.51 (110 us of it there).
 struct PagedTileParams : PagedAttnParams {   // row_o null: rows go to `out`.  Over the prefix: k, v and their strides are the prefix's, one page

@@ -53,7 +53,7 @@ __global__ __launch_bounds__(256) void attn_paged_combine_kernel(const CombinePa
     // A head per lane: which of them are not done (of most large batches nearly all are).
     const int head0 = chunk * p.heads, head = head0 + lane;
     // (W = 4: one, looked at where what lies before its parts has been asked for, too: a way to memory less, 14.2 -> 13.3 us for the
-    // fp32 batch of the tiny configuration)
+    // fp32 batch of the tiny configuration while it took this form)
     for (uint64_t todo = W == 4 ? 1 : __builtin_amdgcn_ballot_w64(lane < p.heads && head < Hq && own_of(min(head, Hq - 1)).wave != kDirect); todo; todo &= todo - 1) {
         const int hq = head0 + __builtin_ctzll(todo), hkv = div_by(hq, p.by_G), g = hq - hkv * p.G;
         const int64_t flat = ((int64_t)l * Hq + hq) * n_rows + row;

@@ -9,7 +9,7 @@ using namespace kvc;
 // operand comes from global memory in the layout the instruction wants (of K and Q 16-byte pieces, piece j of lane (n, g) holding channels 16 * j + 4 * g ... + 3,
 // of V four consecutive channels of one key).  A wavefront is alone and walks 16 keys after the other, which lie in one page; the next ones are requested
 // when this one's operands have been multiplied.  What bounds it: matrix cores where there is much of it (fp32 MFMA, 1/16 of the bf16 rate), else the chain of
-// one wavefront.  2 layers of 4 heads, D = 64, 5 sequences of up to 300 tokens and 33 rows: 8.1 us, the whole call 13.3 (165 with a block
+// one wavefront.  2 layers of 4 heads, D = 64, 5 sequences of up to 300 tokens and 33 rows: 8.1 us, the whole call 12.9 (165 with a block
 // per tile of rows); one layer, 8 heads, 8 sequences of 600 to 3100 tokens at D = 128, one row each, G = 4: the whole call 29 us, 16 by its bytes.
 template <int D>
 __global__ __launch_bounds__(64 * kPagedBlockWaves, D == 256 ? 1 : 2) void attn_paged_f32_kernel(const PagedAttnParams)

@@ -96,7 +96,7 @@ __device__ __forceinline__ void exact_tile()
 // KEYS = kWindow: the block walks the 32-key halves of the sinks, then those of its queries' windows (window_units()), as if they lay behind each other.  The
 // first pairs of tiles, where some query does not see some key, are masked like the last; a block whose results are not all finite computes its
 // rows again by attn_exact_rows(), because a hidden key's value may have been multiplied by its probability 0.
-// FORM: wavefronts per SIMD + form(KEYS) (one argument for both: a whole cache's kernels keep the names that the profiles have).
+// FORM: wavefronts per SIMD + form(KEYS) (one argument for both: a whole cache's kernels keep the template arguments that the profiles know them by).
 constexpr int form(Keys keys) { return 16 * (int)keys; }
 template <int FORM>
 using ParamsOf = std::conditional_t<FORM / 16 == (int)Keys::kPaged, PagedTileParams, AttnParams>;
